@@ -30,6 +30,13 @@
  *                  (paper Sec. 3.3, Eq. 3).
  *   moa_rule_loss  the loss table of candidate rules from that profile
  *                  (paper Sec. 3.3, Eq. 4), input of the rule selection.
+ *   moa_paged_append, moa_paged_prefill, moa_paged_decode,
+ *   moa_paged_decode_shared
+ *                  the same attention over a paged cache: every KV head of
+ *                  every sequence has pages of its own, so that a head with a
+ *                  narrow window gives back what it no longer sees, prompts
+ *                  enter in chunks of any length, and sequences share the
+ *                  pages of a common prefix.
  *
  * Definitions used throughout (s = num_sink, w_g = window of KV head g):
  *   window    w_g = min(max(floor(alpha_g + beta_g * N), 1), N), evaluated
@@ -272,6 +279,98 @@ moa_status_t moa_influence(const moa_desc_t* desc, const void* q, const void* k,
 moa_status_t moa_rule_loss(const float* ebar, int32_t num_heads, int64_t n, int32_t num_sink, uint32_t flags,
                            const double* alpha, const double* beta, int32_t num_rules, double* dl,
                            double* density, void* hip_stream);
+
+/* --------------------------------------------------------------------------
+ * Paged cache.
+ *
+ * A page holds page_size consecutive positions of one KV head: positions
+ * i * page_size .. (i + 1) * page_size - 1 of head g of sequence b are in page
+ * table[b][g][i], rows 0 .. page_size - 1.  A page number outside
+ * [0, num_pages), and a position from max_pages * page_size on, is absent: its
+ * keys are not seen and new tokens there are not stored.  So a caller may take
+ * back the pages of head g that no later query sees (those wholly at positions
+ * >= s and < pos - w_g + 1).  Sequences may share pages that none of them
+ * writes any more; two tokens of one append must not go to the same row.
+ *
+ * The tokens of a call are packed: rows seq_start[b] .. seq_start[b + 1] - 1 of
+ * q, k_new, v_new, o and q_out are sequence b's, at positions positions[b],
+ * positions[b] + 1, ...; a sequence may have none.  seq_start (device int32
+ * [batch + 1]) is non-decreasing; rows in front of seq_start[0] and from
+ * seq_start[batch] on belong to no sequence and are left as they were in o and
+ * q_out.  A negative positions[b] leaves sequence b's rows and pages as they
+ * were.  table and positions live on the device, so a captured graph replays
+ * with their present contents.
+ *
+ * A query at position p of head g sees the keys j <= p with j < s or in its band,
+ * token-exact in the two decode calls and, with MOA_BLOCK_BAND, in blocks in
+ * moa_paged_prefill, as in moa_prefill.  A query that sees no key (all its pages
+ * are absent) gets zeros.  What lies in rows that no query of the call sees is
+ * not looked at; a value row that some query sees has to be finite.
+ * ----------------------------------------------------------------------- */
+typedef struct {
+  void* k_pages;             /* device [num_pages, page_size, head_dim], the plan's type, 16-byte aligned */
+  void* v_pages;
+  const int32_t* table;      /* device [batch, num_kv_heads, max_pages] */
+  int64_t num_pages;         /* >= 1; num_pages * page_size <= 2^31 */
+  int32_t page_size;         /* 16, 32, 64, 128 or 256 */
+  int32_t max_pages;         /* pages per (sequence, head) in the table; max_pages * page_size <= 2^30 */
+} moa_pages_t;
+
+/* Rotation of queries and keys by their positions: dimensions 0 .. rotary_dim - 1
+ * of each head are turned in pairs, pair i by the angle position * inv_freq[i]:
+ * (x, y) -> (x cos - y sin, y cos + x sin).  Pair i is dimensions (i, i +
+ * rotary_dim / 2), or (2 i, 2 i + 1) when interleaved is 1.  Angles are formed in
+ * fp64, products in fp32, rounded once to the plan's type. */
+typedef struct {
+  const float* inv_freq;     /* device [rotary_dim / 2] */
+  int32_t rotary_dim;        /* a multiple of 16, at most head_dim */
+  int32_t interleaved;       /* 0 or 1 */
+} moa_rope_t;
+
+/* Stores n_tokens packed new tokens in the pages, rotated (keys) and as they are
+ * (values), and writes the rotated queries to q_out.  q [n_tokens, num_q_heads,
+ * head_dim], k_new, v_new [n_tokens, num_kv_heads, head_dim] with q_stride,
+ * k_stride, v_stride elements from token to token (heads contiguous; a multiple
+ * of 16 bytes), so that they may be parts of one projection's output; q_out is
+ * contiguous and may be q itself if that is.  q and q_out may both be NULL: only
+ * keys and values.  rope NULL: nothing is rotated (the tokens are, already).
+ * seq_start NULL: one token per sequence (n_tokens == batch).  1 <= batch <= 65535,
+ * 0 <= n_tokens < 2^30 (0 does nothing). */
+moa_status_t moa_paged_append(const moa_plan_t* plan, const moa_pages_t* pages, const void* q, int64_t q_stride,
+                              const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, void* q_out,
+                              const moa_rope_t* rope, const int32_t* positions, const int32_t* seq_start,
+                              int32_t batch, int64_t n_tokens, void* hip_stream);
+
+/* Bytes of device workspace that any of the three calls below needs for `batch`
+ * sequences with n_tokens packed tokens in all (batch of them in the decode
+ * calls).  Returns 0 for a NULL plan, batch < 1 or n_tokens < 1. */
+size_t moa_paged_workspace_bytes(const moa_plan_t* plan, int32_t batch, int64_t n_tokens);
+
+/* Attention of n_tokens packed new tokens over the pages, which already hold them
+ * (moa_paged_append): chunks of prompts of any length, whole prompts, drafted
+ * tokens.  q, o [n_tokens, num_q_heads, head_dim], rotated as the keys are.
+ * The workspace is as in moa_decode: 256-byte aligned, its contents need no
+ * initialisation and mean nothing after the call; calls that share one are ordered
+ * on one stream.  o and the workspace overlap nothing else.  0 <= n_tokens < 2^30
+ * (0 does nothing). */
+moa_status_t moa_paged_prefill(const moa_plan_t* plan, const moa_pages_t* pages, const void* q, void* o,
+                               const int32_t* positions, const int32_t* seq_start, int32_t batch, int64_t n_tokens,
+                               void* workspace, size_t ws_bytes, void* hip_stream);
+
+/* Attention of one token per sequence, at position positions[b], over the pages,
+ * which already hold it.  q, o [batch, num_q_heads, head_dim]. */
+moa_status_t moa_paged_decode(const moa_plan_t* plan, const moa_pages_t* pages, const void* q, void* o,
+                              const int32_t* positions, int32_t batch, void* workspace, size_t ws_bytes,
+                              void* hip_stream);
+
+/* The same for sequences that share their first prefix_len positions: keys j <
+ * prefix_len of head g are read through prefix_table (device int32 [num_kv_heads,
+ * max_pages]) once for the whole batch, keys from prefix_len on through the
+ * table, whose entries in front of that page are not looked at.  A page across the
+ * border is looked up in both.  0 <= prefix_len <= max_pages * page_size. */
+moa_status_t moa_paged_decode_shared(const moa_plan_t* plan, const moa_pages_t* pages, const int32_t* prefix_table,
+                                     int64_t prefix_len, const void* q, void* o, const int32_t* positions,
+                                     int32_t batch, void* workspace, size_t ws_bytes, void* hip_stream);
 
 /* Thread-local message of the calling thread's last non-OK status ("" if none). */
 const char* moa_last_error(void);

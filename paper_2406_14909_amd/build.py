@@ -25,8 +25,9 @@ BINDING_PATH = os.path.join(PKG_DIR, "_binding.so")
 # matrix-core ceilings of the GPU.
 PROBES = ["stream_read", "mfma_loop"]
 
-HIP_SOURCES = ["kv_append.hip", "decode.hip", "prefill.hip", "prefill_f32.hip", "influence.hip", "rule_loss.hip"]
-HOST_SOURCES = ["moa_api.cpp"]
+HIP_SOURCES = ["kv_append.hip", "decode.hip", "prefill.hip", "prefill_f32.hip", "influence.hip", "rule_loss.hip",
+               "paged_append.hip", "paged_attention.hip"]
+HOST_SOURCES = ["moa_api.cpp", "paged_api.cpp"]
 
 ARCH = "gfx950"
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

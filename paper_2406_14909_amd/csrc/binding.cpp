@@ -40,6 +40,10 @@ struct Api {
   decltype(&moa_decode_ragged) decode_ragged;
   decltype(&moa_influence) influence;
   decltype(&moa_rule_loss) rule_loss;
+  decltype(&moa_paged_append) paged_append;
+  decltype(&moa_paged_prefill) paged_prefill;
+  decltype(&moa_paged_decode) paged_decode;
+  decltype(&moa_paged_decode_shared) paged_decode_shared;
 };
 
 // What the checks need of a library and a plan; held by a capsule.
@@ -89,6 +93,19 @@ struct Check {
     const at::Tensor* t = any(o);
     if (t && (t->scalar_type() != type || t->sizes() != shape)) ok = false;
     return ok ? t : nullptr;
+  }
+  // Packed tokens [n, heads, d], contiguous but for the tokens; null where they are
+  // not of this kind.
+  const at::Tensor* tokens(PyObject* o, at::ScalarType type, at::IntArrayRef shape, int64_t* stride) {
+    const at::Tensor* t = ok ? plain(o) : nullptr;
+    if (!t || (device >= 0 && t->device().index() != device) || t->scalar_type() != type || t->sizes() != shape ||
+        t->stride(2) != 1 || (shape[1] > 1 && t->stride(1) != shape[2])) {
+      ok = false;
+      return nullptr;
+    }
+    device = t->device().index();
+    *stride = shape[0] > 1 ? t->stride(0) : shape[1] * shape[2];
+    return t;
   }
   // Tensors checked and the call's device current.
   bool done() const { return ok && device >= 0 && c10::hip::current_device() == device; }
@@ -366,6 +383,159 @@ PyObject* rule_loss(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   MOA_LEAVE
 }
 
+// k_pages, v_pages and table of a paged call of `bsz` sequences.
+moa_pages_t pages_of(const Bound& b, Check& c, PyObject* kp, PyObject* vp, PyObject* table, int64_t bsz) {
+  moa_pages_t p = {};
+  const at::Tensor* k = c.any(kp);
+  const at::Tensor* t = c.any(table);
+  if (!b.plan || !k || !t || k->dim() != 3 || t->dim() != 3) {
+    c.ok = false;
+    return p;
+  }
+  const int64_t np = k->size(0), ps = k->size(1), mp = t->size(2);
+  c(kp, b.dtype, {np, ps, b.d});
+  const at::Tensor* v = c(vp, b.dtype, {np, ps, b.d});
+  c(table, at::kInt, {bsz, b.hkv, mp});
+  if (!c.ok || ps > INT32_MAX || mp > INT32_MAX || bsz > INT32_MAX) {
+    c.ok = false;
+    return p;
+  }
+  p.k_pages = k->data_ptr();
+  p.v_pages = v->data_ptr();
+  p.table = static_cast<const int32_t*>(t->data_ptr());
+  p.num_pages = np;
+  p.page_size = static_cast<int32_t>(ps);
+  p.max_pages = static_cast<int32_t>(mp);
+  return p;
+}
+
+// paged_append(bound, k_pages, v_pages, table, q, k_new, v_new, positions, seq_start, inv_freq, interleaved, q_out)
+PyObject* paged_append(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  MOA_ENTER(12)
+  const at::Tensor* at_ = c.any(args[7]);
+  const at::Tensor* k0 = plain(args[5]);
+  if (!b->plan || !at_ || at_->dim() != 1 || !k0 || k0->dim() != 3 || !PyBool_Check(args[10])) return none();
+  const int64_t bsz = at_->size(0), n = k0->size(0);
+  c(args[7], at::kInt, {bsz});
+  const moa_pages_t pages = pages_of(*b, c, args[1], args[2], args[3], bsz);
+  int64_t qs = 0, ks = 0, vs = 0;
+  const at::Tensor* k = c.tokens(args[5], b->dtype, {n, b->hkv, b->d}, &ks);
+  const at::Tensor* v = c.tokens(args[6], b->dtype, {n, b->hkv, b->d}, &vs);
+  const bool with_q = args[4] != Py_None;
+  const at::Tensor* q = with_q ? c.tokens(args[4], b->dtype, {n, b->hq, b->d}, &qs) : nullptr;
+  const at::Tensor* ss = args[8] != Py_None ? c(args[8], at::kInt, {bsz + 1}) : nullptr;
+  const at::Tensor* f = args[9] != Py_None ? c.any(args[9]) : nullptr;
+  if (!c.done() || (f && (f->dim() != 1 || f->scalar_type() != at::kFloat || f->size(0) > INT32_MAX / 2)))
+    return none();
+  at::Tensor fresh;
+  const at::Tensor* out = &fresh;
+  if (!with_q) {
+    if (args[11] != Py_None) return none();
+  } else if (args[11] == Py_None) {
+    fresh = at::empty({n, b->hq, b->d}, q->options());
+  } else {
+    out = c(args[11], b->dtype, {n, b->hq, b->d});
+  }
+  if (!c.done()) return none();
+  moa_rope_t rope = {};
+  if (f) {
+    rope.inv_freq = static_cast<const float*>(f->data_ptr());
+    rope.rotary_dim = static_cast<int32_t>(2 * f->size(0));
+    rope.interleaved = args[10] == Py_True;
+  }
+  void *pq = with_q ? q->data_ptr() : nullptr, *po = with_q ? out->data_ptr() : nullptr;
+  void *pk = k->data_ptr(), *pv = v->data_ptr(), *s = c.stream();
+  const int32_t* pp = static_cast<const int32_t*>(at_->data_ptr());
+  const int32_t* ps = ss ? static_cast<const int32_t*>(ss->data_ptr()) : nullptr;
+  if (!call(*b, [&] {
+        return b->api.paged_append(b->plan, &pages, pq, qs, pk, ks, pv, vs, po, f ? &rope : nullptr, pp, ps,
+                                   static_cast<int32_t>(bsz), n, s);
+      }))
+    return nullptr;
+  if (!with_q) Py_RETURN_TRUE;
+  return args[11] == Py_None ? THPVariable_Wrap(fresh) : same(args[11]);
+  MOA_LEAVE
+}
+
+// q, pages, positions, workspace and o of a paged attention call
+struct PagedTensors {
+  const at::Tensor *q, *ps = nullptr, *w = nullptr;
+  moa_pages_t pages = {};
+  int64_t n = 0, bsz = 0;
+  // one_each: one token per sequence
+  PagedTensors(const Bound& b, Check& c, PyObject* oq, PyObject* kp, PyObject* vp, PyObject* table, PyObject* pos,
+               PyObject* work, bool one_each)
+      : q(c.any(oq)) {
+    ps = c.any(pos);
+    if (!b.plan || !q || !ps || q->dim() != 3 || ps->dim() != 1) {
+      c.ok = false;
+      return;
+    }
+    n = q->size(0);
+    bsz = ps->size(0);
+    c(oq, b.dtype, {one_each ? bsz : n, b.hq, b.d});
+    c(pos, at::kInt, {bsz});
+    pages = pages_of(b, c, kp, vp, table, bsz);
+    w = c.any(work);
+  }
+  const int32_t* positions() const { return static_cast<const int32_t*>(ps->data_ptr()); }
+};
+
+// paged_prefill(bound, q, k_pages, v_pages, table, positions, seq_start, workspace, o)
+PyObject* paged_prefill(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  MOA_ENTER(9)
+  const PagedTensors t(*b, c, args[1], args[2], args[3], args[4], args[5], args[7], false);
+  const at::Tensor* ss = c(args[6], at::kInt, {t.bsz + 1});
+  Out o(args[8], t.q, c);
+  if (!c.done() || !o.t) return none();
+  void *pq = t.q->data_ptr(), *po = o.t->data_ptr(), *pw = t.w->data_ptr(), *s = c.stream();
+  const int32_t* ps = static_cast<const int32_t*>(ss->data_ptr());
+  const size_t nw = t.w->nbytes();
+  if (!call(*b, [&] {
+        return b->api.paged_prefill(b->plan, &t.pages, pq, po, t.positions(), ps, static_cast<int32_t>(t.bsz), t.n, pw, nw, s);
+      }))
+    return nullptr;
+  return o.answer();
+  MOA_LEAVE
+}
+
+// paged_decode(bound, q, k_pages, v_pages, table, positions, workspace, o)
+PyObject* paged_decode(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  MOA_ENTER(8)
+  const PagedTensors t(*b, c, args[1], args[2], args[3], args[4], args[5], args[6], true);
+  Out o(args[7], t.q, c);
+  if (!c.done() || !o.t) return none();
+  void *pq = t.q->data_ptr(), *po = o.t->data_ptr(), *pw = t.w->data_ptr(), *s = c.stream();
+  const size_t nw = t.w->nbytes();
+  if (!call(*b, [&] {
+        return b->api.paged_decode(b->plan, &t.pages, pq, po, t.positions(), static_cast<int32_t>(t.bsz), pw, nw, s);
+      }))
+    return nullptr;
+  return o.answer();
+  MOA_LEAVE
+}
+
+// paged_decode_shared(bound, q, k_pages, v_pages, prefix_table, prefix_len, table, positions, workspace, o)
+PyObject* paged_decode_shared(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  MOA_ENTER(10)
+  int64_t len;
+  if (!as_int(args[5], &len)) return none();
+  const PagedTensors t(*b, c, args[1], args[2], args[3], args[6], args[7], args[8], true);
+  const at::Tensor* pre = c(args[4], at::kInt, {b->hkv, int64_t(t.pages.max_pages)});
+  Out o(args[9], t.q, c);
+  if (!c.done() || !o.t) return none();
+  void *pq = t.q->data_ptr(), *po = o.t->data_ptr(), *pw = t.w->data_ptr(), *s = c.stream();
+  const int32_t* pp = static_cast<const int32_t*>(pre->data_ptr());
+  const size_t nw = t.w->nbytes();
+  if (!call(*b, [&] {
+        return b->api.paged_decode_shared(b->plan, &t.pages, pp, len, pq, po, t.positions(), static_cast<int32_t>(t.bsz), pw,
+                                          nw, s);
+      }))
+    return nullptr;
+  return o.answer();
+  MOA_LEAVE
+}
+
 // bind(addresses of the entry points, plan address or 0, num_q_heads, num_kv_heads, head_dim, cache rows, is bf16,
 //      function that raises for a status)
 PyObject* bind(PyObject*, PyObject* args) {
@@ -406,7 +576,8 @@ PyObject* bind(PyObject*, PyObject* args) {
 #define MOA_FAST(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {
     MOA_FAST(prefill), MOA_FAST(kv_append), MOA_FAST(kv_append_ragged), MOA_FAST(decode), MOA_FAST(decode_noalloc),
-    MOA_FAST(decode_ragged), MOA_FAST(influence), MOA_FAST(rule_loss), {"bind", bind, METH_VARARGS, nullptr},
+    MOA_FAST(decode_ragged), MOA_FAST(influence), MOA_FAST(rule_loss), MOA_FAST(paged_append), MOA_FAST(paged_prefill),
+    MOA_FAST(paged_decode), MOA_FAST(paged_decode_shared), {"bind", bind, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

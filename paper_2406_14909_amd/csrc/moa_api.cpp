@@ -80,15 +80,6 @@ static int64_t rule_window(double alpha, double beta, int64_t n, int32_t num_sin
   return static_cast<int64_t>(floor(x));
 }
 
-static bool aligned16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15u) == 0; }
-
-static bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + nb && y < x + na;
-}
-
-static size_t elem_size(const moa_plan_s& p) { return p.desc.dtype == MOA_BF16 ? 2 : 4; }
-
 // Decode writes o and `ws_need` bytes of the workspace; true when either
 // overlaps another argument (or the other written buffer).
 static bool decode_overlap(const moa_plan_s& p, const void* q, const void* kc, const void* vc, const void* o,

@@ -27,6 +27,14 @@ namespace moa {
 moa_status_t fail(moa_status_t st, const std::string& msg);
 moa_status_t ok();
 
+// Checks of pointer arguments.
+inline bool aligned16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15u) == 0; }
+inline bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + nb && y < x + na;
+}
+inline size_t elem_size(const moa_plan_s& p) { return p.desc.dtype == MOA_BF16 ? 2 : 4; }
+
 // ---------------------------------------------------------------------------
 // Kernel argument blocks (passed by value; the per-head tables ride along).
 // ---------------------------------------------------------------------------

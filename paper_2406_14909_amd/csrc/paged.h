@@ -1,0 +1,100 @@
+// Arguments and key arithmetic of the paged entry points, shared by the host and the
+// kernels.  Plain C++, so that it also compiles without a GPU toolchain.
+#pragma once
+
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "moa_internal.h"
+
+#if defined(__HIPCC__)
+#include <hip/hip_runtime.h>
+#define MOA_PAGED_FN __host__ __device__ __forceinline__
+#else
+#define MOA_PAGED_FN inline
+#endif
+
+namespace moa {
+
+constexpr int kMinPageShift = 4;         // 16 positions: the rows that a wave of a tile load covers
+constexpr int kMaxPageShift = 8;
+constexpr int64_t kMaxPosition = int64_t(1) << 30;
+constexpr int64_t kMaxPageRows = int64_t(1) << 31;   // rows of a page pool
+
+// New tokens into the pages, rotated on the way.
+struct PagedAppendArgs {
+  const void* q;             // null: only keys and values
+  const void* kn;
+  const void* vn;
+  void* q_out;
+  void* kp;
+  void* vp;
+  const int32_t* table;      // [batch, hkv, max_pages]
+  const int32_t* positions;  // [batch]
+  const int32_t* seq_start;  // [batch + 1], or null: one token per sequence
+  const float* inv_freq;     // [rotary / 2]
+  int64_t q_stride;          // bytes from token to token
+  int64_t k_stride;
+  int64_t v_stride;
+  int32_t n_tokens;
+  int32_t batch;
+  int32_t hq;                // 0 without queries
+  int32_t hkv;
+  int32_t num_pages;
+  int32_t page_shift;
+  int32_t max_pages;
+  int32_t rotary;            // 0: nothing is rotated
+  int32_t interleaved;
+};
+
+// Attention over the pages.
+struct PagedArgs {
+  const void* q;
+  void* o;
+  const void* kp;
+  const void* vp;
+  const int32_t* table;
+  const int32_t* prefix_table;   // [hkv, max_pages] of the keys in front of prefix_len, or null
+  const int32_t* positions;
+  const int32_t* seq_start;      // null: one token per sequence
+  float* part;
+  int32_t n_tokens;
+  int32_t batch;
+  int32_t hq;
+  int32_t hkv;
+  int32_t num_pages;
+  int32_t page_shift;
+  int32_t max_pages;
+  int32_t num_sink;
+  int32_t prefix_len;
+  int32_t band_shift;            // the band of position i starts at ((i >> shift) - window + 1) << shift
+  float scale_log2;
+  int32_t window[MOA_MAX_KV_HEADS];
+};
+
+// Keys of one query position, as a run of sinks and a band behind them, both cut at
+// `from` (keys in front of it are read elsewhere) and at the end of the table.  Key x
+// of the `count` visible ones, counted from 0, is at position at(x).
+struct VisibleKeys {
+  int32_t from, sinks, band, count;
+  MOA_PAGED_FN int32_t at(int32_t x) const { return x < sinks ? from + x : band + (x - sinks); }
+};
+MOA_PAGED_FN VisibleKeys visible_keys(int32_t pos, int32_t window, int32_t band_shift, int32_t num_sink, int32_t from,
+                                      int32_t capacity) {
+  const int32_t end = pos < capacity ? pos + 1 : capacity;
+  VisibleKeys v;
+  v.from = from;
+  const int32_t s = num_sink < end ? num_sink : end;
+  v.sinks = s > from ? s - from : 0;
+  const int32_t first = ((pos >> band_shift) - window + 1) * (1 << band_shift);
+  const int32_t low = num_sink > from ? num_sink : from;
+  v.band = first > low ? first : low;
+  v.count = v.sinks + (end > v.band ? end - v.band : 0);
+  return v;
+}
+
+int launch_paged_append(const PagedAppendArgs& a, int dtype, int head_dim, void* stream);
+int launch_paged_attention(const PagedArgs& a, int dtype, int head_dim, void* stream);
+
+}  // namespace moa

@@ -1,0 +1,242 @@
+// Host side of the paged entry points: argument checks and dispatch to the launchers.
+#include <string.h>
+
+#include <algorithm>
+#include <string>
+
+#include "moa_internal.h"
+#include "paged.h"
+
+namespace moa {
+
+namespace {
+
+constexpr int kMaxBatch = 65535;
+
+moa_status_t invalid(const char* who, const char* what) {
+  return fail(MOA_ERR_INVALID_ARG, std::string(who) + ": " + what);
+}
+
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+size_t pool_bytes(const moa_plan_s& p, const moa_pages_t& pages) {
+  return elem_size(p) * static_cast<size_t>(pages.num_pages) * pages.page_size * p.desc.head_dim;
+}
+
+size_t rows_bytes(const moa_plan_s& p, int64_t n, int heads) {
+  return elem_size(p) * static_cast<size_t>(n) * heads * p.desc.head_dim;
+}
+
+moa_status_t check_pages(const char* who, const moa_plan_t* plan, const moa_pages_t* pages, const int32_t* positions,
+                         int32_t batch, int64_t n_tokens) {
+  if (!plan || !pages) return invalid(who, "null plan or pages");
+  if (!pages->k_pages || !pages->v_pages || !pages->table || !positions) return invalid(who, "null pointer");
+  if (!aligned16(pages->k_pages) || !aligned16(pages->v_pages) || !aligned4(pages->table) || !aligned4(positions))
+    return invalid(who, "pages must be 16-byte aligned, table and positions 4-byte");
+  const int32_t ps = pages->page_size;
+  if (ps < (1 << kMinPageShift) || ps > (1 << kMaxPageShift) || (ps & (ps - 1)) != 0)
+    return fail(MOA_ERR_UNSUPPORTED, std::string(who) + ": page_size must be 16, 32, 64, 128 or 256");
+  if (pages->num_pages < 1 || pages->num_pages > kMaxPageRows / ps)
+    return invalid(who, "need num_pages >= 1 and num_pages * page_size <= 2^31");
+  if (pages->max_pages < 1 || pages->max_pages > kMaxPosition / ps)
+    return invalid(who, "need max_pages >= 1 and max_pages * page_size <= 2^30");
+  if (batch < 1 || batch > kMaxBatch) return invalid(who, "batch must be in [1, 65535]");
+  if (n_tokens < 0 || n_tokens >= (int64_t(1) << 30)) return invalid(who, "n_tokens must be in [0, 2^30)");
+  const size_t pool = pool_bytes(*plan, *pages);
+  if (overlaps(pages->k_pages, pool, pages->v_pages, pool)) return invalid(who, "k_pages overlaps v_pages");
+  return MOA_OK;
+}
+
+int page_shift(const moa_pages_t& pages) { return __builtin_ctz(static_cast<unsigned>(pages.page_size)); }
+
+// Checks the arguments that the three attention calls have in common and fills in
+// those of the kernels.
+moa_status_t attention_args(const char* who, const moa_plan_t* plan, const moa_pages_t* pages, const void* q, void* o,
+                            const int32_t* positions, int32_t batch, int64_t n_tokens, void* workspace, size_t ws_bytes,
+                            PagedArgs* a) {
+  const moa_status_t st = check_pages(who, plan, pages, positions, batch, n_tokens);
+  if (st != MOA_OK) return st;
+  if (!q || !o) return invalid(who, "null tensor pointer");
+  if (!aligned16(q) || !aligned16(o)) return invalid(who, "tensors must be 16-byte aligned");
+  const moa_plan_s& p = *plan;
+  const moa_desc_t& d = p.desc;
+  const size_t need = moa_paged_workspace_bytes(plan, batch, n_tokens);
+  if (!workspace || ws_bytes < need)
+    return fail(MOA_ERR_WORKSPACE, std::string(who) + ": workspace missing or smaller than moa_paged_workspace_bytes (" +
+                                       std::to_string(need) + " bytes)");
+  if (reinterpret_cast<uintptr_t>(workspace) & 255u)
+    return fail(MOA_ERR_WORKSPACE, std::string(who) + ": workspace must be 256-byte aligned");
+  const size_t qb = rows_bytes(p, n_tokens, d.num_q_heads), pool = pool_bytes(p, *pages);
+  const size_t tb = sizeof(int32_t) * static_cast<size_t>(batch) * d.num_kv_heads * pages->max_pages;
+  const struct { const void* p; size_t n; } reads[] = {
+      {q, qb}, {pages->k_pages, pool}, {pages->v_pages, pool}, {pages->table, tb}, {positions, sizeof(int32_t) * batch}};
+  for (const auto& r : reads)
+    if (overlaps(o, qb, r.p, r.n) || overlaps(workspace, need, r.p, r.n))
+      return invalid(who, "o or the workspace overlaps another argument");
+  if (overlaps(o, qb, workspace, need)) return invalid(who, "o overlaps the workspace");
+  memset(a, 0, sizeof(*a));
+  a->q = q; a->o = o; a->kp = pages->k_pages; a->vp = pages->v_pages;
+  a->table = pages->table;
+  a->positions = positions;
+  a->part = static_cast<float*>(workspace);
+  a->n_tokens = static_cast<int32_t>(n_tokens);
+  a->batch = batch;
+  a->hq = d.num_q_heads;
+  a->hkv = d.num_kv_heads;
+  a->num_pages = static_cast<int32_t>(std::min<int64_t>(pages->num_pages, INT32_MAX));
+  a->page_shift = page_shift(*pages);
+  a->max_pages = pages->max_pages;
+  a->num_sink = d.num_sink;
+  a->scale_log2 = p.scale * 1.4426950408889634f;
+  for (int h = 0; h < d.num_kv_heads; ++h) a->window[h] = p.window[h];
+  return MOA_OK;
+}
+
+moa_status_t launched(const char* who, int err) {
+  if (err == kGridTooLarge) return fail(MOA_ERR_UNSUPPORTED, std::string(who) + ": too much work for one launch");
+  if (err) return fail(MOA_ERR_HIP, std::string(who) + ": kernel launch failed (hipError " + std::to_string(err) + ")");
+  return ok();
+}
+
+}  // namespace
+
+}  // namespace moa
+
+using namespace moa;
+
+extern "C" {
+
+moa_status_t moa_paged_append(const moa_plan_t* plan, const moa_pages_t* pages, const void* q, int64_t q_stride,
+                              const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, void* q_out,
+                              const moa_rope_t* rope, const int32_t* positions, const int32_t* seq_start,
+                              int32_t batch, int64_t n_tokens, void* hip_stream) {
+  const char* who = "moa_paged_append";
+  const moa_status_t st = check_pages(who, plan, pages, positions, batch, n_tokens);
+  if (st != MOA_OK) return st;
+  if (!seq_start && n_tokens != batch) return invalid(who, "without seq_start there is one token per sequence");
+  if (n_tokens == 0) return ok();
+  if (!k_new || !v_new || !q != !q_out) return invalid(who, "null tensor pointer");
+  if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(q_out) || !aligned4(seq_start))
+    return invalid(who, "tensors must be 16-byte aligned (seq_start 4-byte)");
+  const moa_desc_t& d = plan->desc;
+  const int64_t es = static_cast<int64_t>(elem_size(*plan));
+  const int64_t q_row = int64_t(d.num_q_heads) * d.head_dim, k_row = int64_t(d.num_kv_heads) * d.head_dim;
+  // a token's heads are contiguous; tokens do not run into each other
+  const struct { int64_t stride, row; } rows[] = {{q ? q_stride : q_row, q_row}, {k_stride, k_row}, {v_stride, k_row}};
+  for (const auto& r : rows)
+    if (r.stride < r.row || r.stride > (int64_t(1) << 40) || r.stride * es % 16 != 0)
+      return invalid(who, "a token stride is smaller than a token or no multiple of 16 bytes");
+  if (rope) {
+    if (!rope->inv_freq || !aligned4(rope->inv_freq)) return invalid(who, "null or misaligned inv_freq");
+    if (rope->rotary_dim < 16 || rope->rotary_dim > d.head_dim || rope->rotary_dim % 16 != 0)
+      return fail(MOA_ERR_UNSUPPORTED, "moa_paged_append: rotary_dim must be a multiple of 16, at most head_dim");
+    if (rope->interleaved != 0 && rope->interleaved != 1) return invalid(who, "interleaved must be 0 or 1");
+  }
+  const size_t pool = pool_bytes(*plan, *pages);
+  const size_t qb = static_cast<size_t>(((n_tokens - 1) * (q ? q_stride : q_row) + q_row) * es);
+  const size_t kb = static_cast<size_t>(((n_tokens - 1) * k_stride + k_row) * es);
+  const size_t vb = static_cast<size_t>(((n_tokens - 1) * v_stride + k_row) * es);
+  const size_t ob = rows_bytes(*plan, n_tokens, d.num_q_heads);
+  const size_t tb = sizeof(int32_t) * static_cast<size_t>(batch) * d.num_kv_heads * pages->max_pages;
+  const struct { const void* p; size_t n; } reads[] = {
+      {k_new, kb}, {v_new, vb}, {pages->table, tb}, {positions, sizeof(int32_t) * batch},
+      {seq_start, seq_start ? sizeof(int32_t) * (batch + 1) : 0},
+      {rope ? rope->inv_freq : nullptr, rope ? sizeof(float) * (rope->rotary_dim / 2) : 0}};
+  for (const void* pages_of : {static_cast<const void*>(pages->k_pages), static_cast<const void*>(pages->v_pages)}) {
+    for (const auto& r : reads)
+      if (r.n && overlaps(pages_of, pool, r.p, r.n)) return invalid(who, "the pages overlap another argument");
+    if (q && (overlaps(pages_of, pool, q, qb) || overlaps(pages_of, pool, q_out, ob)))
+      return invalid(who, "the pages overlap another argument");
+  }
+  if (q) {
+    for (const auto& r : reads)
+      if (r.n && overlaps(q_out, ob, r.p, r.n)) return invalid(who, "q_out overlaps another argument");
+    if (overlaps(q_out, ob, q, qb) && !(q_out == q && q_stride == q_row))
+      return invalid(who, "q_out overlaps q without being q");
+  }
+  PagedAppendArgs a;
+  memset(&a, 0, sizeof(a));
+  a.q = q; a.kn = k_new; a.vn = v_new; a.q_out = q_out;
+  a.kp = pages->k_pages; a.vp = pages->v_pages; a.table = pages->table;
+  a.positions = positions;
+  a.seq_start = seq_start;
+  a.q_stride = q_stride * es;
+  a.k_stride = k_stride * es;
+  a.v_stride = v_stride * es;
+  a.n_tokens = static_cast<int32_t>(n_tokens);
+  a.batch = batch;
+  a.hq = q ? d.num_q_heads : 0;
+  a.hkv = d.num_kv_heads;
+  a.num_pages = static_cast<int32_t>(std::min<int64_t>(pages->num_pages, INT32_MAX));
+  a.page_shift = page_shift(*pages);
+  a.max_pages = pages->max_pages;
+  if (rope) {
+    a.inv_freq = rope->inv_freq;
+    a.rotary = rope->rotary_dim;
+    a.interleaved = rope->interleaved;
+  }
+  return launched(who, launch_paged_append(a, d.dtype, d.head_dim, hip_stream));
+}
+
+size_t moa_paged_workspace_bytes(const moa_plan_t* plan, int32_t batch, int64_t n_tokens) {
+  if (!plan || batch < 1 || n_tokens < 1) return 0;
+  return 256;
+}
+
+moa_status_t moa_paged_prefill(const moa_plan_t* plan, const moa_pages_t* pages, const void* q, void* o,
+                               const int32_t* positions, const int32_t* seq_start, int32_t batch, int64_t n_tokens,
+                               void* workspace, size_t ws_bytes, void* hip_stream) {
+  const char* who = "moa_paged_prefill";
+  PagedArgs a;
+  if (n_tokens == 0) {
+    const moa_status_t none = check_pages(who, plan, pages, positions, batch, 0);
+    return none != MOA_OK ? none : seq_start ? ok() : invalid(who, "null or misaligned seq_start");
+  }
+  const moa_status_t st = attention_args(who, plan, pages, q, o, positions, batch, n_tokens, workspace, ws_bytes, &a);
+  if (st != MOA_OK) return st;
+  if (!seq_start || !aligned4(seq_start)) return invalid(who, "null or misaligned seq_start");
+  const moa_desc_t& d = plan->desc;
+  const size_t sb = sizeof(int32_t) * (static_cast<size_t>(batch) + 1);
+  if (overlaps(o, rows_bytes(*plan, n_tokens, d.num_q_heads), seq_start, sb) ||
+      overlaps(workspace, moa_paged_workspace_bytes(plan, batch, n_tokens), seq_start, sb))
+    return invalid(who, "o or the workspace overlaps seq_start");
+  a.seq_start = seq_start;
+  if (d.flags & MOA_BLOCK_BAND) {
+    a.band_shift = 6;
+    static_assert(MOA_BAND_BLOCK == 64, "band_shift is log2(MOA_BAND_BLOCK)");
+    for (int h = 0; h < d.num_kv_heads; ++h) a.window[h] = (a.window[h] + MOA_BAND_BLOCK - 1) / MOA_BAND_BLOCK;
+  }
+  return launched(who, launch_paged_attention(a, d.dtype, d.head_dim, hip_stream));
+}
+
+moa_status_t moa_paged_decode(const moa_plan_t* plan, const moa_pages_t* pages, const void* q, void* o,
+                              const int32_t* positions, int32_t batch, void* workspace, size_t ws_bytes,
+                              void* hip_stream) {
+  const char* who = "moa_paged_decode";
+  PagedArgs a;
+  const moa_status_t st = attention_args(who, plan, pages, q, o, positions, batch, batch, workspace, ws_bytes, &a);
+  if (st != MOA_OK) return st;
+  return launched(who, launch_paged_attention(a, plan->desc.dtype, plan->desc.head_dim, hip_stream));
+}
+
+moa_status_t moa_paged_decode_shared(const moa_plan_t* plan, const moa_pages_t* pages, const int32_t* prefix_table,
+                                     int64_t prefix_len, const void* q, void* o, const int32_t* positions,
+                                     int32_t batch, void* workspace, size_t ws_bytes, void* hip_stream) {
+  const char* who = "moa_paged_decode_shared";
+  PagedArgs a;
+  const moa_status_t st = attention_args(who, plan, pages, q, o, positions, batch, batch, workspace, ws_bytes, &a);
+  if (st != MOA_OK) return st;
+  if (!prefix_table || !aligned4(prefix_table)) return invalid(who, "null or misaligned prefix_table");
+  if (prefix_len < 0 || prefix_len > int64_t(pages->max_pages) * pages->page_size)
+    return invalid(who, "prefix_len must be in [0, max_pages * page_size]");
+  const moa_desc_t& d = plan->desc;
+  const size_t pb = sizeof(int32_t) * static_cast<size_t>(d.num_kv_heads) * pages->max_pages;
+  if (overlaps(o, rows_bytes(*plan, batch, d.num_q_heads), prefix_table, pb) ||
+      overlaps(workspace, moa_paged_workspace_bytes(plan, batch, batch), prefix_table, pb))
+    return invalid(who, "o or the workspace overlaps prefix_table");
+  a.prefix_table = prefix_table;
+  a.prefix_len = static_cast<int32_t>(prefix_len);
+  return launched(who, launch_paged_attention(a, d.dtype, d.head_dim, hip_stream));
+}
+
+}  // extern "C"

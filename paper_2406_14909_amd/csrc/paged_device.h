@@ -1,0 +1,42 @@
+// Device helpers of the paged kernels.
+#pragma once
+
+#include "moa_device.h"
+#include "paged.h"
+
+namespace moa {
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// The sequence of packed row t: the last b with seq_start[b] <= t, or -1 where no
+// sequence has the row.  All lanes of the wave search together, 64 probes per trip to
+// memory; whatever seq_start holds, only its batch + 1 entries are read.
+__device__ __forceinline__ int sequence_of(const int32_t* seq_start, int batch, int t) {
+  const int lane = threadIdx.x & 63;
+  int b = 0, n = batch;
+  while (true) {
+    const int stride = (n + 63) >> 6;
+    const bool below = lane * stride < n && seq_start[b + lane * stride] <= t;
+    const int c = __builtin_popcountll(__ballot(below));
+    if (c == 0) return -1;
+    b += (c - 1) * stride;
+    n = min(stride, n - (c - 1) * stride);
+    if (stride == 1) break;
+  }
+  b = uniform(b);
+  return t < seq_start[b + 1] ? b : -1;
+}
+
+// Position of packed row t of sequence b, negative for an idle sequence.
+__device__ __forceinline__ int token_position(const int32_t* positions, const int32_t* seq_start, int b, int t) {
+  const int p0 = positions[b];
+  if (p0 < 0 || seq_start == nullptr) return p0;
+  return static_cast<int>(min(int64_t(p0) + t - seq_start[b], int64_t(0x7fffffff)));
+}
+
+// First row of a page in the pool, or -1 where the page is absent.
+__device__ __forceinline__ int page_row(int page, int num_pages, int page_shift) {
+  return static_cast<uint32_t>(page) < static_cast<uint32_t>(num_pages) ? page << page_shift : -1;
+}
+
+}  // namespace moa

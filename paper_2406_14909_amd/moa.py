@@ -31,6 +31,8 @@ EXPORTED = (
     "moa_plan", "moa_plan_tables", "moa_plan_free", "moa_prefill", "moa_kv_append",
     "moa_decode_workspace_bytes", "moa_decode", "moa_last_error", "moa_kv_append_ragged",
     "moa_decode_ragged", "moa_influence", "moa_rule_loss", "moa_decode_noalloc",
+    "moa_paged_append", "moa_paged_workspace_bytes", "moa_paged_prefill", "moa_paged_decode",
+    "moa_paged_decode_shared",
 )
 
 
@@ -48,6 +50,25 @@ class moa_desc_t(ctypes.Structure):
     ]
 
 
+class moa_pages_t(ctypes.Structure):
+    _fields_ = [
+        ("k_pages", ctypes.c_void_p),
+        ("v_pages", ctypes.c_void_p),
+        ("table", ctypes.c_void_p),
+        ("num_pages", ctypes.c_int64),
+        ("page_size", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32),
+    ]
+
+
+class moa_rope_t(ctypes.Structure):
+    _fields_ = [
+        ("inv_freq", ctypes.c_void_p),
+        ("rotary_dim", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+    ]
+
+
 MOA_SPAN_INCLUDES_SINKS = 1
 MOA_BLOCK_BAND = 2
 MOA_BAND_BLOCK = 64
@@ -61,7 +82,8 @@ class MoaError(RuntimeError):
 
 # Entry points that the native call path takes, in the order of its table.
 _NATIVE = ("moa_prefill", "moa_kv_append", "moa_decode", "moa_decode_noalloc", "moa_kv_append_ragged",
-           "moa_decode_ragged", "moa_influence", "moa_rule_loss")
+           "moa_decode_ragged", "moa_influence", "moa_rule_loss", "moa_paged_append", "moa_paged_prefill",
+           "moa_paged_decode", "moa_paged_decode_shared")
 
 _lib = None
 _fast = None        # the native call path (_binding), loaded with the library
@@ -108,6 +130,17 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.moa_rule_loss.argtypes = [vp, i32, i64, i32, ctypes.c_uint32, ctypes.POINTER(ctypes.c_double),
                                   ctypes.POINTER(ctypes.c_double), i32, vp, vp, vp]
     lib.moa_rule_loss.restype = ctypes.c_int
+    pages, rope = ctypes.POINTER(moa_pages_t), ctypes.POINTER(moa_rope_t)
+    lib.moa_paged_append.argtypes = [vp, pages, vp, i64, vp, i64, vp, i64, vp, rope, vp, vp, i32, i64, vp]
+    lib.moa_paged_append.restype = ctypes.c_int
+    lib.moa_paged_workspace_bytes.argtypes = [vp, i32, i64]
+    lib.moa_paged_workspace_bytes.restype = ctypes.c_size_t
+    lib.moa_paged_prefill.argtypes = [vp, pages, vp, vp, vp, vp, i32, i64, vp, ctypes.c_size_t, vp]
+    lib.moa_paged_prefill.restype = ctypes.c_int
+    lib.moa_paged_decode.argtypes = [vp, pages, vp, vp, vp, i32, vp, ctypes.c_size_t, vp]
+    lib.moa_paged_decode.restype = ctypes.c_int
+    lib.moa_paged_decode_shared.argtypes = [vp, pages, vp, i64, vp, vp, vp, i32, vp, ctypes.c_size_t, vp]
+    lib.moa_paged_decode_shared.restype = ctypes.c_int
     lib.moa_last_error.argtypes = []
     lib.moa_last_error.restype = ctypes.c_char_p
     from . import _binding
@@ -444,3 +477,187 @@ def moa_rule_loss(ebar, n: int, num_sink: int, alpha, beta, flags: int = 0, stre
                                             dl.data_ptr(), dens.data_ptr(), _stream(ebar, stream)))
     return dl, dens
 
+
+
+# ---------------------------------------------------------------------------
+# Paged cache: k_pages, v_pages [num_pages, page_size, D]; a page holds page_size
+# consecutive positions of one KV head, table[b, g, i] (int32, GPU) is the page of
+# positions i * page_size .. of head g of sequence b, and a number outside
+# [0, num_pages) an absent one.  See include/moa.h.
+# ---------------------------------------------------------------------------
+def new_paged_cache(plan: Plan, num_pages: int, page_size: int = 64, device="cuda"):
+    """(k_pages, v_pages) of `num_pages` pages; which page holds what is the caller's to say, in the table."""
+    import torch
+    shape = (int(num_pages), int(page_size), plan.head_dim)
+    return (torch.zeros(shape, dtype=plan.torch_dtype, device=device),
+            torch.zeros(shape, dtype=plan.torch_dtype, device=device))
+
+
+def moa_paged_workspace_bytes(plan: Plan, batch: int, n_tokens: int) -> int:
+    return int(load_library().moa_paged_workspace_bytes(plan.handle, int(batch), int(n_tokens)))
+
+
+def new_paged_workspace(plan: Plan, batch: int, n_tokens: Optional[int] = None, device="cuda"):
+    """Workspace for paged calls of up to `batch` sequences with up to `n_tokens` packed tokens
+    in all (one each if not given); its contents need no initialisation."""
+    import torch
+    nbytes = max(256, moa_paged_workspace_bytes(plan, batch, batch if n_tokens is None else n_tokens))
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def _need_rank(t, rank, name):
+    if t.dim() != rank:
+        raise MoaError(MOA_ERR_INVALID_ARG, f"{name}: expected {rank} dimensions, got shape {tuple(t.shape)}")
+
+
+def _pages(plan: Plan, k_pages, v_pages, table, bsz):
+    import torch
+    _need_rank(k_pages, 3, "k_pages")
+    _need_rank(table, 3, "table")
+    shape = (int(k_pages.shape[0]), int(k_pages.shape[1]), plan.head_dim)
+    _need(k_pages, shape, plan.torch_dtype, "k_pages")
+    _need(v_pages, shape, plan.torch_dtype, "v_pages")
+    _need(table, (bsz, plan.num_kv_heads, int(table.shape[2])), torch.int32, "table")
+    return moa_pages_t(k_pages.data_ptr(), v_pages.data_ptr(), table.data_ptr(), shape[0], shape[1],
+                       int(table.shape[2]))
+
+
+def _token_stride(t, shape, dtype, name):
+    """Elements from token to token of [T, H, D] tokens whose heads are contiguous."""
+    if tuple(t.shape) != tuple(shape):
+        raise MoaError(MOA_ERR_INVALID_ARG, f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.dtype != dtype:
+        raise MoaError(MOA_ERR_INVALID_ARG, f"{name}: expected dtype {dtype}, got {t.dtype}")
+    if t.device.type != "cuda":
+        raise MoaError(MOA_ERR_INVALID_ARG, f"{name}: must be a GPU tensor")
+    n, h, d = (int(x) for x in shape)
+    if t.stride(2) != 1 or (h > 1 and t.stride(1) != d):
+        raise MoaError(MOA_ERR_INVALID_ARG, f"{name}: a token's heads must be contiguous")
+    return int(t.stride(0)) if n > 1 else h * d
+
+
+def _seq_start(seq_start, bsz):
+    import torch
+    _need(seq_start, (bsz + 1,), torch.int32, "seq_start")
+
+
+def moa_paged_append(plan: Plan, k_pages, v_pages, table, q, k_new, v_new, positions, seq_start=None, inv_freq=None,
+                     interleaved: bool = False, q_out=None, stream=None):
+    """Stores packed new tokens in the pages and rotates queries and keys by their positions on the way.
+
+    q: [T, H_q, D] or None, k_new, v_new: [T, H_kv, D] (parts of one projection's output may be passed
+    as they are); positions: int32[B], of each sequence's first new token; seq_start: int32[B + 1], the
+    row where each sequence's tokens start (None: one token each, T = B); inv_freq: fp32 [R / 2], radians
+    per position (None: nothing is rotated).  Returns q_out, the rotated queries (q itself may be given)."""
+    if stream is None:
+        done = _fast.paged_append(plan._bound, k_pages, v_pages, table, q, k_new, v_new, positions, seq_start, inv_freq,
+                                  interleaved, q_out)
+        if done is not None:
+            return None if done is True else done
+    import torch
+    _need_rank(k_new, 3, "k_new")
+    _need_rank(positions, 1, "positions")
+    n, bsz = int(k_new.shape[0]), int(positions.shape[0])
+    dt = plan.torch_dtype
+    pages = _pages(plan, k_pages, v_pages, table, bsz)
+    _positions(positions, bsz)
+    k_stride = _token_stride(k_new, (n, plan.num_kv_heads, plan.head_dim), dt, "k_new")
+    v_stride = _token_stride(v_new, (n, plan.num_kv_heads, plan.head_dim), dt, "v_new")
+    tensors = dict(k_pages=k_pages, v_pages=v_pages, table=table, k_new=k_new, v_new=v_new, positions=positions)
+    q_stride = 0
+    if q is not None:
+        shape = (n, plan.num_q_heads, plan.head_dim)
+        q_stride = _token_stride(q, shape, dt, "q")
+        if q_out is None:
+            q_out = torch.empty(shape, dtype=dt, device=q.device)
+        _need(q_out, shape, dt, "q_out")
+        tensors.update(q=q, q_out=q_out)
+    elif q_out is not None:
+        raise MoaError(MOA_ERR_INVALID_ARG, "q_out without q")
+    if seq_start is not None:
+        _seq_start(seq_start, bsz)
+        tensors["seq_start"] = seq_start
+    rope = None
+    if inv_freq is not None:
+        _need_rank(inv_freq, 1, "inv_freq")
+        _need(inv_freq, inv_freq.shape, torch.float32, "inv_freq")
+        rope = ctypes.byref(moa_rope_t(inv_freq.data_ptr(), 2 * int(inv_freq.shape[0]), int(bool(interleaved))))
+        tensors["inv_freq"] = inv_freq
+    with torch.cuda.device(_one_device(**tensors)):
+        _check(load_library().moa_paged_append(
+            plan.handle, ctypes.byref(pages), None if q is None else q.data_ptr(), q_stride, k_new.data_ptr(), k_stride,
+            v_new.data_ptr(), v_stride, None if q is None else q_out.data_ptr(), rope, positions.data_ptr(),
+            None if seq_start is None else seq_start.data_ptr(), bsz, n, _stream(k_new, stream)))
+    return q_out
+
+
+def _paged_attention(plan, q, k_pages, v_pages, table, positions, workspace, o, stream, call, **more):
+    """The checks that the attention calls share; call(lib, pages, n, batch, workspace bytes, o, stream) makes it."""
+    import torch
+    _need_rank(q, 3, "q")
+    _need_rank(positions, 1, "positions")
+    n, bsz = int(q.shape[0]), int(positions.shape[0])
+    dt = plan.torch_dtype
+    _need(q, (n if "seq_start" in more else bsz, plan.num_q_heads, plan.head_dim), dt, "q")
+    pages = _pages(plan, k_pages, v_pages, table, bsz)
+    _positions(positions, bsz)
+    if o is None:
+        o = torch.empty_like(q)
+    _need(o, q.shape, dt, "o")
+    if workspace.device.type != "cuda" or not workspace.is_contiguous():
+        raise MoaError(MOA_ERR_WORKSPACE, "workspace must be a contiguous GPU tensor")
+    nbytes = workspace.numel() * workspace.element_size()
+    device = _one_device(q=q, k_pages=k_pages, v_pages=v_pages, table=table, positions=positions, workspace=workspace,
+                         o=o, **more)
+    with torch.cuda.device(device):
+        _check(call(load_library(), ctypes.byref(pages), n, bsz, nbytes, o, _stream(q, stream)))
+    return o
+
+
+def moa_paged_prefill(plan: Plan, q, k_pages, v_pages, table, positions, seq_start, workspace, o=None, stream=None):
+    """Attention of packed new tokens (rotated, and stored by moa_paged_append) over the pages.
+
+    q, o: [T, H_q, D]; positions: int32[B], of each sequence's first new token; seq_start: int32[B + 1]."""
+    if stream is None:
+        done = _fast.paged_prefill(plan._bound, q, k_pages, v_pages, table, positions, seq_start, workspace, o)
+        if done is not None:
+            return done
+    _need_rank(positions, 1, "positions")
+    _seq_start(seq_start, int(positions.shape[0]))
+    return _paged_attention(
+        plan, q, k_pages, v_pages, table, positions, workspace, o, stream,
+        lambda lib, pages, n, bsz, nbytes, out, s: lib.moa_paged_prefill(
+            plan.handle, pages, q.data_ptr(), out.data_ptr(), positions.data_ptr(), seq_start.data_ptr(), bsz, n,
+            workspace.data_ptr(), nbytes, s), seq_start=seq_start)
+
+
+def moa_paged_decode(plan: Plan, q, k_pages, v_pages, table, positions, workspace, o=None, stream=None):
+    """Attention of one token per sequence, at position positions[b], over the pages (q, o: [B, H_q, D])."""
+    if stream is None:
+        done = _fast.paged_decode(plan._bound, q, k_pages, v_pages, table, positions, workspace, o)
+        if done is not None:
+            return done
+    return _paged_attention(
+        plan, q, k_pages, v_pages, table, positions, workspace, o, stream,
+        lambda lib, pages, n, bsz, nbytes, out, s: lib.moa_paged_decode(
+            plan.handle, pages, q.data_ptr(), out.data_ptr(), positions.data_ptr(), bsz, workspace.data_ptr(), nbytes,
+            s))
+
+
+def moa_paged_decode_shared(plan: Plan, q, k_pages, v_pages, prefix_table, prefix_len: int, table, positions, workspace,
+                            o=None, stream=None):
+    """moa_paged_decode of sequences whose first prefix_len positions are the same pages
+    (prefix_table: int32 [H_kv, max_pages]), which are read once for the whole batch."""
+    if stream is None:
+        done = _fast.paged_decode_shared(plan._bound, q, k_pages, v_pages, prefix_table, prefix_len, table, positions,
+                                         workspace, o)
+        if done is not None:
+            return done
+    import torch
+    _need_rank(table, 3, "table")
+    _need(prefix_table, (plan.num_kv_heads, int(table.shape[2])), torch.int32, "prefix_table")
+    return _paged_attention(
+        plan, q, k_pages, v_pages, table, positions, workspace, o, stream,
+        lambda lib, pages, n, bsz, nbytes, out, s: lib.moa_paged_decode_shared(
+            plan.handle, pages, prefix_table.data_ptr(), int(prefix_len), q.data_ptr(), out.data_ptr(),
+            positions.data_ptr(), bsz, workspace.data_ptr(), nbytes, s), prefix_table=prefix_table)
