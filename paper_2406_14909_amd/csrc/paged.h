@@ -58,7 +58,10 @@ struct PagedArgs {
   const int32_t* prefix_table;   // [hkv, max_pages] of the keys in front of prefix_len, or null
   const int32_t* positions;
   const int32_t* seq_start;      // null: one token per sequence
-  float* part;
+  float* part;                   // workspace: partial results
+  int32_t* plan;                 // workspace: the split, from the first kernel of a call to the merge
+  const float* prefix_part;      // workspace: partial results of the prefix, or null
+  int32_t slots;                 // resident work-groups (set by the launcher)
   int32_t n_tokens;
   int32_t batch;
   int32_t hq;
@@ -71,6 +74,7 @@ struct PagedArgs {
   int32_t band_shift;            // the band of position i starts at ((i >> shift) - window + 1) << shift
   float scale_log2;
   int32_t window[MOA_MAX_KV_HEADS];
+  int32_t prefix_slot[MOA_MAX_KV_HEADS + 1];   // first piece of each head's prefix (a tile of rows has them all)
 };
 
 // Keys of one query position, as a run of sinks and a band behind them, both cut at
@@ -94,7 +98,11 @@ MOA_PAGED_FN VisibleKeys visible_keys(int32_t pos, int32_t window, int32_t band_
   return v;
 }
 
+constexpr int kPagedPartPad = 4;         // a partial row: head_dim sums, m, l, 2 pad floats
+constexpr int kPagedMaxWorkers = 4096;   // decode workers (work-groups) per launch, at most
+
 int launch_paged_append(const PagedAppendArgs& a, int dtype, int head_dim, void* stream);
 int launch_paged_attention(const PagedArgs& a, int dtype, int head_dim, void* stream);
+int launch_paged_decode(const PagedArgs& a, int dtype, int head_dim, int group, void* stream);
 
 }  // namespace moa

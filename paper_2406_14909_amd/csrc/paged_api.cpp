@@ -92,6 +92,28 @@ moa_status_t attention_args(const char* who, const moa_plan_t* plan, const moa_p
   return MOA_OK;
 }
 
+// Workspace of the decode calls: partial results fp32 [workers + pairs][group][head_dim + 4],
+// one slot per worker and per (sequence, KV head) pair, and the split of the call, int32
+// [4 + pairs + 1].
+size_t up256(size_t n) { return (n + 255) & ~static_cast<size_t>(255); }
+
+size_t decode_part_bytes(const moa_plan_s& p, int32_t batch) {
+  const size_t rows = kPagedMaxWorkers + static_cast<size_t>(batch) * p.desc.num_kv_heads;
+  return up256(rows * sizeof(float) * static_cast<size_t>(p.group) * (p.desc.head_dim + kPagedPartPad));
+}
+
+size_t decode_plan_bytes(const moa_plan_s& p, int32_t batch) {
+  return up256((static_cast<size_t>(batch) * p.desc.num_kv_heads + 5) * sizeof(int32_t));
+}
+
+// Rounds of all caches of a decode call are counted in 31 bits.
+bool countable(const moa_plan_s& p, const moa_pages_t& pages, int32_t batch) {
+  int64_t keys = 0;
+  for (int h = 0; h < p.desc.num_kv_heads; ++h)
+    keys += std::min<int64_t>(p.capacity[h], int64_t(pages.max_pages) * pages.page_size) / 64 + 1;
+  return keys * batch < (int64_t(1) << 31);
+}
+
 moa_status_t launched(const char* who, int err) {
   if (err == kGridTooLarge) return fail(MOA_ERR_UNSUPPORTED, std::string(who) + ": too much work for one launch");
   if (err) return fail(MOA_ERR_HIP, std::string(who) + ": kernel launch failed (hipError " + std::to_string(err) + ")");
@@ -180,7 +202,7 @@ moa_status_t moa_paged_append(const moa_plan_t* plan, const moa_pages_t* pages, 
 
 size_t moa_paged_workspace_bytes(const moa_plan_t* plan, int32_t batch, int64_t n_tokens) {
   if (!plan || batch < 1 || n_tokens < 1) return 0;
-  return 256;
+  return decode_part_bytes(*plan, batch) + decode_plan_bytes(*plan, batch);
 }
 
 moa_status_t moa_paged_prefill(const moa_plan_t* plan, const moa_pages_t* pages, const void* q, void* o,
@@ -216,7 +238,9 @@ moa_status_t moa_paged_decode(const moa_plan_t* plan, const moa_pages_t* pages, 
   PagedArgs a;
   const moa_status_t st = attention_args(who, plan, pages, q, o, positions, batch, batch, workspace, ws_bytes, &a);
   if (st != MOA_OK) return st;
-  return launched(who, launch_paged_attention(a, plan->desc.dtype, plan->desc.head_dim, hip_stream));
+  if (!countable(*plan, *pages, batch)) return launched(who, kGridTooLarge);
+  a.plan = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + decode_part_bytes(*plan, batch));
+  return launched(who, launch_paged_decode(a, plan->desc.dtype, plan->desc.head_dim, plan->group, hip_stream));
 }
 
 moa_status_t moa_paged_decode_shared(const moa_plan_t* plan, const moa_pages_t* pages, const int32_t* prefix_table,

@@ -1,6 +1,9 @@
 // Device helpers of the paged kernels.
 #pragma once
 
+#include <algorithm>
+#include <atomic>
+
 #include "moa_device.h"
 #include "paged.h"
 
@@ -37,6 +40,21 @@ __device__ __forceinline__ int token_position(const int32_t* positions, const in
 // First row of a page in the pool, or -1 where the page is absent.
 __device__ __forceinline__ int page_row(int page, int num_pages, int page_shift) {
   return static_cast<uint32_t>(page) < static_cast<uint32_t>(num_pages) ? page << page_shift : -1;
+}
+
+// Resident work-groups of `kernel` on the current device (cached per device by the
+// caller; threads that launch at once store the same value).
+inline int resident_groups(const void* kernel, int threads, std::atomic<int>* cache) {
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) dev = 0;
+  const int known = cache[dev].load(std::memory_order_relaxed);
+  if (known > 0) return known;
+  int cus = 0, per_cu = 0;
+  if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) cus = 1;
+  if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, kernel, threads, 0) != hipSuccess) per_cu = 1;
+  const int groups = std::max(1, cus) * std::max(1, per_cu);
+  cache[dev].store(groups, std::memory_order_relaxed);
+  return groups;
 }
 
 }  // namespace moa
