@@ -60,8 +60,9 @@ struct PagedArgs {
   const int32_t* seq_start;      // null: one token per sequence
   float* part;                   // workspace: partial results
   int32_t* plan;                 // workspace: the split, from the first kernel of a call to the merge
-  const float* prefix_part;      // workspace: partial results of the prefix, or null
-  int32_t slots;                 // resident work-groups (set by the launcher)
+  float* rows_part;              // workspace: partial results of row tiles (decode: of the shared prefix, or null)
+  int32_t slots;                 // work-groups that the keys are cut for
+  int32_t least_tiles;           // fewest 64-key tiles of a piece, where rows are many
   int32_t n_tokens;
   int32_t batch;
   int32_t hq;
@@ -71,10 +72,12 @@ struct PagedArgs {
   int32_t max_pages;
   int32_t num_sink;
   int32_t prefix_len;
+  int32_t group_shift;           // log2(hq / hkv)
   int32_t band_shift;            // the band of position i starts at ((i >> shift) - window + 1) << shift
   float scale_log2;
   int32_t window[MOA_MAX_KV_HEADS];
-  int32_t prefix_slot[MOA_MAX_KV_HEADS + 1];   // first piece of each head's prefix (a tile of rows has them all)
+  int16_t kv_order[MOA_MAX_KV_HEADS];          // KV heads, widest window first
+  int32_t prefix_slot[MOA_MAX_KV_HEADS + 1];   // first partial result of each head's prefix
 };
 
 // Keys of one query position, as a run of sinks and a band behind them, both cut at
@@ -102,7 +105,14 @@ constexpr int kPagedPartPad = 4;         // a partial row: head_dim sums, m, l, 
 constexpr int kPagedMaxWorkers = 4096;   // decode workers (work-groups) per launch, at most
 
 int launch_paged_append(const PagedAppendArgs& a, int dtype, int head_dim, void* stream);
-int launch_paged_attention(const PagedArgs& a, int dtype, int head_dim, void* stream);
+constexpr int kPagedRowGroups = 512;     // work-groups that the keys of row tiles are cut for (two per compute unit)
+constexpr int kPagedMaxPieces = 256;     // pieces of a row tile's keys, at most
+MOA_PAGED_FN int paged_tile_rows(int dtype) { return dtype == MOA_BF16 ? 128 : 32; }
+
+// The launches of row tiles take their grid: no fewer work-groups than items.
+int launch_paged_rows(const PagedArgs& a, int head_dim, int64_t groups, void* stream);       // bf16
+int launch_paged_rows_f32(const PagedArgs& a, int head_dim, int64_t groups, void* stream);
+int launch_paged_merge(const PagedArgs& a, int dtype, int head_dim, int tile_rows, int64_t segs, void* stream);
 int launch_paged_decode(const PagedArgs& a, int dtype, int head_dim, int group, void* stream);
 
 }  // namespace moa

@@ -88,22 +88,48 @@ moa_status_t attention_args(const char* who, const moa_plan_t* plan, const moa_p
   a->max_pages = pages->max_pages;
   a->num_sink = d.num_sink;
   a->scale_log2 = p.scale * 1.4426950408889634f;
-  for (int h = 0; h < d.num_kv_heads; ++h) a->window[h] = p.window[h];
+  a->group_shift = __builtin_ctz(static_cast<unsigned>(p.group));
+  for (int h = 0; h < d.num_kv_heads; ++h) {
+    a->window[h] = p.window[h];
+    a->kv_order[h] = p.kv_order[h];
+  }
   return MOA_OK;
 }
 
-// Workspace of the decode calls: partial results fp32 [workers + pairs][group][head_dim + 4],
-// one slot per worker and per (sequence, KV head) pair, and the split of the call, int32
-// [4 + pairs + 1].
 size_t up256(size_t n) { return (n + 255) & ~static_cast<size_t>(255); }
 
-size_t decode_part_bytes(const moa_plan_s& p, int32_t batch) {
-  const size_t rows = kPagedMaxWorkers + static_cast<size_t>(batch) * p.desc.num_kv_heads;
-  return up256(rows * sizeof(float) * static_cast<size_t>(p.group) * (p.desc.head_dim + kPagedPartPad));
+size_t row_bytes(const moa_plan_s& p) { return sizeof(float) * (p.desc.head_dim + kPagedPartPad); }
+
+// Row tiles of `tokens` tokens in `sequences` sequences, for one KV head, at most.
+int64_t row_tiles(const moa_plan_s& p, int64_t tokens, int64_t sequences) {
+  return tokens * p.group / paged_tile_rows(p.desc.dtype) + std::min(tokens, sequences);
 }
 
-size_t decode_plan_bytes(const moa_plan_s& p, int32_t batch) {
-  return up256((static_cast<size_t>(batch) * p.desc.num_kv_heads + 5) * sizeof(int32_t));
+// Workspaces.  Decode: partial results fp32 [workers + pairs][group][head_dim + 4], one
+// slot per worker and per (sequence, KV head) pair, the split of the call, int32
+// [4 + pairs + 1], and where a prefix is shared the partial results of its row tiles.
+// Prefill: partial results of the row tiles that are cut, and what the merge needs of them.
+struct DecodeSpace {
+  size_t plan, rows, bytes;      // offsets of the split and the row tiles' results, and the end
+};
+DecodeSpace decode_space(const moa_plan_s& p, int32_t batch) {
+  const size_t pairs = static_cast<size_t>(batch) * p.desc.num_kv_heads;
+  const int rows = paged_tile_rows(p.desc.dtype);
+  const size_t tiles = (static_cast<size_t>(batch) * p.group + rows - 1) / rows * p.desc.num_kv_heads;
+  DecodeSpace s;
+  s.plan = up256((kPagedMaxWorkers + pairs) * p.group * row_bytes(p));
+  s.rows = s.plan + up256((pairs + 5) * sizeof(int32_t));
+  s.bytes = s.rows + up256((tiles + kPagedRowGroups) * rows * row_bytes(p));
+  return s;
+}
+struct PrefillSpace {
+  size_t plan, bytes;
+};
+PrefillSpace prefill_space(const moa_plan_s& p) {
+  PrefillSpace s;
+  s.plan = up256(size_t(2) * kPagedRowGroups * paged_tile_rows(p.desc.dtype) * row_bytes(p));
+  s.bytes = s.plan + up256(32 + size_t(kPagedRowGroups) * 32);
+  return s;
 }
 
 // Rounds of all caches of a decode call are counted in 31 bits.
@@ -202,7 +228,7 @@ moa_status_t moa_paged_append(const moa_plan_t* plan, const moa_pages_t* pages, 
 
 size_t moa_paged_workspace_bytes(const moa_plan_t* plan, int32_t batch, int64_t n_tokens) {
   if (!plan || batch < 1 || n_tokens < 1) return 0;
-  return decode_part_bytes(*plan, batch) + decode_plan_bytes(*plan, batch);
+  return std::max(decode_space(*plan, batch).bytes, prefill_space(*plan).bytes);
 }
 
 moa_status_t moa_paged_prefill(const moa_plan_t* plan, const moa_pages_t* pages, const void* q, void* o,
@@ -228,7 +254,19 @@ moa_status_t moa_paged_prefill(const moa_plan_t* plan, const moa_pages_t* pages,
     static_assert(MOA_BAND_BLOCK == 64, "band_shift is log2(MOA_BAND_BLOCK)");
     for (int h = 0; h < d.num_kv_heads; ++h) a.window[h] = (a.window[h] + MOA_BAND_BLOCK - 1) / MOA_BAND_BLOCK;
   }
-  return launched(who, launch_paged_attention(a, d.dtype, d.head_dim, hip_stream));
+  const int64_t tiles = row_tiles(*plan, n_tokens, batch) * d.num_kv_heads;
+  char* ws = static_cast<char*>(workspace);
+  a.rows_part = static_cast<float*>(workspace);
+  a.plan = reinterpret_cast<int32_t*>(ws + prefill_space(*plan).plan);
+  a.slots = kPagedRowGroups;
+  a.least_tiles = 2;
+  // items: the row tiles, and as many pieces more as the keys are cut for; dealt to the dies in whole rounds
+  const int64_t groups = (tiles + kPagedRowGroups + 127) / 128 * 128;
+  int err = d.dtype == MOA_BF16 ? launch_paged_rows(a, d.head_dim, groups, hip_stream)
+                                : launch_paged_rows_f32(a, d.head_dim, groups, hip_stream);
+  if (!err) err = launch_paged_merge(a, d.dtype, d.head_dim, paged_tile_rows(d.dtype),
+                                     std::min<int64_t>(tiles, kPagedRowGroups), hip_stream);
+  return launched(who, err);
 }
 
 moa_status_t moa_paged_decode(const moa_plan_t* plan, const moa_pages_t* pages, const void* q, void* o,
@@ -239,7 +277,7 @@ moa_status_t moa_paged_decode(const moa_plan_t* plan, const moa_pages_t* pages, 
   const moa_status_t st = attention_args(who, plan, pages, q, o, positions, batch, batch, workspace, ws_bytes, &a);
   if (st != MOA_OK) return st;
   if (!countable(*plan, *pages, batch)) return launched(who, kGridTooLarge);
-  a.plan = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + decode_part_bytes(*plan, batch));
+  a.plan = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + decode_space(*plan, batch).plan);
   return launched(who, launch_paged_decode(a, plan->desc.dtype, plan->desc.head_dim, plan->group, hip_stream));
 }
 
@@ -258,9 +296,35 @@ moa_status_t moa_paged_decode_shared(const moa_plan_t* plan, const moa_pages_t* 
   if (overlaps(o, rows_bytes(*plan, batch, d.num_q_heads), prefix_table, pb) ||
       overlaps(workspace, moa_paged_workspace_bytes(plan, batch, batch), prefix_table, pb))
     return invalid(who, "o or the workspace overlaps prefix_table");
-  a.prefix_table = prefix_table;
-  a.prefix_len = static_cast<int32_t>(prefix_len);
-  return launched(who, launch_paged_attention(a, d.dtype, d.head_dim, hip_stream));
+  if (!countable(*plan, *pages, batch)) return launched(who, kGridTooLarge);
+  const DecodeSpace space = decode_space(*plan, batch);
+  char* ws = static_cast<char*>(workspace);
+  a.plan = reinterpret_cast<int32_t*>(ws + space.plan);
+  if (prefix_len > 0) {
+    a.prefix_table = prefix_table;
+    a.prefix_len = static_cast<int32_t>(prefix_len);
+    a.rows_part = reinterpret_cast<float*>(ws + space.rows);
+    // Every head's prefix in pieces of about the same number of key tiles.
+    const int rows = paged_tile_rows(d.dtype);
+    const int64_t tiles = (int64_t(batch) * plan->group + rows - 1) / rows;
+    int64_t keys[MOA_MAX_KV_HEADS], steps = 0;
+    for (int h = 0; h < d.num_kv_heads; ++h) {
+      const int64_t seen = std::min<int64_t>(prefix_len, int64_t(d.num_sink) + plan->window[h]);
+      keys[h] = (seen + 63) / 64;
+      steps += tiles * keys[h];
+    }
+    const int64_t longest = std::max<int64_t>(2, (steps + kPagedRowGroups - 1) / kPagedRowGroups);
+    int64_t slots = 0;
+    for (int h = 0; h < d.num_kv_heads; ++h) {
+      a.prefix_slot[h] = static_cast<int32_t>(slots);
+      slots += tiles * std::max<int64_t>(1, keys[h] / longest);
+    }
+    a.prefix_slot[d.num_kv_heads] = static_cast<int32_t>(slots);
+    const int err = d.dtype == MOA_BF16 ? launch_paged_rows(a, d.head_dim, slots, hip_stream)
+                                        : launch_paged_rows_f32(a, d.head_dim, slots, hip_stream);
+    if (err) return launched(who, err);
+  }
+  return launched(who, launch_paged_decode(a, d.dtype, d.head_dim, plan->group, hip_stream));
 }
 
 }  // extern "C"

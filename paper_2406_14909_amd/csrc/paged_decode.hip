@@ -69,12 +69,16 @@ __device__ __forceinline__ float dot2_ones(bf16 a, bf16 b, float acc) {
 #endif
 }
 
+// With a shared prefix: the keys behind it.  A sequence that is still inside the prefix has
+// its keys read here, all of them, so that those that a tile of sequences reads of the
+// prefix are one run without holes.
 __device__ __forceinline__ VisibleKeys keys_of(const PagedArgs& a, int pos, int g) {
-  return visible_keys(pos, a.window[g], 0, a.num_sink, a.prefix_len, a.max_pages << a.page_shift);
+  return visible_keys(pos, a.window[g], 0, a.num_sink, pos + 1 < a.prefix_len ? 0 : a.prefix_len,
+                      a.max_pages << a.page_shift);
 }
 
 __device__ __forceinline__ uint32_t rounds_of(const PagedArgs& a, int pos, int g, int round_shift) {
-  return paged_rounds(pos, pos < 0 ? 0 : keys_of(a, pos, g).count, round_shift, a.prefix_part != nullptr);
+  return paged_rounds(pos, pos < 0 ? 0 : keys_of(a, pos, g).count, round_shift, a.rows_part != nullptr);
 }
 
 // Shared state of the walk over a worker's piece.
@@ -180,7 +184,8 @@ template <class Part>
 __device__ __forceinline__ void for_each_span(const PagedArgs& a, Walk& s, int b, int g, const VisibleKeys& keys, int x0,
                                               int x1, int round_shift, Part&& part) {
   const VisiblePages pages(keys, a.page_shift);
-  const int32_t* table = a.table + (int64_t(b) * a.hkv + g) * a.max_pages;
+  const int32_t* table = keys.from < a.prefix_len ? a.prefix_table + int64_t(g) * a.max_pages
+                                                  : a.table + (int64_t(b) * a.hkv + g) * a.max_pages;
   const int span = ((kPageRows - 3) << a.page_shift) >> round_shift << round_shift;
   auto number = [&](int x) { return pages.number(x < keys.sinks, keys.at(x) >> a.page_shift); };
   for (int lo = x0; lo < x1; lo += span) {
@@ -350,7 +355,7 @@ __global__ void __launch_bounds__(kThreads) paged_decode_valu_kernel(PagedArgs a
       }
     }
     __syncthreads();
-    merge_waves_and_store<T, D, G>(a, s_acc, s_ml, b, g, pair, whole && a.prefix_part == nullptr);
+    merge_waves_and_store<T, D, G>(a, s_acc, s_ml, b, g, pair, whole && a.rows_part == nullptr);
     __syncthreads();                                // LDS is used by the next cache
   });
 }
@@ -526,7 +531,7 @@ __global__ void __launch_bounds__(kThreads, 3) paged_decode_mma_kernel(PagedArgs
       }
     }
     __syncthreads();
-    merge_waves_and_store<bf16, D, G>(a, s_acc, s_ml, b, g, pair, whole && a.prefix_part == nullptr);
+    merge_waves_and_store<bf16, D, G>(a, s_acc, s_ml, b, g, pair, whole && a.rows_part == nullptr);
     __syncthreads();                                // LDS is used by the next cache
   });
 }
@@ -542,7 +547,7 @@ __global__ void __launch_bounds__(kThreads, 3) paged_decode_mma_kernel(PagedArgs
 template <int G>
 constexpr int merge_heads() { return G <= 2 ? G : 2; }
 
-template <typename T, int D, int G>
+template <typename T, int D, int G, bool kShared>
 __global__ void __launch_bounds__(256) paged_combine_kernel(PagedArgs a) {
   constexpr int PS = D + kPagedPartPad;
   constexpr int V4 = D / 4;
@@ -559,13 +564,27 @@ __global__ void __launch_bounds__(256) paged_combine_kernel(PagedArgs a) {
   const uint32_t x0 = a.plan[kPlanHead + pair], x1 = a.plan[kPlanHead + pair + 1];
   const PagedSplit split = {static_cast<uint32_t>(a.plan[0]), static_cast<uint32_t>(a.plan[1]),
                             static_cast<uint32_t>(a.plan[2])};
-  if (x0 == x1) return;                               // idle
-  const uint32_t w0 = split.worker_of(x0), w1 = split.worker_of(x1 - 1);
-  if (w0 == w1) return;                               // its worker wrote the output
-  const int np = static_cast<int>(w1 - w0) + 1;
   const int pg = static_cast<int>(threadIdx.x) / TPR, j = static_cast<int>(threadIdx.x) % TPR;
   const int h = j / V4, d4 = j % V4;
-  const float* part0 = a.part + ((int64_t(w0) + pair) * G + h0 + h) * PS;
+  // Partials 0 .. n_own - 1 are the workers', the others those of the shared prefix.
+  int n_own = 0, np;
+  const float *own = a.part, *prefix = nullptr;
+  if (x0 < x1) {
+    const uint32_t w0 = split.worker_of(x0), w1 = split.worker_of(x1 - 1);
+    n_own = static_cast<int>(w1 - w0) + 1;
+    own = a.part + ((int64_t(w0) + pair) * G + h0 + h) * PS;
+  }
+  np = n_own;
+  if constexpr (kShared) {
+    if (a.positions[b] < 0) return;                   // idle
+    constexpr int RT = sizeof(T) == 2 ? 128 : 32;     // rows of a tile
+    const int row = b * G + h0 + h, tiles = (a.batch * G + RT - 1) / RT;
+    const int pieces = (a.prefix_slot[g + 1] - a.prefix_slot[g]) / tiles;
+    np += pieces;
+    prefix = a.rows_part + ((int64_t(a.prefix_slot[g]) + int64_t(row / RT) * pieces - int64_t(n_own)) * RT + row % RT) * PS;
+  } else if (n_own <= 1) {
+    return;                                           // idle, or its worker wrote the output
+  }
   float m = kNegBig, l = 0.0f;
   f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
   for (int p0 = pg; p0 < np; p0 += PG * MD) {
@@ -573,7 +592,9 @@ __global__ void __launch_bounds__(256) paged_combine_kernel(PagedArgs a) {
     f32x4 xp[MD];
 #pragma unroll
     for (int u = 0; u < MD; ++u) {
-      const float* q = part0 + int64_t(min(p0 + u * PG, np - 1)) * G * PS;
+      const int p = min(p0 + u * PG, np - 1);
+      const float* q = own + int64_t(p) * G * PS;
+      if constexpr (kShared) q = p < n_own ? q : prefix + int64_t(p) * (sizeof(T) == 2 ? 128 : 32) * PS;
       mp[u] = q[D];
       lp[u] = q[D + 1];
       xp[u] = *reinterpret_cast<const f32x4*>(q + 4 * d4);
@@ -630,8 +651,9 @@ int launch_t(PagedArgs a, void* stream) {
   hipError_t e = hipLaunchKernel(kernel, dim3(static_cast<unsigned>(a.slots)), dim3(kThreads), args, 0,
                                  static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return static_cast<int>(e);
-  e = hipLaunchKernel(reinterpret_cast<const void*>(&paged_combine_kernel<T, D, G>),
-                      dim3(static_cast<unsigned>(a.batch) * a.hkv * (G / merge_heads<G>())), dim3(256), args, 0,
+  const void* combine = a.rows_part != nullptr ? reinterpret_cast<const void*>(&paged_combine_kernel<T, D, G, true>)
+                                               : reinterpret_cast<const void*>(&paged_combine_kernel<T, D, G, false>);
+  e = hipLaunchKernel(combine, dim3(static_cast<unsigned>(a.batch) * a.hkv * (G / merge_heads<G>())), dim3(256), args, 0,
                       static_cast<hipStream_t>(stream));
   return static_cast<int>(e);
 }
