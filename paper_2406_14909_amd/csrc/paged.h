@@ -62,7 +62,10 @@ struct PagedArgs {
   int32_t* plan;                 // workspace: the split, from the first kernel of a call to the merge
   float* rows_part;              // workspace: partial results of row tiles (decode: of the shared prefix, or null)
   int32_t slots;                 // work-groups that the keys are cut for
-  int32_t least_tiles;           // fewest 64-key tiles of a piece, where rows are many
+  int32_t least_cost;            // rows: keys of a piece, at least
+  int32_t whole_cost;            // rows: keys of a row tile that is not worth cutting
+  int32_t log_slots;             // rows: log2(slots)
+  int32_t log_prefix_workers;    // a shared prefix is cut for 2^log_prefix_workers work-groups
   int32_t n_tokens;
   int32_t batch;
   int32_t hq;
@@ -76,8 +79,9 @@ struct PagedArgs {
   int32_t band_shift;            // the band of position i starts at ((i >> shift) - window + 1) << shift
   float scale_log2;
   int32_t window[MOA_MAX_KV_HEADS];
-  int16_t kv_order[MOA_MAX_KV_HEADS];          // KV heads, widest window first
-  int32_t prefix_slot[MOA_MAX_KV_HEADS + 1];   // first partial result of each head's prefix
+  int32_t window_in_order[MOA_MAX_KV_HEADS];   // and the same, widest first,
+  int16_t kv_order[MOA_MAX_KV_HEADS];          // of these KV heads
+  int32_t prefix_cost[MOA_MAX_KV_HEADS + 1];   // key tiles of the heads in front, of a shared prefix
 };
 
 // Keys of one query position, as a run of sinks and a band behind them, both cut at
@@ -105,14 +109,14 @@ constexpr int kPagedPartPad = 4;         // a partial row: head_dim sums, m, l, 
 constexpr int kPagedMaxWorkers = 4096;   // decode workers (work-groups) per launch, at most
 
 int launch_paged_append(const PagedAppendArgs& a, int dtype, int head_dim, void* stream);
-constexpr int kPagedRowGroups = 512;     // work-groups that the keys of row tiles are cut for (two per compute unit)
-constexpr int kPagedMaxPieces = 256;     // pieces of a row tile's keys, at most
-MOA_PAGED_FN int paged_tile_rows(int dtype) { return dtype == MOA_BF16 ? 128 : 32; }
+constexpr int kPagedLogRowGroups = 9;
+constexpr int kPagedRowGroups = 1 << kPagedLogRowGroups;   // work-groups that row tiles are cut for (two per compute unit)
+MOA_PAGED_FN int paged_tile_rows(int dtype) { return dtype == MOA_BF16 ? 128 : 64; }
 
 // The launches of row tiles take their grid: no fewer work-groups than items.
 int launch_paged_rows(const PagedArgs& a, int head_dim, int64_t groups, void* stream);       // bf16
 int launch_paged_rows_f32(const PagedArgs& a, int head_dim, int64_t groups, void* stream);
-int launch_paged_merge(const PagedArgs& a, int dtype, int head_dim, int tile_rows, int64_t segs, void* stream);
+int launch_paged_merge(const PagedArgs& a, int dtype, int head_dim, void* stream);
 int launch_paged_decode(const PagedArgs& a, int dtype, int head_dim, int group, void* stream);
 
 }  // namespace moa

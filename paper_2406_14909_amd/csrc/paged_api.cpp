@@ -5,7 +5,7 @@
 #include <string>
 
 #include "moa_internal.h"
-#include "paged.h"
+#include "paged_split.h"
 
 namespace moa {
 
@@ -128,7 +128,7 @@ struct PrefillSpace {
 PrefillSpace prefill_space(const moa_plan_s& p) {
   PrefillSpace s;
   s.plan = up256(size_t(2) * kPagedRowGroups * paged_tile_rows(p.desc.dtype) * row_bytes(p));
-  s.bytes = s.plan + up256(32 + size_t(kPagedRowGroups) * 32);
+  s.bytes = s.plan + up256(size_t(kPagedRowGroups) * 16);
   return s;
 }
 
@@ -255,17 +255,22 @@ moa_status_t moa_paged_prefill(const moa_plan_t* plan, const moa_pages_t* pages,
     for (int h = 0; h < d.num_kv_heads; ++h) a.window[h] = (a.window[h] + MOA_BAND_BLOCK - 1) / MOA_BAND_BLOCK;
   }
   const int64_t tiles = row_tiles(*plan, n_tokens, batch) * d.num_kv_heads;
+  if (tiles >= kMaxGrid || tiles * (std::min<int64_t>(int64_t(pages->max_pages) * pages->page_size, kMaxPosition) + kTileCost) >=
+                               (int64_t(1) << 53))    // the cost of a call is cut in 64 bits
+    return launched(who, kGridTooLarge);
   char* ws = static_cast<char*>(workspace);
   a.rows_part = static_cast<float*>(workspace);
   a.plan = reinterpret_cast<int32_t*>(ws + prefill_space(*plan).plan);
   a.slots = kPagedRowGroups;
-  a.least_tiles = 2;
-  // items: the row tiles, and as many pieces more as the keys are cut for; dealt to the dies in whole rounds
-  const int64_t groups = (tiles + kPagedRowGroups + 127) / 128 * 128;
+  a.log_slots = kPagedLogRowGroups;
+  a.least_cost = kLeastRowCost;
+  a.whole_cost = kWholeRowCost;
+  for (int h = 0; h < d.num_kv_heads; ++h) a.window_in_order[h] = a.window[a.kv_order[h]];
+  // a work-group per row tile, dealt to the dies in whole rounds, or per piece
+  const int64_t groups = std::max<int64_t>((tiles + 127) / 128 * 128, kPagedRowGroups);
   int err = d.dtype == MOA_BF16 ? launch_paged_rows(a, d.head_dim, groups, hip_stream)
                                 : launch_paged_rows_f32(a, d.head_dim, groups, hip_stream);
-  if (!err) err = launch_paged_merge(a, d.dtype, d.head_dim, paged_tile_rows(d.dtype),
-                                     std::min<int64_t>(tiles, kPagedRowGroups), hip_stream);
+  if (!err) err = launch_paged_merge(a, d.dtype, d.head_dim, hip_stream);
   return launched(who, err);
 }
 
@@ -304,24 +309,18 @@ moa_status_t moa_paged_decode_shared(const moa_plan_t* plan, const moa_pages_t* 
     a.prefix_table = prefix_table;
     a.prefix_len = static_cast<int32_t>(prefix_len);
     a.rows_part = reinterpret_cast<float*>(ws + space.rows);
-    // Every head's prefix in pieces of about the same number of key tiles.
     const int rows = paged_tile_rows(d.dtype);
     const int64_t tiles = (int64_t(batch) * plan->group + rows - 1) / rows;
-    int64_t keys[MOA_MAX_KV_HEADS], steps = 0;
+    int64_t cost = 0;
     for (int h = 0; h < d.num_kv_heads; ++h) {
-      const int64_t seen = std::min<int64_t>(prefix_len, int64_t(d.num_sink) + plan->window[h]);
-      keys[h] = (seen + 63) / 64;
-      steps += tiles * keys[h];
+      a.prefix_cost[h] = static_cast<int32_t>(cost);
+      cost += (std::min<int64_t>(prefix_len, int64_t(d.num_sink) + plan->window[h] + 63) + 63) / 64;
     }
-    const int64_t longest = std::max<int64_t>(2, (steps + kPagedRowGroups - 1) / kPagedRowGroups);
-    int64_t slots = 0;
-    for (int h = 0; h < d.num_kv_heads; ++h) {
-      a.prefix_slot[h] = static_cast<int32_t>(slots);
-      slots += tiles * std::max<int64_t>(1, keys[h] / longest);
-    }
-    a.prefix_slot[d.num_kv_heads] = static_cast<int32_t>(slots);
-    const int err = d.dtype == MOA_BF16 ? launch_paged_rows(a, d.head_dim, slots, hip_stream)
-                                        : launch_paged_rows_f32(a, d.head_dim, slots, hip_stream);
+    a.prefix_cost[d.num_kv_heads] = static_cast<int32_t>(cost);
+    a.log_prefix_workers = row_split(cost * tiles, 2, kPagedLogRowGroups).log_workers;
+    const int64_t workers = int64_t(1) << a.log_prefix_workers;
+    const int err = d.dtype == MOA_BF16 ? launch_paged_rows(a, d.head_dim, workers, hip_stream)
+                                        : launch_paged_rows_f32(a, d.head_dim, workers, hip_stream);
     if (err) return launched(who, err);
   }
   return launched(who, launch_paged_decode(a, d.dtype, d.head_dim, plan->group, hip_stream));

@@ -20,7 +20,7 @@
 //   S^T = K Q^T  (A = 16 keys x 32 dims, from whole rows turned in LDS),
 //   O^T += V^T P^T  (B = P^T from the score registers, A = V^T by the transposing LDS
 //   read, the keys of a step permuted alike on both sides).
-#include "paged_device.h"
+#include "paged_rows.h"
 #include "paged_split.h"
 
 namespace moa {
@@ -555,6 +555,7 @@ __global__ void __launch_bounds__(256) paged_combine_kernel(PagedArgs a) {
   constexpr int TPR = HS * V4;               // threads per partial
   constexpr int PG = 256 / TPR;              // partials read at once
   constexpr int MD = 4;                      // in flight per thread
+  constexpr int RT = sizeof(T) == 2 ? 128 : 64;   // rows of a prefix tile
   static_assert(TPR <= 256 && 256 % TPR == 0, "thread mapping");
   __shared__ f32x4 s_acc[256];
   __shared__ float s_m[256], s_l[256];
@@ -577,11 +578,13 @@ __global__ void __launch_bounds__(256) paged_combine_kernel(PagedArgs a) {
   np = n_own;
   if constexpr (kShared) {
     if (a.positions[b] < 0) return;                   // idle
-    constexpr int RT = sizeof(T) == 2 ? 128 : 32;     // rows of a tile
-    const int row = b * G + h0 + h, tiles = (a.batch * G + RT - 1) / RT;
-    const int pieces = (a.prefix_slot[g + 1] - a.prefix_slot[g]) / tiles;
-    np += pieces;
-    prefix = a.rows_part + ((int64_t(a.prefix_slot[g]) + int64_t(row / RT) * pieces - int64_t(n_own)) * RT + row % RT) * PS;
+    const int row = b * G + h0 + h, tiles = prefix_row_tiles<RT>(a.batch, a.group_shift);
+    const RowSplit rows = {int64_t(a.prefix_cost[a.hkv]) * tiles, a.log_prefix_workers};
+    const int64_t each = a.prefix_cost[g + 1] - a.prefix_cost[g];
+    const int64_t c0 = int64_t(a.prefix_cost[g]) * tiles + row / RT * each;
+    const int w0 = rows.worker_of(c0);
+    np += rows.worker_of(c0 + each - 1) - w0 + 1;
+    prefix = a.rows_part + ((int64_t(w0) + g * tiles + row / RT - n_own) * RT + row % RT) * PS;
   } else if (n_own <= 1) {
     return;                                           // idle, or its worker wrote the output
   }
@@ -594,7 +597,7 @@ __global__ void __launch_bounds__(256) paged_combine_kernel(PagedArgs a) {
     for (int u = 0; u < MD; ++u) {
       const int p = min(p0 + u * PG, np - 1);
       const float* q = own + int64_t(p) * G * PS;
-      if constexpr (kShared) q = p < n_own ? q : prefix + int64_t(p) * (sizeof(T) == 2 ? 128 : 32) * PS;
+      if constexpr (kShared) q = p < n_own ? q : prefix + int64_t(p) * RT * PS;
       mp[u] = q[D];
       lp[u] = q[D + 1];
       xp[u] = *reinterpret_cast<const f32x4*>(q + 4 * d4);

@@ -1,16 +1,17 @@
 // Attention of many query rows over a paged cache in fp32: the work of paged_prefill.hip for
-// fp32 plans, in tiles of 32 rows.
+// fp32 plans, in tiles of 64 rows.
 //
 // Bound by the fp32 matrix units (32x32x2, a sixteenth of the bf16 rate): operands come
-// straight from memory, a tile's keys once per 32 rows.  The 4 waves of a work-group take
-// the 32-key tiles of the rows' span in turn and meet in LDS at the end, so that a short
-// prompt's rows are done by four waves side by side.
-//   S^T = K Q^T: a lane holds key lane % 32 and half of the dimensions (which half goes with
-//   which step of the product is free), 16 bytes per load.
+// straight from memory, a tile's keys once per 32 rows.  Two waves share each 32 rows, and
+// all four the rows of a tile that has no more: they take the 32-key tiles of the rows' span
+// in turn and meet in LDS at the end.
+//   S^T = K Q^T: a lane holds key lane % 32 and half of the dimensions, every other four of
+//   them (which goes with which step of the product is free), so that the two halves' 16-byte
+//   loads are neighbours.
 //   O^T += V^T P^T: B = P^T from the score registers, a lane's A = V of one key of a pair,
 //   dimension lane % 32 of 32.
-// A lane looks up the page of its key a tile ahead; keys that no row sees and keys on absent
-// pages are not read, and count as zeros with weight 0.
+// A lane looks up the page of its key two tiles ahead.  Keys that no row sees and keys on
+// absent pages read the pool's first row instead, and count as zeros with weight 0.
 #include "paged_rows.h"
 
 namespace moa {
@@ -18,7 +19,7 @@ namespace moa {
 namespace {
 
 constexpr int kWaves = 4;
-constexpr int kRows = 32;
+constexpr int kRows = 64;
 constexpr float kRescaleSlack = 8.0f;   // log2 headroom before the offset is raised
 
 __device__ __forceinline__ f32x16 mma(float a, float b, const f32x16& c) {
@@ -32,195 +33,212 @@ __device__ __forceinline__ f32x16 mma(float a, float b, const f32x16& c) {
 }
 
 template <int D, bool kShared>
-__global__ void __launch_bounds__(kWaves * 64, 1) paged_rows_f32_kernel(PagedArgs a) {
+__global__ void __launch_bounds__(kWaves * 64, D == 64 ? 2 : 1) paged_rows_f32_kernel(PagedArgs a) {
   constexpr int PS = D + kPagedPartPad;
   constexpr int H = D / 2;                // dimensions of a half-wave
   constexpr int DT = D / 32;
   constexpr int kRegs = DT * 16 + 2;      // a lane's state
   __shared__ union {
-    PagedPlanLds plan;
+    RowPlanLds plan;
     float state[(kWaves - 1) * kRegs * 64];
   } s_mem;
-
-  PagedItem it;
-  if constexpr (kShared) {
-    it = uniform(prefix_item<kRows>(a));
-  } else {
-    it = uniform(paged_item<kRows>(a, s_mem.plan));
-    __syncthreads();                      // the plan's LDS becomes the states'
-  }
-  if (it.rows <= 0) return;
 
   const int lane = threadIdx.x & 63;
   const int wave = uniform(threadIdx.x >> 6);
   const int lrow = lane & 31;
   const int half = lane >> 5;
   const int gs = a.group_shift;
-  const int g = it.g;
-  const int wband = a.window[g], bsh = a.band_shift, s = a.num_sink;
-  auto band_start = [&](int i) { return ((i >> bsh) - wband + 1) * (1 << bsh); };
+  auto tile = [&](const PagedItem& item) {
+    const PagedItem it = uniform(item);
+    __syncthreads();                      // the LDS of the tile before is free
+    const int g = it.g;
+    const int wband = a.window[g], bsh = a.band_shift, s = a.num_sink;
+    auto band_start = [&](int i) { return ((i >> bsh) - wband + 1) * (1 << bsh); };
 
-  const bool in_tile = lrow < it.rows;
-  const int token = it.token + (lrow >> gs);
-  const int head = g * (1 << gs) + (lrow & ((1 << gs) - 1));
-  int my_pos = -1;
-  if (in_tile) my_pos = kShared ? a.positions[token] : it.pos + (lrow >> gs);
-  if (kShared && my_pos < a.prefix_len - 1) my_pos = -1;   // idle, or inside the prefix: not read here
-  int p_first = my_pos >= 0 ? my_pos : 0x7fffffff, p_last = my_pos;
+    const bool narrow = it.rows <= 32;
+    const int row_block = narrow ? 0 : wave & 1;
+    const int kg = narrow ? wave : wave >> 1, groups = narrow ? kWaves : kWaves / 2;   // of key tiles
+    const int my_row = row_block * 32 + lrow;
+    const bool in_tile = my_row < it.rows;
+    const int token = it.token + (my_row >> gs);
+    const int head = g * (1 << gs) + (my_row & ((1 << gs) - 1));
+    int my_pos = -1;
+    if (in_tile) my_pos = kShared ? a.positions[token] : it.pos + (my_row >> gs);
+    if (kShared && my_pos < a.prefix_len - 1) my_pos = -1;   // idle, or inside the prefix: not read here
+    int p_first = my_pos >= 0 ? my_pos : 0x7fffffff, p_last = my_pos;
 #pragma unroll
-  for (int off = 1; off < 32; off *= 2) {
-    p_first = min(p_first, __shfl_xor(p_first, off, 64));
-    p_last = max(p_last, __shfl_xor(p_last, off, 64));
-  }
-  p_first = uniform(p_first);
-  p_last = uniform(p_last);
-
-  // Keys that some row sees: [0, sinks) and [band_lo, key_end); 64-key tiles of this piece.
-  const int cap = a.max_pages << a.page_shift;
-  int key_end = min(p_last, cap - 1) + 1;
-  if constexpr (kShared) key_end = min(key_end, a.prefix_len);
-  const int sinks = min(s, key_end);
-  const int band_lo = p_last < 0 ? key_end : min(max(0, band_start(p_first)), key_end);
-  const int ta = (sinks + 63) / 64;
-  const int tb = max(ta, band_lo / 64);
-  const int ntiles = ta + (band_lo < key_end ? max(0, (key_end - 1) / 64 - tb + 1) : 0);
-  const int t0 = static_cast<int>(int64_t(ntiles) * it.piece / it.pieces);
-  const int t1 = static_cast<int>(int64_t(ntiles) * (it.piece + 1) / it.pieces);
-  const int32_t* table =
-      kShared ? a.prefix_table + int64_t(g) * a.max_pages : a.table + int64_t(it.pair) * a.max_pages;
-
-  // First key of the wave's u-th 32-key tile, and the pool's row of this lane's key there.
-  auto tile_j0 = [&](int u) {
-    const int t = t0 + (u >> 1);
-    return (t < ta ? t : tb + (t - ta)) * 64 + 32 * (u & 1);
-  };
-  auto row_of = [&](int j0) {
-    const int j = j0 + lrow;
-    if (j >= key_end || (j >= sinks && j < band_lo)) return -1;
-    const int r = page_row(table[j >> a.page_shift], a.num_pages, a.page_shift);
-    return r < 0 ? -1 : r + (j & ((1 << a.page_shift) - 1));
-  };
-
-  const int end = 2 * (t1 - t0);
-  int u = wave;
-  int row = u < end ? row_of(tile_j0(u)) : -1;
-  float qf[H];
-#pragma unroll
-  for (int i = 0; i < H; i += 4) {
-    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (my_pos >= 0)
-      x = *reinterpret_cast<const f32x4*>(static_cast<const float*>(a.q) + (int64_t(token) * a.hq + head) * D + half * H + i);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) qf[i + e] = x[e];
-  }
-  f32x16 oacc[DT];
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt) oacc[dt] = f32x16{};
-  float m_run = kNegBig, l_run = 0.0f;
-  const float c2 = a.scale_log2;
-
-  for (; u < end; u += kWaves) {
-    const int j0 = tile_j0(u);
-    const uint32_t there = static_cast<uint32_t>(__ballot(row >= 0));
-    f32x4 kf[H / 4];
-    float vf[16][DT];
-#pragma unroll
-    for (int i = 0; i < H / 4; ++i) {
-      kf[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      if (row >= 0) kf[i] = *reinterpret_cast<const f32x4*>(static_cast<const float*>(a.kp) + int64_t(row) * D + half * H + 4 * i);
+    for (int off = 1; off < 32; off *= 2) {
+      p_first = min(p_first, __shfl_xor(p_first, off, 64));
+      p_last = max(p_last, __shfl_xor(p_last, off, 64));
     }
+    p_first = uniform(p_first);
+    p_last = uniform(p_last);
+
+    // Keys that some row sees: [0, sinks) and [band_lo, key_end); 64-key tiles of this piece.
+    const int cap = a.max_pages << a.page_shift;
+    int key_end = min(p_last, cap - 1) + 1;
+    if constexpr (kShared) key_end = min(key_end, a.prefix_len);
+    const int sinks = min(s, key_end);
+    const int band_lo = p_last < 0 ? key_end : min(max(0, band_start(p_first)), key_end);
+    const int ta = (sinks + 63) / 64;
+    const int tb = max(ta, band_lo / 64);
+    const int ntiles = ta + (band_lo < key_end ? max(0, (key_end - 1) / 64 - tb + 1) : 0);
+    const int t0 = uniform(row_part(ntiles, it.num0, it.den));
+    const int t1 = uniform(row_part(ntiles, it.num1, it.den));
+    const int32_t* const table = it.table;
+
+    // First key of the wave's u-th 32-key tile, and the pool's row of this lane's key there.
+    auto tile_j0 = [&](int u) {
+      const int t = t0 + (u >> 1);
+      return (t < ta ? t : tb + (t - ta)) * 64 + 32 * (u & 1);
+    };
+    auto row_of = [&](int j0) {
+      const int j = j0 + lrow;
+      if (j >= key_end || (j >= sinks && j < band_lo)) return -1;
+      const int r = page_row(table[j >> a.page_shift], a.num_pages, a.page_shift);
+      return r < 0 ? -1 : r + (j & ((1 << a.page_shift) - 1));
+    };
+
+    const int end = 2 * (t1 - t0);
+    int u = kg;
+    auto row_at = [&](int v) { return v < end ? row_of(tile_j0(v)) : -1; };
+    int row = row_at(u);
+    // K of a tile is asked for behind the scores of the one before, V in front of its own
+    // scores: each has a product's time to arrive, in one set of registers.
+    f32x4 kf[H / 4];
+    auto load_k = [&](int r) {
+      const float* p = static_cast<const float*>(a.kp) + int64_t(max(r, 0)) * D + half * 4;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int vrow = __shfl(row, (r >> 2) * 8 + half * 4 + (r & 3), 64);
+      for (int i = 0; i < H / 4; ++i) kf[i] = *reinterpret_cast<const f32x4*>(p + 8 * i);
+    };
+    if (u < end) load_k(row);
+    int row_next = row_at(u + groups);
+    float qf[H];
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        vf[r][dt] = 0.0f;
-        if (vrow >= 0) vf[r][dt] = static_cast<const float*>(a.vp)[int64_t(vrow) * D + dt * 32 + lrow];
+    for (int i = 0; i < H; i += 4) {
+      f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (my_pos >= 0)
+        x = *reinterpret_cast<const f32x4*>(static_cast<const float*>(a.q) + (int64_t(token) * a.hq + head) * D + 2 * i + half * 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) qf[i + e] = x[e];
+    }
+    f32x16 oacc[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) oacc[dt] = f32x16{};
+    float m_run = kNegBig, l_run = 0.0f;
+    const float c2 = a.scale_log2;
+
+    for (; u < end; u += groups) {
+      const int j0 = tile_j0(u);
+      const uint32_t there = static_cast<uint32_t>(__ballot(row >= 0));
+      float vf[16][DT];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int vrow = max(__shfl(row, (r >> 2) * 8 + half * 4 + (r & 3), 64), 0);
+        const float* p = static_cast<const float*>(a.vp) + int64_t(vrow) * D + lrow;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) vf[r][dt] = p[dt * 32];
+      }
+      sched_fence();
+      f32x16 sacc = f32x16{};
+#pragma unroll
+      for (int i = 0; i < H / 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sacc = mma(kf[i][e], qf[4 * i + e], sacc);
+      sched_fence();
+      if (u + groups < end) load_k(row_next);
+      row = row_next;
+      row_next = row_at(u + 2 * groups);
+      sched_fence();
+      if (there != 0xffffffffu) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt)
+            vf[r][dt] = there >> ((r >> 2) * 8 + half * 4 + (r & 3)) & 1 ? vf[r][dt] : 0.0f;
+      }
+
+      const int jl = j0 + half * 4;                           // key of register 0 of this lane
+      const int hi = min(my_pos, key_end - 1) - jl, band = band_start(my_pos) - jl, sink = s - jl;
+      float tmax = -INFINITY;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int dj = (r >> 2) * 8 + (r & 3);
+        const bool vis = (dj <= hi) & ((dj < sink) | (dj >= band)) & ((there >> (dj + half * 4) & 1) != 0);
+        sacc[r] = vis ? sacc[r] * c2 : -INFINITY;
+        tmax = fmaxf(tmax, sacc[r]);
+      }
+      if (__any(tmax > m_run + kRescaleSlack)) {
+        const float m_new = fmaxf(m_run, max_xor<32>(tmax));
+        const float alpha = fast_exp2(m_run - m_new);
+        m_run = m_new;
+        l_run *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) oacc[dt] *= alpha;
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float p = fast_exp2(sacc[r] - m_run);
+        l_run += p;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) oacc[dt] = mma(vf[r][dt], p, oacc[dt]);
       }
     }
-    row = u + kWaves < end ? row_of(tile_j0(u + kWaves)) : -1;
+    l_run = sum_xor<32>(l_run);
 
-    f32x16 sacc = f32x16{};
+    // The waves' states of the same rows sit in the same lanes.
+    if (kg > 0) {
+      float* p = s_mem.state + (narrow ? kg - 1 : row_block) * kRegs * 64 + lane;
 #pragma unroll
-    for (int i = 0; i < H / 4; ++i)
+      for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sacc = mma(kf[i][e], qf[4 * i + e], sacc);
-
-    const int jl = j0 + half * 4;                           // key of register 0 of this lane
-    const int hi = min(my_pos, key_end - 1) - jl, band = band_start(my_pos) - jl, sink = s - jl;
-    float tmax = -INFINITY;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int dj = (r >> 2) * 8 + (r & 3);
-      const bool vis = (dj <= hi) & ((dj < sink) | (dj >= band)) & ((there >> (dj + half * 4) & 1) != 0);
-      sacc[r] = vis ? sacc[r] * c2 : -INFINITY;
-      tmax = fmaxf(tmax, sacc[r]);
+        for (int r = 0; r < 16; ++r) p[(dt * 16 + r) * 64] = oacc[dt][r];
+      p[(kRegs - 2) * 64] = m_run;
+      p[(kRegs - 1) * 64] = l_run;
     }
-    if (__any(tmax > m_run + kRescaleSlack)) {
-      const float m_new = fmaxf(m_run, max_xor<32>(tmax));
-      const float alpha = fast_exp2(m_run - m_new);
-      m_run = m_new;
-      l_run *= alpha;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) oacc[dt] *= alpha;
-    }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const float p = fast_exp2(sacc[r] - m_run);
-      l_run += p;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) oacc[dt] = mma(vf[r][dt], p, oacc[dt]);
-    }
-  }
-  l_run = sum_xor<32>(l_run);
-
-  // The waves' states of the same rows sit in the same lanes.
-  if (wave > 0) {
-    float* p = s_mem.state + (wave - 1) * kRegs * 64 + lane;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) p[(dt * 16 + r) * 64] = oacc[dt][r];
-    p[(kRegs - 2) * 64] = m_run;
-    p[(kRegs - 1) * 64] = l_run;
-  }
-  __syncthreads();
-  if (wave > 0) return;
+    __syncthreads();
+    if (kg > 0) return;
 #pragma unroll 1
-  for (int v = 0; v < kWaves - 1; ++v) {
-    const float* p = s_mem.state + v * kRegs * 64 + lane;
-    const float m2 = p[(kRegs - 2) * 64];
-    const float m_new = fmaxf(m_run, m2);
-    const float f1 = fast_exp2(m_run - m_new), f2 = fast_exp2(m2 - m_new);
-    m_run = m_new;
-    l_run = l_run * f1 + p[(kRegs - 1) * 64] * f2;
+    for (int v = 0; v < groups - 1; ++v) {
+      const float* p = s_mem.state + (narrow ? v : row_block) * kRegs * 64 + lane;
+      const float m2 = p[(kRegs - 2) * 64];
+      const float m_new = fmaxf(m_run, m2);
+      const float f1 = fast_exp2(m_run - m_new), f2 = fast_exp2(m2 - m_new);
+      m_run = m_new;
+      l_run = l_run * f1 + p[(kRegs - 1) * 64] * f2;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) oacc[dt][r] = oacc[dt][r] * f1 + p[(dt * 16 + r) * 64] * f2;
+    }
+    if (!in_tile) return;
+    float* out;
+    float f = 1.0f;
+    if (it.slot >= 0) {                   // by rows, or as the lanes hold them (see paged_prefill.hip)
+      float* const pp = a.rows_part + int64_t(it.slot) * kRows * (kShared ? PS : D + 2);
+      float* const st = kShared ? pp + my_row * PS + D : pp + kRows * D + my_row * 2;
+      if (half == 0) {
+        st[0] = m_run;
+        st[1] = l_run;
+      }
+      out = kShared ? pp + my_row * PS + half * 4 : pp + (row_block * (D / 8) * 64 + lane) * 4;
+    } else {
+      out = static_cast<float*>(a.o) + (int64_t(token) * a.hq + head) * D + half * 4;
+      f = l_run > 0.0f ? 1.0f / l_run : 0.0f;               // a row that sees no key is 0
+    }
+    const int step = !kShared && it.slot >= 0 ? 256 : 8;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) oacc[dt][r] = oacc[dt][r] * f1 + p[(dt * 16 + r) * 64] * f2;
-  }
-  if (!in_tile) return;
-  float* out;
-  float f = 1.0f;
-  if (it.slot >= 0) {
-    out = a.rows_part + (int64_t(it.slot) * kRows + lrow) * PS;
-    if (half == 0) {
-      out[D] = m_run;
-      out[D + 1] = l_run;
-    }
-  } else {
-    out = static_cast<float*>(a.o) + (int64_t(token) * a.hq + head) * D;
-    f = l_run > 0.0f ? 1.0f / l_run : 0.0f;                 // a row that sees no key is 0
-  }
+      for (int grp = 0; grp < 4; ++grp) {
+        f32x4 x;
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-    for (int grp = 0; grp < 4; ++grp) {
-      f32x4 x;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = oacc[dt][grp * 4 + e] * f;
-      *reinterpret_cast<f32x4*>(out + dt * 32 + grp * 8 + half * 4) = x;
-    }
+        for (int e = 0; e < 4; ++e) x[e] = oacc[dt][grp * 4 + e] * f;
+        *reinterpret_cast<f32x4*>(out + (dt * 4 + grp) * step) = x;
+      }
+  };
+  if constexpr (kShared) for_each_prefix_tile<kRows>(a, blockIdx.x, tile);
+  else for_each_row_tile<kRows>(a, s_mem.plan, tile);
 }
 
 template <int D, bool kShared>

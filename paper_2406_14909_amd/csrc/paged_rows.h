@@ -1,212 +1,278 @@
-// Work items of the paged attention of many query rows: ragged chunks of tokens over
-// their caches, or the tokens of a whole batch over a shared prefix.
+// How the work of paged attention of many query rows is shared out: ragged chunks of tokens
+// over their caches, or the tokens of a whole batch over a shared prefix.
 //
-// Rows are (token, query head of the KV head) pairs, token by token, in tiles of ROWS; the
-// keys of a tile are walked in tiles of 64 positions.  An item is one row tile and one of
-// the pieces that its key tiles are cut into.  A row tile that is not cut writes its
-// output, the others leave partial results and a merge follows.
+// Rows are (token, query head) pairs of one KV head, token by token, in tiles of ROWS; the
+// keys of a row tile are walked in tiles of 64 positions.  A row tile costs the keys that
+// its last token may see, and kTileCost more for its start and end.  The cost of all row
+// tiles of all (sequence, KV head) pairs, laid end to end, is cut into equal pieces, one
+// per work-group ("worker"); a worker walks the row tiles that its piece touches.  A row
+// tile inside one piece writes its output, one that is cut leaves partial results, in a slot
+// of the worker, and a merge follows.  Where there are row tiles enough, every work-group
+// takes a whole one instead: no partial results, and neighbours share keys in their die's L2.
 //
-// The lengths live on the device.  Each work-group forms the plan for itself: a (sequence,
-// KV head) pair with T row tiles of at most E key tiles is work for T * E steps; pieces
-// have at most L = max(least, all steps / groups) of them, so that there are no more pieces
-// of cut tiles than 2 * groups, whatever the lengths, and long prompts are not cut at all.
+// The lengths live on the device.  Each work-group forms the plan for itself: one trip to
+// memory and a prefix sum over the pairs; a row tile's place within its pair has a closed form.
 #pragma once
 
 #include "paged_device.h"
+#include "paged_split.h"
 
 namespace moa {
 
-// What the merge has to know of a row tile that was cut.
-struct PagedSeg {
-  int32_t token;     // first packed token
-  int32_t head;      // KV head
-  int32_t rows;
-  int32_t slot;      // of its first piece
-  int32_t pieces;
-  int32_t pad[3];
-};
 
+// One row tile and a part [num0, num1) of den of its key tiles.
 struct PagedItem {
   int g;
-  int pair;          // b * hkv + g (prefill)
-  int token;         // packed token of the row tile's first row
-  int rows;          // rows of the tile
+  const int32_t* table;
+  int token;         // packed token of the first row
+  int rows;
   int pos;           // position of the first row (prefill)
-  int piece, pieces;
+  int64_t num0, num1, den;
   int slot;          // of the partial result, -1: none
 };
+
+__device__ __forceinline__ int64_t uniform64(int64_t x) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<int>(x & 0xffffffff));
+  const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<int>(x >> 32));
+  return static_cast<int64_t>((uint64_t(hi) << 32) | lo);
+}
 
 // The same in scalar registers.
 __device__ __forceinline__ PagedItem uniform(const PagedItem& i) {
   PagedItem u;
   u.g = uniform(i.g);
-  u.pair = uniform(i.pair);
+  u.table = reinterpret_cast<const int32_t*>(uniform64(reinterpret_cast<int64_t>(i.table)));
   u.token = uniform(i.token);
   u.rows = uniform(i.rows);
   u.pos = uniform(i.pos);
-  u.piece = uniform(i.piece);
-  u.pieces = uniform(i.pieces);
+  u.num0 = uniform64(i.num0);
+  u.num1 = uniform64(i.num1);
+  u.den = uniform64(i.den);
   u.slot = uniform(i.slot);
   return u;
 }
 
-struct PagedPlanLds {
-  double steps[4];
-  uint32_t sum[4][3];
-  int pair;
-  uint32_t before[3];
+// A (sequence, KV head) pair: its sequence's packed rows and position, its head, its cost.
+// Pairs of a sequence are in the order of their heads' windows, widest first.
+struct RowPair {
+  int b, order, start, pos;
+  int64_t tokens;
+  PairCost cost;
 };
-
-template <int ROWS>
-__device__ __forceinline__ void pair_work(const PagedArgs& a, int pair, int& tiles, int& keys) {
-  const int b = pair / a.hkv, g = a.kv_order[pair - b * a.hkv];
-  const int p0 = a.positions[b];
-  const int64_t n = int64_t(a.seq_start[b + 1]) - a.seq_start[b];
-  tiles = keys = 0;
-  if (p0 < 0 || n <= 0 || a.seq_start[b] < 0 || a.seq_start[b + 1] > a.n_tokens) return;
-  constexpr int kShift = __builtin_ctz(ROWS);
-  tiles = static_cast<int>(((n << a.group_shift) + ROWS - 1) >> kShift);
-  const int64_t end = min(int64_t(p0) + n, int64_t(a.max_pages) << a.page_shift);
-  const int64_t span = (int64_t(a.window[g]) << a.band_shift) + (ROWS >> a.group_shift) + a.num_sink;
-  keys = static_cast<int>(min((end + 63) >> 6, (span >> 6) + 3));
+struct RowPlanLds {
+  int64_t cost[4], longest[4];
+  uint32_t tiles[4];
+  // where this work-group begins
+  int index, tile;
+  int64_t before;                // cost in front of the pair
+  RowPair pair;
+};
+__device__ __forceinline__ RowPair uniform(const RowPair& p) {
+  return {uniform(p.b), uniform(p.order), uniform(p.start), uniform(p.pos), uniform64(p.tokens),
+          {uniform(p.cost.tiles), uniform(p.cost.first), uniform(p.cost.shift), uniform(p.cost.most)}};
 }
 
-// The item of this work-group, of kThreads = 256 threads; rows = 0: none.
 template <int ROWS>
-__device__ __forceinline__ PagedItem paged_item(const PagedArgs& a, PagedPlanLds& s) {
+__device__ __forceinline__ RowPair row_pair(const PagedArgs& a, int pair) {
+  RowPair p;
+  p.b = pair / a.hkv;
+  p.order = pair - p.b * a.hkv;
+  p.start = a.seq_start[p.b];
+  const int end = a.seq_start[p.b + 1];
+  p.pos = a.positions[p.b];
+  p.tokens = p.start < 0 || end > a.n_tokens ? 0 : int64_t(end) - p.start;
+  p.cost = pair_cost(p.tokens, p.pos, a.window_in_order[p.order], a.band_shift, a.num_sink, a.group_shift, ROWS,
+                     int64_t(a.max_pages) << a.page_shift);
+  return p;
+}
+
+// Calls tile(item) for each row tile that this work-group has a part in (256 threads).
+// Work-group uniform; `tile` ends with a barrier where LDS is used again.
+template <int ROWS, class Tile>
+__device__ __forceinline__ void for_each_row_tile(const PagedArgs& a, RowPlanLds& s, Tile&& tile) {
   constexpr int kThreads = 256;
   const int pairs = a.batch * a.hkv;
   const int each = (pairs + kThreads - 1) / kThreads;
   const int p0 = static_cast<int>(threadIdx.x) * each;
   const int p1 = min(pairs, p0 + each);
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-  int tiles = 0, keys = 0;
-  double steps = 0.0;
+  int64_t cost = 0, longest = 0;
+  uint32_t tiles = 0;
+  RowPair mine = {};                                 // the thread's last pair, of one the only one
   for (int p = p0; p < p1; ++p) {
-    pair_work<ROWS>(a, p, tiles, keys);
-    steps += double(tiles) * keys;
+    mine = row_pair<ROWS>(a, p);
+    const PairCost& c = mine.cost;
+    cost += c.before(c.tiles);
+    longest = max(longest, c.longest());
+    tiles += c.tiles;
   }
-#pragma unroll
-  for (int off = 1; off < 64; off *= 2) steps += __shfl_xor(steps, off, 64);
-  if (lane == 0) s.steps[wave] = steps;
-  __syncthreads();
-  steps = s.steps[0] + s.steps[1] + s.steps[2] + s.steps[3];
-  const int longest = max(a.least_tiles, static_cast<int>(min(ceil(steps / a.slots), 1.0e9)));   // L
-
-  // items, pieces of cut tiles, cut tiles
-  uint32_t own[3] = {0, 0, 0};
-  auto add = [&](uint32_t (&c)[3]) {
-    const uint32_t pieces = min((keys + longest - 1) / max(longest, 1), kPagedMaxPieces);
-    c[0] += tiles * pieces;
-    c[1] += pieces > 1 ? tiles * pieces : 0;
-    c[2] += pieces > 1 ? tiles : 0;
-    return pieces;
-  };
-  for (int p = p0; p < p1; ++p) {
-    if (each > 1) pair_work<ROWS>(a, p, tiles, keys);
-    add(own);
-  }
-  uint32_t incl[3] = {own[0], own[1], own[2]};
+  int64_t cost_to = cost;
+  uint32_t tiles_to = tiles;
 #pragma unroll
   for (int off = 1; off < 64; off *= 2) {
-#pragma unroll
-    for (int c = 0; c < 3; ++c) {
-      const uint32_t other = __shfl_up(incl[c], off, 64);
-      incl[c] += lane >= off ? other : 0;
-    }
+    const int64_t c = __shfl_up(cost_to, off, 64);
+    const uint32_t t = __shfl_up(tiles_to, off, 64);
+    cost_to += lane >= off ? c : 0;
+    tiles_to += lane >= off ? t : 0;
+    longest = max(longest, static_cast<int64_t>(__shfl_xor(longest, off, 64)));
   }
   if (lane == 63) {
-#pragma unroll
-    for (int c = 0; c < 3; ++c) s.sum[wave][c] = incl[c];
+    s.cost[wave] = cost_to;
+    s.longest[wave] = longest;
+    s.tiles[wave] = tiles_to;
   }
   __syncthreads();
-  uint32_t total = 0, cut = 0, at[3];
-#pragma unroll
-  for (int c = 0; c < 3; ++c) at[c] = incl[c] - own[c];
+  int64_t units = 0, before = cost_to - cost;
+  uint32_t all = 0, tiles_before = tiles_to - tiles;
+  longest = 0;
 #pragma unroll
   for (int v = 0; v < 4; ++v) {
-    total += s.sum[v][0];
-    cut += s.sum[v][2];
-#pragma unroll
-    for (int c = 0; c < 3; ++c) at[c] += v < wave ? s.sum[v][c] : 0;
+    before += v < wave ? s.cost[v] : 0;
+    tiles_before += v < wave ? s.tiles[v] : 0;
+    units += s.cost[v];
+    all += s.tiles[v];
+    longest = max(longest, s.longest[v]);
   }
-  // (more items than work-groups: seq_start is no packing of n_tokens rows, and nothing is merged)
-  if (blockIdx.x == 0 && threadIdx.x == 0)
-    a.plan[0] = total <= gridDim.x ? static_cast<int32_t>(min(cut, static_cast<uint32_t>(a.slots))) : 0;
+  units = uniform64(units);
+  longest = uniform64(longest);
+  all = uniform(all);
 
-  // Items go to the dies in units of 16 neighbours, which share keys, one unit to each die
-  // in turn and back again; few items singly.
-  const uint32_t unit = total >= 16 * kNumXcd * 4 ? 16 : 1;
-  const uint32_t die = blockIdx.x % kNumXcd, local = blockIdx.x / kNumXcd;
-  const uint32_t round = local / unit;
-  const uint32_t item = (round * kNumXcd + (round & 1 ? kNumXcd - 1 - die : die)) * unit + local % unit;
-  PagedItem it = {};
-  if (item >= total) return it;
-  if (item >= at[0] && item < at[0] + own[0]) {      // one thread
-    int p = p0;
+  // A row tile of a pair, whole or in part.
+  auto item_of = [&](const RowPair& p, int i, int64_t num0, int64_t num1, int64_t den, int slot) {
+    const int first = i * (ROWS >> a.group_shift);           // token of the sequence's new ones
+    PagedItem it;
+    it.g = a.kv_order[p.order];
+    it.table = a.table + (int64_t(p.b) * a.hkv + it.g) * a.max_pages;
+    it.token = p.start + first;
+    it.rows = static_cast<int>(min(int64_t(ROWS), (p.tokens << a.group_shift) - int64_t(i) * ROWS));
+    it.pos = static_cast<int>(min(int64_t(p.pos) + first, int64_t(0x7fffffff) - ROWS));
+    it.num0 = num0;
+    it.num1 = num1;
+    it.den = den;
+    it.slot = slot;
+    return it;
+  };
+
+  // Whole row tiles: where the longest is not worth cutting, or short beside what each of the
+  // resident work-groups has to do.
+  PagedSeg* const segs = reinterpret_cast<PagedSeg*>(a.plan);
+  if (longest <= a.whole_cost || 2 * longest * a.slots <= units) {
+    if (blockIdx.x < static_cast<uint32_t>(a.slots) && threadIdx.x == 0) segs[blockIdx.x].rows = 0;
+    // Dealt to the dies in units of 16 neighbours, one unit to each die in turn and back
+    // again; few singly.  Of a pair the last first: theirs are the most keys.
+    const uint32_t unit = all >= 16 * kNumXcd * 4 ? 16 : 1;
+    const uint32_t die = blockIdx.x % kNumXcd, local = blockIdx.x / kNumXcd;
+    const uint32_t round = local / unit;
+    const uint32_t n = (round * kNumXcd + (round & 1 ? kNumXcd - 1 - die : die)) * unit + local % unit;
+    if (n >= all) return;
+    if (n >= tiles_before && n < tiles_before + tiles) {     // one thread
+      uint32_t at = tiles_before;
+      for (int p = p0; each > 1; ++p) {
+        mine = row_pair<ROWS>(a, p);
+        if (n < at + mine.cost.tiles) break;
+        at += mine.cost.tiles;
+      }
+      s.tile = static_cast<int>(mine.cost.tiles - 1 - (n - at));
+      s.pair = mine;
+    }
+    __syncthreads();
+    const RowPair p = uniform(s.pair);
+    const int i = uniform(s.tile);
+    tile(item_of(p, i, 0, 1, 1, -1));
+    return;
+  }
+
+  // Pieces.  Workers of neighbouring pieces sit on one die.
+  const RowSplit split = row_split(units, a.least_cost, a.log_slots);
+  if (blockIdx.x >= static_cast<uint32_t>(a.slots)) return;
+  const int workers = split.workers(), per_die = max(1, workers / kNumXcd);
+  int w = static_cast<int>(blockIdx.x);
+  if (w < workers && workers >= kNumXcd) w = w % kNumXcd * per_die + w / kNumXcd;
+  PagedSeg cut = {0, 0, 0, 0};
+  if (w < workers) {
+    int64_t x = uniform64(split.start(w));
+    const int64_t x_end = uniform64(split.start(w + 1));
+    if (x >= before && x < before + cost) {                  // one thread
+      int64_t at = before;
+      int p = p0;
+      for (; each > 1; ++p) {
+        mine = row_pair<ROWS>(a, p);
+        const int64_t n = mine.cost.before(mine.cost.tiles);
+        if (x < at + n) break;
+        at += n;
+      }
+      s.index = p;
+      s.before = at;
+      s.pair = mine;
+    }
+    __syncthreads();
+    int pair = uniform(s.index);
+    int64_t at = uniform64(s.before);
+    RowPair p = uniform(s.pair);
+    int i = 0;                                               // the row tile that x lies in: 64 probes at once
+    for (int n = p.cost.tiles; n > 1;) {
+      const int stride = (n + 63) >> 6;
+      const bool below = lane * stride < n && p.cost.before(i + lane * stride) <= x - at;
+      const int k = __builtin_popcountll(__ballot(below)) - 1;
+      i += k * stride;
+      n = min(stride, n - k * stride);
+    }
+    i = uniform(i);
     while (true) {
-      if (each > 1) pair_work<ROWS>(a, p, tiles, keys);
-      uint32_t c[3] = {0, 0, 0};
-      add(c);
-      if (item < at[0] + c[0]) break;
-#pragma unroll
-      for (int k = 0; k < 3; ++k) at[k] += c[k];
-      ++p;
-    }
-    s.pair = p;
-#pragma unroll
-    for (int k = 0; k < 3; ++k) s.before[k] = at[k];
-  }
-  __syncthreads();
-  const int pair = uniform(s.pair);
-  const uint32_t k = item - uniform(s.before[0]);
-  pair_work<ROWS>(a, pair, tiles, keys);
-  tiles = uniform(tiles);
-  it.pieces = uniform(min((keys + longest - 1) / max(longest, 1), kPagedMaxPieces));
-  const int b = pair / a.hkv;
-  it.g = uniform(a.kv_order[pair - b * a.hkv]);
-  it.pair = b * a.hkv + it.g;
-  const int start = uniform(a.seq_start[b]);
-  const int64_t rows = (int64_t(uniform(a.seq_start[b + 1])) - start) << a.group_shift;
-  const int from_end = k / it.pieces;                // the last row tiles first: theirs are the most keys
-  it.piece = k - from_end * it.pieces;
-  const int tile = tiles - 1 - from_end;
-  const int tok = tile * (ROWS >> a.group_shift);
-  it.token = start + tok;
-  it.rows = static_cast<int>(min(int64_t(ROWS), rows - int64_t(tile) * ROWS));
-  it.pos = static_cast<int>(min(int64_t(uniform(a.positions[b])) + tok, int64_t(0x7fffffff) - ROWS));
-  it.slot = -1;
-  if (it.pieces > 1) {
-    it.slot = uniform(s.before[1]) + k;
-    const uint32_t seg = uniform(s.before[2]) + from_end;
-    if (it.slot >= 2 * a.slots || seg >= static_cast<uint32_t>(a.slots)) {   // not for a well-formed seq_start
-      it.rows = 0;
-    } else if (it.piece == 0 && threadIdx.x == 0) {
-      reinterpret_cast<PagedSeg*>(a.plan + 8)[seg] = {it.token, it.g, it.rows, it.slot, it.pieces, {0, 0, 0}};
+      const int n = p.cost.tiles;
+      for (; i < n && x < x_end; ++i) {
+        const int64_t c0 = at + uniform64(p.cost.before(i)), c1 = at + uniform64(p.cost.before(i + 1));
+        const int64_t end = min(x_end, c1);
+        const bool whole = x == c0 && end == c1;
+        const PagedItem it = item_of(p, i, x - c0, end - c0, c1 - c0, whole ? -1 : x == c0 ? 2 * w + 1 : 2 * w);
+        if (x == c0 && !whole) cut = {it.token, it.g, it.rows, split.worker_of(c1 - 1) - w + 1};
+        tile(it);
+        x = end;
+      }
+      if (x >= x_end) break;
+      at += uniform64(p.cost.before(n));
+      i = 0;
+      ++pair;
+      p = uniform(row_pair<ROWS>(a, pair));
     }
   }
-  return it;
+  if (threadIdx.x == 0) segs[w] = cut;
 }
 
-// The item of a work-group over the shared prefix: rows are (sequence, query head) pairs.
-// The pieces of the heads are counted on the host; all of them leave partial results.
-template <int ROWS>
-__device__ __forceinline__ PagedItem prefix_item(const PagedArgs& a) {
-  const int item = static_cast<int>(blockIdx.x);
+// The same over a shared prefix: rows are (sequence, query head) pairs, all heads have the
+// same number of row tiles, and head g's cost a.prefix_cost[g + 1] - a.prefix_cost[g] key
+// tiles each, cut for 2^a.log_prefix_workers work-groups.  All of them leave partial results, at slot
+// worker + row tile, which is unique as workers and row tiles are ordered alike.
+template <int ROWS, class Tile>
+__device__ __forceinline__ void for_each_prefix_tile(const PagedArgs& a, int w, Tile&& tile) {
   const int lane = threadIdx.x & 63;
-  const int end = a.prefix_slot[min(lane, a.hkv - 1) + 1];
-  PagedItem it = {};
-  it.g = __builtin_popcountll(__ballot(lane < a.hkv && end <= item));
-  if (it.g >= a.hkv) return it;
-  const int first = a.prefix_slot[it.g];
-  const int tiles = static_cast<int>(((int64_t(a.batch) << a.group_shift) + ROWS - 1) / ROWS);
-  it.pieces = (a.prefix_slot[it.g + 1] - first) / tiles;
-  const int tile = (item - first) / it.pieces;
-  it.piece = (item - first) - tile * it.pieces;
-  it.token = tile * (ROWS >> a.group_shift);
-  it.rows = min(ROWS, (a.batch << a.group_shift) - tile * ROWS);
-  it.slot = item;
-  return it;
+  const int tiles = prefix_row_tiles<ROWS>(a.batch, a.group_shift);
+  const int64_t my_end = a.prefix_cost[min(lane, a.hkv - 1) + 1];
+  const RowSplit split = {int64_t(a.prefix_cost[a.hkv]) * tiles, a.log_prefix_workers};
+  if (w >= split.workers()) return;
+  int64_t x = uniform64(split.start(w));
+  const int64_t x_end = uniform64(split.start(w + 1));
+  int g = __builtin_popcountll(__ballot(lane < a.hkv && my_end * tiles <= x));
+  while (x < x_end) {
+    const int64_t first = int64_t(a.prefix_cost[g]) * tiles, each = a.prefix_cost[g + 1] - a.prefix_cost[g];
+    for (int i = uniform(static_cast<int>(static_cast<uint32_t>(x - first) / static_cast<uint32_t>(each))); i < tiles && x < x_end; ++i) {
+      const int64_t c0 = first + i * each;
+      const int64_t end = min(x_end, c0 + each);
+      PagedItem it;
+      it.g = g;
+      it.table = a.prefix_table + int64_t(g) * a.max_pages;
+      it.token = i * (ROWS >> a.group_shift);
+      it.rows = static_cast<int>(min(int64_t(ROWS), (int64_t(a.batch) << a.group_shift) - int64_t(i) * ROWS));
+      it.pos = 0;
+      it.num0 = x - c0;
+      it.num1 = end - c0;
+      it.den = each;
+      it.slot = w + g * tiles + i;
+      tile(it);
+      x = end;
+    }
+    ++g;
+  }
 }
 
 }  // namespace moa

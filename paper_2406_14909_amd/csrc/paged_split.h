@@ -1,7 +1,7 @@
-// How the keys of a paged decode call are cut into workers' pieces.  The lengths live on
-// the device, so every work-group forms the split itself, from the positions, and the
-// first one leaves it to the merge.  Plain C++, so that it also compiles without a GPU
-// toolchain.
+// How the work of a paged call is cut into workers' pieces: of a decode call the keys of its
+// caches, of many query rows (a prefill, or a batch over a shared prefix) the key tiles of
+// its row tiles.  The lengths live on the device, so every work-group forms the split
+// itself.  Plain C++, so that it also compiles without a GPU toolchain.
 #pragma once
 
 #include "paged.h"
@@ -58,5 +58,89 @@ struct VisiblePages {
     return sink ? index - first_sink : index - first_band + sink_pages;
   }
 };
+
+// ---------------------------------------------------------------------------
+// Row tiles.
+// ---------------------------------------------------------------------------
+constexpr int kTileCost = 96;        // keys: what a row tile's start and end cost, about
+
+// A piece costs two partial results of 128 rows on their way out and back (67 KB each) and a
+// start, so it has kLeastRowCost at least, and a call whose row tiles all cost no more than
+// kWholeRowCost is not cut (8 heads x 4 query heads: 512 tokens, tiles of up to 608: whole
+// 22 us, cut 43; 1,500 tokens, up to 1,596: 63 and 61; 64 tokens behind 8,000: 36, 33, 38 and
+// 54 us in pieces of 128, 256, 512 and 1,024).
+constexpr int kLeastRowCost = 256;
+constexpr int kWholeRowCost = 1024;
+
+// Cost of the row tiles of one (sequence, KV head) pair: tile i ends at key
+// min(first + step * (i + 1), most), step being its tokens.
+struct PairCost {
+  int tiles, first, shift, most;     // step = 1 << shift
+  MOA_PAGED_FN int64_t before(int64_t i) const {                  // of tiles 0 .. i - 1
+    int64_t ramp = most > first ? (most - first) >> shift : 0;    // tiles that end within `most`
+    ramp = ramp < i ? ramp : i;
+    return i * kTileCost + ramp * first + ((ramp * (ramp + 1)) << shift) / 2 + (i - ramp) * most;
+  }
+  MOA_PAGED_FN int64_t longest() const { return tiles > 0 ? before(tiles) - before(tiles - 1) : 0; }
+};
+
+MOA_PAGED_FN PairCost pair_cost(int64_t tokens, int pos, int window, int band_shift, int num_sink, int group_shift,
+                                int tile_rows, int64_t capacity) {
+  const int step = tile_rows >> group_shift;
+  PairCost c = {0, 0, __builtin_ctz(static_cast<unsigned>(step)), 0};
+  if (pos < 0 || tokens <= 0) return c;
+  c.tiles = static_cast<int>(((tokens << group_shift) + tile_rows - 1) / tile_rows);
+  int64_t most = (int64_t(window) << band_shift) + step + num_sink + 64;
+  most = most < capacity ? most : capacity;
+  const int64_t end = int64_t(pos) + tokens;
+  c.most = static_cast<int>(most < end ? most : end);
+  c.first = static_cast<int>(pos < capacity ? pos : capacity);
+  return c;
+}
+
+// 2^log_workers pieces of equal cost, to one: a power of two, so that no piece's start takes
+// a division (a chain of several hundred cycles, in 64 bits).
+struct RowSplit {
+  int64_t units;
+  int32_t log_workers;
+  MOA_PAGED_FN int32_t workers() const { return units > 0 ? 1 << log_workers : 0; }
+  MOA_PAGED_FN int64_t start(int64_t w) const { return (units * w) >> log_workers; }
+  MOA_PAGED_FN int32_t worker_of(int64_t x) const {
+    // near enough in fp32, then set right
+    int32_t w = static_cast<int32_t>(static_cast<float>(x) * (static_cast<float>(1 << log_workers) / static_cast<float>(units)));
+    w = w < (1 << log_workers) ? w : (1 << log_workers) - 1;
+    while (start(w) > x) --w;
+    while (start(w + 1) <= x) ++w;
+    return w;
+  }
+};
+// As many pieces of at least `least` as there are, up to 2^log_most.
+MOA_PAGED_FN RowSplit row_split(int64_t units, int32_t least, int32_t log_most) {
+  RowSplit s = {units, log_most};
+  while (s.log_workers > 0 && (units >> s.log_workers) < least) --s.log_workers;
+  return s;
+}
+// Key tile of `n` at which the part [0, num) of den of a row tile ends: the same for the
+// worker in front and the one behind, 0 at 0 and n at den, and rising with num.
+MOA_PAGED_FN int32_t row_part(int32_t n, int64_t num, int64_t den) {
+  if (num >= den) return n;
+  const int32_t t = static_cast<int32_t>(static_cast<float>(n) * (static_cast<float>(num) / static_cast<float>(den)));
+  return t < n ? t : n;
+}
+
+// What the merge has to know of a row tile that was cut: its pieces are those of `pieces`
+// workers, the first of which wrote to slot 2 w + 1 and the others to 2 w.
+struct PagedSeg {
+  int32_t token;     // first packed token
+  int32_t head;      // KV head
+  int32_t rows;      // 0: nothing to merge
+  int32_t pieces;
+};
+
+// Row tiles of a KV head's queries over a shared prefix.
+template <int ROWS>
+MOA_PAGED_FN int prefix_row_tiles(int batch, int group_shift) {
+  return static_cast<int>(((int64_t(batch) << group_shift) + ROWS - 1) / ROWS);
+}
 
 }  // namespace moa

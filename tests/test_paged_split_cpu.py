@@ -74,6 +74,62 @@ extern "C" int walk(int pairs, const uint32_t* rounds, uint32_t slots, uint32_t*
   return 0;
 }
 
+// Row tiles of pairs (tokens, position, window) cut for `slots` workers: 0 when every key tile
+// of every row tile is walked once, the merge finds all pieces in slots of their own, and no
+// piece costs more than its share.  tiles[i]: key tiles of a row tile, by some rule.
+extern "C" int row_walk(int pairs, const int64_t* tokens, const int* pos, const int* window, int sink, int gs, int rows,
+                        int64_t cap, int least, int log_slots, int* out) {
+  std::vector<PairCost> cost;
+  std::vector<int64_t> at;
+  int64_t units = 0;
+  for (int i = 0; i < pairs; ++i) {
+    cost.push_back(pair_cost(tokens[i], pos[i], window[i], 0, sink, gs, rows, cap));
+    const PairCost& c = cost.back();
+    if (c.before(0) != 0) return 1;
+    const int step = rows >> gs;
+    int64_t sum = 0;
+    for (int k = 0; k < c.tiles && k < 300; ++k) {
+      int64_t end = int64_t(c.first) + step * (k + 1);
+      sum += kTileCost + std::min<int64_t>(end, c.most);
+      if (c.before(k + 1) != sum) return 2;
+    }
+    if (c.tiles > 0 && int64_t(c.tiles) * step < tokens[i]) return 3;
+    at.push_back(units);
+    units += c.before(c.tiles);
+  }
+  const RowSplit s = row_split(units, least, log_slots);
+  const int workers = s.workers();
+  if (units == 0) return workers == 0 ? 0 : 4;
+  if (workers < 1 || workers > 1 << log_slots || s.start(0) != 0 || s.start(workers) != units) return 5;
+  if (workers > 1 && units / workers < least) return 10;
+  std::vector<char> used(2 * size_t(workers), 0);
+  int parts = 0;
+  for (int i = 0; i < pairs; ++i) {
+    for (int k = 0; k < cost[i].tiles; ++k) {
+      const int64_t c0 = at[i] + cost[i].before(k), c1 = at[i] + cost[i].before(k + 1);
+      const int w0 = s.worker_of(c0), w1 = s.worker_of(c1 - 1);
+      const int n = 1 + (k * 7 + i) % 50;                     // key tiles
+      int next = 0;
+      for (int w = w0; w <= w1; ++w) {
+        const int64_t x = std::max(c0, s.start(w)), end = std::min(c1, s.start(w + 1));
+        if (end <= x) return 6;
+        const int t0 = row_part(n, x - c0, c1 - c0), t1 = row_part(n, end - c0, c1 - c0);
+        if (t0 != next || t1 < t0) return 7;
+        next = t1;
+        if (w0 != w1) {
+          const size_t slot = 2 * size_t(w) + (x == c0 ? 1 : 0);
+          if ((w == w0) != (x == c0) || used[slot]++) return 8;
+        }
+      }
+      if (next != n) return 9;
+      parts = std::max(parts, w1 - w0 + 1);
+    }
+  }
+  out[0] = workers;
+  out[1] = parts;
+  return 0;
+}
+
 extern "C" uint32_t rounds(int pos, int count, int shift, int merge) { return paged_rounds(pos, count, shift, merge != 0); }
 """
 
@@ -120,3 +176,18 @@ def test_rounds(lib):
     assert [lib.rounds(-1, 0, 7, m) for m in (0, 1)] == [0, 0]
     assert [lib.rounds(5, 0, 7, m) for m in (0, 1)] == [1, 0]
     assert [lib.rounds(5, n, 7, 0) for n in (1, 128, 129)] == [1, 1, 2]
+
+
+def test_every_key_tile_of_a_row_tile_is_walked_once(lib):
+    rng = random.Random(3)
+    for _ in range(500):
+        pairs = rng.choice([1, 3, 8, 64])
+        tokens = [rng.choice([0, 1, 5, 128, rng.randint(1, 20000)]) for _ in range(pairs)]
+        pos = [rng.choice([-1, 0, 0, 100, rng.randint(0, 200000), 2 ** 31 - 5]) for _ in range(pairs)]
+        window = [rng.choice([1, 64, 1000, rng.randint(1, 100000)]) for _ in range(pairs)]
+        rows = rng.choice([32, 128])
+        cap = rng.choice([64, 5000, 1 << 20, 1 << 30])
+        out = (ctypes.c_int * 2)()
+        args = ((ctypes.c_int64 * pairs)(*tokens), (ctypes.c_int * pairs)(*pos), (ctypes.c_int * pairs)(*window))
+        assert lib.row_walk(pairs, *args, rng.choice([0, 64, 3000]), rng.choice([0, 1, 2, 3]), rows, ctypes.c_int64(cap),
+                            rng.choice([1, 128, 512]), rng.choice([0, 6, 9]), out) == 0, (tokens, pos, window, rows, cap)
