@@ -172,7 +172,7 @@ __global__ void __launch_bounds__(kWaves * 64, 2) paged_rows_kernel(PagedArgs a)
     auto tile_j0 = [&](int t) { return (t < ta ? t : tb + (t - ta)) * BN; };
 
     const int ps_mask = (1 << a.page_shift) - 1;
-    const int32_t* const table = it.table;
+    const int32_t* const table = (kShared ? a.prefix_table : a.table) + it.table;
 
     // Page numbers of a tile's four groups of 16 keys.
     struct Pages {

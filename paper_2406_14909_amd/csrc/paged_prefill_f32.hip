@@ -85,7 +85,7 @@ __global__ void __launch_bounds__(kWaves * 64, D == 64 ? 2 : 1) paged_rows_f32_k
     const int ntiles = ta + (band_lo < key_end ? max(0, (key_end - 1) / 64 - tb + 1) : 0);
     const int t0 = uniform(row_part(ntiles, it.num0, it.den));
     const int t1 = uniform(row_part(ntiles, it.num1, it.den));
-    const int32_t* const table = it.table;
+    const int32_t* const table = (kShared ? a.prefix_table : a.table) + it.table;
 
     // First key of the wave's u-th 32-key tile, and the pool's row of this lane's key there.
     auto tile_j0 = [&](int u) {
@@ -212,8 +212,17 @@ __global__ void __launch_bounds__(kWaves * 64, D == 64 ? 2 : 1) paged_rows_f32_k
         for (int r = 0; r < 16; ++r) oacc[dt][r] = oacc[dt][r] * f1 + p[(dt * 16 + r) * 64] * f2;
     }
     if (!in_tile) return;
-    float* out;
-    float f = 1.0f;
+    auto store = [&](float* out, int step, float f) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int grp = 0; grp < 4; ++grp) {
+          f32x4 x;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = oacc[dt][grp * 4 + e] * f;
+          *reinterpret_cast<f32x4*>(out + (dt * 4 + grp) * step) = x;
+        }
+    };
     if (it.slot >= 0) {                   // by rows, or as the lanes hold them (see paged_prefill.hip)
       float* const pp = a.rows_part + int64_t(it.slot) * kRows * (kShared ? PS : D + 2);
       float* const st = kShared ? pp + my_row * PS + D : pp + kRows * D + my_row * 2;
@@ -221,21 +230,11 @@ __global__ void __launch_bounds__(kWaves * 64, D == 64 ? 2 : 1) paged_rows_f32_k
         st[0] = m_run;
         st[1] = l_run;
       }
-      out = kShared ? pp + my_row * PS + half * 4 : pp + (row_block * (D / 8) * 64 + lane) * 4;
-    } else {
-      out = static_cast<float*>(a.o) + (int64_t(token) * a.hq + head) * D + half * 4;
-      f = l_run > 0.0f ? 1.0f / l_run : 0.0f;               // a row that sees no key is 0
+      if constexpr (kShared) store(pp + my_row * PS + half * 4, 8, 1.0f);
+      else store(pp + (row_block * (D / 8) * 64 + lane) * 4, 256, 1.0f);
+    } else {                              // a row that sees no key is 0
+      store(static_cast<float*>(a.o) + (int64_t(token) * a.hq + head) * D + half * 4, 8, l_run > 0.0f ? 1.0f / l_run : 0.0f);
     }
-    const int step = !kShared && it.slot >= 0 ? 256 : 8;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int grp = 0; grp < 4; ++grp) {
-        f32x4 x;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = oacc[dt][grp * 4 + e] * f;
-        *reinterpret_cast<f32x4*>(out + (dt * 4 + grp) * step) = x;
-      }
   };
   if constexpr (kShared) for_each_prefix_tile<kRows>(a, blockIdx.x, tile);
   else for_each_row_tile<kRows>(a, s_mem.plan, tile);

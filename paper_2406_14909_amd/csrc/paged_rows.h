@@ -23,7 +23,7 @@ namespace moa {
 // One row tile and a part [num0, num1) of den of its key tiles.
 struct PagedItem {
   int g;
-  const int32_t* table;
+  int64_t table;     // first entry in the page table
   int token;         // packed token of the first row
   int rows;
   int pos;           // position of the first row (prefill)
@@ -41,7 +41,7 @@ __device__ __forceinline__ int64_t uniform64(int64_t x) {
 __device__ __forceinline__ PagedItem uniform(const PagedItem& i) {
   PagedItem u;
   u.g = uniform(i.g);
-  u.table = reinterpret_cast<const int32_t*>(uniform64(reinterpret_cast<int64_t>(i.table)));
+  u.table = uniform64(i.table);
   u.token = uniform(i.token);
   u.rows = uniform(i.rows);
   u.pos = uniform(i.pos);
@@ -142,7 +142,7 @@ __device__ __forceinline__ void for_each_row_tile(const PagedArgs& a, RowPlanLds
     const int first = i * (ROWS >> a.group_shift);           // token of the sequence's new ones
     PagedItem it;
     it.g = a.kv_order[p.order];
-    it.table = a.table + (int64_t(p.b) * a.hkv + it.g) * a.max_pages;
+    it.table = (int64_t(p.b) * a.hkv + it.g) * a.max_pages;
     it.token = p.start + first;
     it.rows = static_cast<int>(min(int64_t(ROWS), (p.tokens << a.group_shift) - int64_t(i) * ROWS));
     it.pos = static_cast<int>(min(int64_t(p.pos) + first, int64_t(0x7fffffff) - ROWS));
@@ -260,7 +260,7 @@ __device__ __forceinline__ void for_each_prefix_tile(const PagedArgs& a, int w, 
       const int64_t end = min(x_end, c0 + each);
       PagedItem it;
       it.g = g;
-      it.table = a.prefix_table + int64_t(g) * a.max_pages;
+      it.table = int64_t(g) * a.max_pages;
       it.token = i * (ROWS >> a.group_shift);
       it.rows = static_cast<int>(min(int64_t(ROWS), (int64_t(a.batch) << a.group_shift) - int64_t(i) * ROWS));
       it.pos = 0;
