@@ -26,8 +26,7 @@ BINDING_PATH = os.path.join(PKG_DIR, "_binding.so")
 PROBES = ["stream_read", "mfma_loop"]
 
 HIP_SOURCES = ["kv_append.hip", "decode.hip", "prefill.hip", "prefill_f32.hip", "influence.hip", "rule_loss.hip",
-               "paged_append.hip", "paged_decode.hip", "paged_prefill.hip", "paged_prefill_f32.hip",
-               "paged_merge.hip"]
+               "paged_append.hip", "paged_decode.hip", "paged_prefill.hip", "paged_shared.hip", "paged_merge.hip"]
 HOST_SOURCES = ["moa_api.cpp", "paged_api.cpp"]
 
 ARCH = "gfx950"

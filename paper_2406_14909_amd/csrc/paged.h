@@ -65,7 +65,7 @@ struct PagedArgs {
   int32_t least_cost;            // rows: keys of a piece, at least
   int32_t whole_cost;            // rows: keys of a row tile that is not worth cutting
   int32_t log_slots;             // rows: log2(slots)
-  int32_t log_prefix_workers;    // a shared prefix is cut for 2^log_prefix_workers work-groups
+  int32_t prefix_items;          // work-groups over a shared prefix
   int32_t n_tokens;
   int32_t batch;
   int32_t hq;
@@ -81,7 +81,7 @@ struct PagedArgs {
   int32_t window[MOA_MAX_KV_HEADS];
   int32_t window_in_order[MOA_MAX_KV_HEADS];   // and the same, widest first,
   int16_t kv_order[MOA_MAX_KV_HEADS];          // of these KV heads
-  int32_t prefix_cost[MOA_MAX_KV_HEADS + 1];   // key tiles of the heads in front, of a shared prefix
+  int32_t prefix_piece[MOA_MAX_KV_HEADS + 1];  // first piece of each head's keys of a shared prefix
 };
 
 // Keys of one query position, as a run of sinks and a band behind them, both cut at
@@ -111,12 +111,16 @@ constexpr int kPagedMaxWorkers = 4096;   // decode workers (work-groups) per lau
 int launch_paged_append(const PagedAppendArgs& a, int dtype, int head_dim, void* stream);
 constexpr int kPagedLogRowGroups = 9;
 constexpr int kPagedRowGroups = 1 << kPagedLogRowGroups;   // work-groups that row tiles are cut for (two per compute unit)
+// Work-groups over a shared prefix, about, and over the keys behind it: one of each per
+// compute unit (16 x 8 x 4 heads on 8,001 keys and 48 x 8 x 8 on 32,700: 22.2 and 52.5 us; 384
+// for the prefix 26.6 and 58.6, 192 23.7 and 56.4; 512 behind it 24.6 and 57.8).
+constexpr int kPagedPrefixItems = 256;
 MOA_PAGED_FN int paged_tile_rows(int dtype) { return dtype == MOA_BF16 ? 128 : 64; }
 
-// The launches of row tiles take their grid: no fewer work-groups than items.
-int launch_paged_rows(const PagedArgs& a, int head_dim, int64_t groups, void* stream);       // bf16
-int launch_paged_rows_f32(const PagedArgs& a, int head_dim, int64_t groups, void* stream);
+// groups: no fewer than there are row tiles, nor than a.slots.
+int launch_paged_rows(const PagedArgs& a, int dtype, int head_dim, int64_t groups, void* stream);
 int launch_paged_merge(const PagedArgs& a, int dtype, int head_dim, void* stream);
+int launch_paged_shared(const PagedArgs& a, int dtype, int head_dim, int group, void* stream);
 int launch_paged_decode(const PagedArgs& a, int dtype, int head_dim, int group, void* stream);
 
 }  // namespace moa

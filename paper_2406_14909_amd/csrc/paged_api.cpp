@@ -119,7 +119,7 @@ DecodeSpace decode_space(const moa_plan_s& p, int32_t batch) {
   DecodeSpace s;
   s.plan = up256((kPagedMaxWorkers + pairs) * p.group * row_bytes(p));
   s.rows = s.plan + up256((pairs + 5) * sizeof(int32_t));
-  s.bytes = s.rows + up256((tiles + kPagedRowGroups) * rows * row_bytes(p));
+  s.bytes = s.rows + up256(std::max<size_t>(tiles, kPagedPrefixItems) * rows * row_bytes(p));
   return s;
 }
 struct PrefillSpace {
@@ -268,8 +268,7 @@ moa_status_t moa_paged_prefill(const moa_plan_t* plan, const moa_pages_t* pages,
   for (int h = 0; h < d.num_kv_heads; ++h) a.window_in_order[h] = a.window[a.kv_order[h]];
   // a work-group per row tile, dealt to the dies in whole rounds, or per piece
   const int64_t groups = std::max<int64_t>((tiles + 127) / 128 * 128, kPagedRowGroups);
-  int err = d.dtype == MOA_BF16 ? launch_paged_rows(a, d.head_dim, groups, hip_stream)
-                                : launch_paged_rows_f32(a, d.head_dim, groups, hip_stream);
+  int err = launch_paged_rows(a, d.dtype, d.head_dim, groups, hip_stream);
   if (!err) err = launch_paged_merge(a, d.dtype, d.head_dim, hip_stream);
   return launched(who, err);
 }
@@ -311,17 +310,28 @@ moa_status_t moa_paged_decode_shared(const moa_plan_t* plan, const moa_pages_t* 
     a.rows_part = reinterpret_cast<float*>(ws + space.rows);
     const int rows = paged_tile_rows(d.dtype);
     const int64_t tiles = (int64_t(batch) * plan->group + rows - 1) / rows;
-    int64_t cost = 0;
+    // Pieces of as few key tiles as give no more than kPagedPrefixItems work-groups.
+    int64_t keys[MOA_MAX_KV_HEADS], sum = 0, pieces = 0;
     for (int h = 0; h < d.num_kv_heads; ++h) {
-      a.prefix_cost[h] = static_cast<int32_t>(cost);
-      cost += (std::min<int64_t>(prefix_len, int64_t(d.num_sink) + plan->window[h] + 63) + 63) / 64;
+      keys[h] = (std::min<int64_t>(prefix_len, int64_t(d.num_sink) + plan->window[h] + 63) + 63) / 64;
+      sum += keys[h];
     }
-    a.prefix_cost[d.num_kv_heads] = static_cast<int32_t>(cost);
-    a.log_prefix_workers = row_split(cost * tiles, 2, kPagedLogRowGroups).log_workers;
-    const int64_t workers = int64_t(1) << a.log_prefix_workers;
-    const int err = d.dtype == MOA_BF16 ? launch_paged_rows(a, d.head_dim, workers, hip_stream)
-                                        : launch_paged_rows_f32(a, d.head_dim, workers, hip_stream);
-    if (err) return launched(who, err);
+    constexpr int64_t most = kPagedPrefixItems;
+    int64_t longest = std::max<int64_t>(2, (sum * tiles + most - 1) / most);
+    for (;; ++longest) {
+      pieces = 0;
+      for (int h = 0; h < d.num_kv_heads; ++h) pieces += (keys[h] + longest - 1) / longest;
+      if (pieces * tiles <= most || pieces == d.num_kv_heads) break;
+    }
+    pieces = 0;
+    for (int h = 0; h < d.num_kv_heads; ++h) {
+      a.prefix_piece[h] = static_cast<int32_t>(pieces);
+      pieces += (keys[h] + longest - 1) / longest;
+    }
+    a.prefix_piece[d.num_kv_heads] = static_cast<int32_t>(pieces);
+    a.prefix_items = static_cast<int32_t>(pieces * tiles);
+    a.slots = kPagedPrefixItems;
+    return launched(who, launch_paged_shared(a, d.dtype, d.head_dim, plan->group, hip_stream));
   }
   return launched(who, launch_paged_decode(a, d.dtype, d.head_dim, plan->group, hip_stream));
 }

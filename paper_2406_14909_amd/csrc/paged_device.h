@@ -42,6 +42,33 @@ __device__ __forceinline__ int page_row(int page, int num_pages, int page_shift)
   return static_cast<uint32_t>(page) < static_cast<uint32_t>(num_pages) ? page << page_shift : -1;
 }
 
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+
+// Transposing LDS read of four bf16: within each 16-lane group, lane 4a+b receives
+// element b of the 8-byte reads issued by lanes 4e+a (e = 0..3), as its element e.
+__device__ __forceinline__ bf16x4 read_tr(const void* p) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const i16x4 r = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (__attribute__((address_space(3))) i16x4*)(const_cast<void*>(p)));
+  return __builtin_bit_cast(bf16x4, r);
+#else
+  (void)p;
+  return bf16x4{};
+#endif
+}
+
+// acc + a + b with a, b in bf16.
+__device__ __forceinline__ float dot2_ones(bf16 a, bf16 b, float acc) {
+  typedef bf16 bf16x2 __attribute__((ext_vector_type(2)));
+#if defined(__HIP_DEVICE_COMPILE__)
+  const bf16x2 ab = {a, b};
+  const bf16x2 ones = {bf16(1.0f), bf16(1.0f)};
+  return __builtin_amdgcn_fdot2_f32_bf16(ab, ones, acc, false);
+#else
+  return acc + float(a) + float(b);
+#endif
+}
+
 // Resident work-groups of `kernel` on the current device (cached per device by the
 // caller; threads that launch at once store the same value).
 inline int resident_groups(const void* kernel, int threads, std::atomic<int>* cache) {

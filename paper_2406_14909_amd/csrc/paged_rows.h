@@ -20,6 +20,8 @@
 namespace moa {
 
 
+constexpr float kRescaleSlack = 8.0f;   // log2 headroom before a running maximum is raised
+
 // One row tile and a part [num0, num1) of den of its key tiles.
 struct PagedItem {
   int g;
@@ -86,10 +88,10 @@ __device__ __forceinline__ RowPair row_pair(const PagedArgs& a, int pair) {
   return p;
 }
 
-// Calls tile(item) for each row tile that this work-group has a part in (256 threads).
+// Calls tile(item) for each row tile that work-group `block` has a part in (256 threads).
 // Work-group uniform; `tile` ends with a barrier where LDS is used again.
 template <int ROWS, class Tile>
-__device__ __forceinline__ void for_each_row_tile(const PagedArgs& a, RowPlanLds& s, Tile&& tile) {
+__device__ __forceinline__ void for_each_row_tile(const PagedArgs& a, int block, RowPlanLds& s, Tile&& tile) {
   constexpr int kThreads = 256;
   const int pairs = a.batch * a.hkv;
   const int each = (pairs + kThreads - 1) / kThreads;
@@ -157,11 +159,11 @@ __device__ __forceinline__ void for_each_row_tile(const PagedArgs& a, RowPlanLds
   // resident work-groups has to do.
   PagedSeg* const segs = reinterpret_cast<PagedSeg*>(a.plan);
   if (longest <= a.whole_cost || 2 * longest * a.slots <= units) {
-    if (blockIdx.x < static_cast<uint32_t>(a.slots) && threadIdx.x == 0) segs[blockIdx.x].rows = 0;
+    if (block < a.slots && threadIdx.x == 0) segs[block].rows = 0;
     // Dealt to the dies in units of 16 neighbours, one unit to each die in turn and back
     // again; few singly.  Of a pair the last first: theirs are the most keys.
     const uint32_t unit = all >= 16 * kNumXcd * 4 ? 16 : 1;
-    const uint32_t die = blockIdx.x % kNumXcd, local = blockIdx.x / kNumXcd;
+    const uint32_t die = block % kNumXcd, local = block / kNumXcd;
     const uint32_t round = local / unit;
     const uint32_t n = (round * kNumXcd + (round & 1 ? kNumXcd - 1 - die : die)) * unit + local % unit;
     if (n >= all) return;
@@ -184,9 +186,9 @@ __device__ __forceinline__ void for_each_row_tile(const PagedArgs& a, RowPlanLds
 
   // Pieces.  Workers of neighbouring pieces sit on one die.
   const RowSplit split = row_split(units, a.least_cost, a.log_slots);
-  if (blockIdx.x >= static_cast<uint32_t>(a.slots)) return;
+  if (block >= a.slots) return;
   const int workers = split.workers(), per_die = max(1, workers / kNumXcd);
-  int w = static_cast<int>(blockIdx.x);
+  int w = block;
   if (w < workers && workers >= kNumXcd) w = w % kNumXcd * per_die + w / kNumXcd;
   PagedSeg cut = {0, 0, 0, 0};
   if (w < workers) {
@@ -239,40 +241,30 @@ __device__ __forceinline__ void for_each_row_tile(const PagedArgs& a, RowPlanLds
   if (threadIdx.x == 0) segs[w] = cut;
 }
 
-// The same over a shared prefix: rows are (sequence, query head) pairs, all heads have the
-// same number of row tiles, and head g's cost a.prefix_cost[g + 1] - a.prefix_cost[g] key
-// tiles each, cut for 2^a.log_prefix_workers work-groups.  All of them leave partial results, at slot
-// worker + row tile, which is unique as workers and row tiles are ordered alike.
-template <int ROWS, class Tile>
-__device__ __forceinline__ void for_each_prefix_tile(const PagedArgs& a, int w, Tile&& tile) {
+// The item of work-group w over a shared prefix: rows are (sequence, query head) pairs, all
+// heads have the same number of row tiles, and head g's keys are cut into
+// a.prefix_piece[g + 1] - a.prefix_piece[g] pieces.  The row tiles of a piece are neighbours,
+// on one die at one time, so that its keys come from memory once.  All items leave partial
+// results, in slot w.  rows = 0: no item.
+template <int ROWS>
+__device__ __forceinline__ PagedItem prefix_item(const PagedArgs& a, int w) {
   const int lane = threadIdx.x & 63;
   const int tiles = prefix_row_tiles<ROWS>(a.batch, a.group_shift);
-  const int64_t my_end = a.prefix_cost[min(lane, a.hkv - 1) + 1];
-  const RowSplit split = {int64_t(a.prefix_cost[a.hkv]) * tiles, a.log_prefix_workers};
-  if (w >= split.workers()) return;
-  int64_t x = uniform64(split.start(w));
-  const int64_t x_end = uniform64(split.start(w + 1));
-  int g = __builtin_popcountll(__ballot(lane < a.hkv && my_end * tiles <= x));
-  while (x < x_end) {
-    const int64_t first = int64_t(a.prefix_cost[g]) * tiles, each = a.prefix_cost[g + 1] - a.prefix_cost[g];
-    for (int i = uniform(static_cast<int>(static_cast<uint32_t>(x - first) / static_cast<uint32_t>(each))); i < tiles && x < x_end; ++i) {
-      const int64_t c0 = first + i * each;
-      const int64_t end = min(x_end, c0 + each);
-      PagedItem it;
-      it.g = g;
-      it.table = int64_t(g) * a.max_pages;
-      it.token = i * (ROWS >> a.group_shift);
-      it.rows = static_cast<int>(min(int64_t(ROWS), (int64_t(a.batch) << a.group_shift) - int64_t(i) * ROWS));
-      it.pos = 0;
-      it.num0 = x - c0;
-      it.num1 = end - c0;
-      it.den = each;
-      it.slot = w + g * tiles + i;
-      tile(it);
-      x = end;
-    }
-    ++g;
-  }
+  const int piece = w / tiles, i = w - piece * tiles;
+  const int my_end = a.prefix_piece[min(lane, a.hkv - 1) + 1];
+  const int g = __builtin_popcountll(__ballot(lane < a.hkv && my_end <= piece));
+  PagedItem it = {};
+  if (g >= a.hkv) return it;
+  const int first = a.prefix_piece[g];
+  it.g = g;
+  it.table = int64_t(g) * a.max_pages;
+  it.token = i * (ROWS >> a.group_shift);
+  it.rows = static_cast<int>(min(int64_t(ROWS), (int64_t(a.batch) << a.group_shift) - int64_t(i) * ROWS));
+  it.num0 = piece - first;
+  it.num1 = piece - first + 1;
+  it.den = a.prefix_piece[g + 1] - first;
+  it.slot = w;
+  return it;
 }
 
 }  // namespace moa

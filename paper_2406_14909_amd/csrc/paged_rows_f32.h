@@ -12,17 +12,18 @@
 //   dimension lane % 32 of 32.
 // A lane looks up the page of its key two tiles ahead.  Keys that no row sees and keys on
 // absent pages read the pool's first row instead, and count as zeros with weight 0.
+#pragma once
+
 #include "paged_rows.h"
 
 namespace moa {
 
 namespace {
 
-constexpr int kWaves = 4;
-constexpr int kRows = 64;
-constexpr float kRescaleSlack = 8.0f;   // log2 headroom before the offset is raised
+constexpr int kRowsF32 = 64;             // query rows per work-group
+constexpr int kRowWaves = 4;
 
-__device__ __forceinline__ f32x16 mma(float a, float b, const f32x16& c) {
+__device__ __forceinline__ f32x16 mma32f(float a, float b, const f32x16& c) {
 #if defined(__HIP_DEVICE_COMPILE__)
   return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
 #else
@@ -32,17 +33,19 @@ __device__ __forceinline__ f32x16 mma(float a, float b, const f32x16& c) {
 #endif
 }
 
+template <int D>
+union RowsF32Lds {
+  RowPlanLds plan;
+  float state[(kRowWaves - 1) * (D / 2 + 2) * 64];
+};
+
+// Work-group w of a launch over ragged chunks, or (kShared) over a shared prefix.
 template <int D, bool kShared>
-__global__ void __launch_bounds__(kWaves * 64, D == 64 ? 2 : 1) paged_rows_f32_kernel(PagedArgs a) {
+__device__ __forceinline__ void rows_f32(const PagedArgs& a, RowsF32Lds<D>& lds, int w) {
   constexpr int PS = D + kPagedPartPad;
   constexpr int H = D / 2;                // dimensions of a half-wave
   constexpr int DT = D / 32;
   constexpr int kRegs = DT * 16 + 2;      // a lane's state
-  __shared__ union {
-    RowPlanLds plan;
-    float state[(kWaves - 1) * kRegs * 64];
-  } s_mem;
-
   const int lane = threadIdx.x & 63;
   const int wave = uniform(threadIdx.x >> 6);
   const int lrow = lane & 31;
@@ -57,7 +60,7 @@ __global__ void __launch_bounds__(kWaves * 64, D == 64 ? 2 : 1) paged_rows_f32_k
 
     const bool narrow = it.rows <= 32;
     const int row_block = narrow ? 0 : wave & 1;
-    const int kg = narrow ? wave : wave >> 1, groups = narrow ? kWaves : kWaves / 2;   // of key tiles
+    const int kg = narrow ? wave : wave >> 1, groups = narrow ? kRowWaves : kRowWaves / 2;   // of key tiles
     const int my_row = row_block * 32 + lrow;
     const bool in_tile = my_row < it.rows;
     const int token = it.token + (my_row >> gs);
@@ -144,7 +147,7 @@ __global__ void __launch_bounds__(kWaves * 64, D == 64 ? 2 : 1) paged_rows_f32_k
 #pragma unroll
       for (int i = 0; i < H / 4; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sacc = mma(kf[i][e], qf[4 * i + e], sacc);
+        for (int e = 0; e < 4; ++e) sacc = mma32f(kf[i][e], qf[4 * i + e], sacc);
       sched_fence();
       if (u + groups < end) load_k(row_next);
       row = row_next;
@@ -181,14 +184,14 @@ __global__ void __launch_bounds__(kWaves * 64, D == 64 ? 2 : 1) paged_rows_f32_k
         const float p = fast_exp2(sacc[r] - m_run);
         l_run += p;
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) oacc[dt] = mma(vf[r][dt], p, oacc[dt]);
+        for (int dt = 0; dt < DT; ++dt) oacc[dt] = mma32f(vf[r][dt], p, oacc[dt]);
       }
     }
     l_run = sum_xor<32>(l_run);
 
     // The waves' states of the same rows sit in the same lanes.
     if (kg > 0) {
-      float* p = s_mem.state + (narrow ? kg - 1 : row_block) * kRegs * 64 + lane;
+      float* p = lds.state + (narrow ? kg - 1 : row_block) * kRegs * 64 + lane;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -200,7 +203,7 @@ __global__ void __launch_bounds__(kWaves * 64, D == 64 ? 2 : 1) paged_rows_f32_k
     if (kg > 0) return;
 #pragma unroll 1
     for (int v = 0; v < groups - 1; ++v) {
-      const float* p = s_mem.state + (narrow ? v : row_block) * kRegs * 64 + lane;
+      const float* p = lds.state + (narrow ? v : row_block) * kRegs * 64 + lane;
       const float m2 = p[(kRegs - 2) * 64];
       const float m_new = fmaxf(m_run, m2);
       const float f1 = fast_exp2(m_run - m_new), f2 = fast_exp2(m2 - m_new);
@@ -224,8 +227,8 @@ __global__ void __launch_bounds__(kWaves * 64, D == 64 ? 2 : 1) paged_rows_f32_k
         }
     };
     if (it.slot >= 0) {                   // by rows, or as the lanes hold them (see paged_prefill.hip)
-      float* const pp = a.rows_part + int64_t(it.slot) * kRows * (kShared ? PS : D + 2);
-      float* const st = kShared ? pp + my_row * PS + D : pp + kRows * D + my_row * 2;
+      float* const pp = a.rows_part + int64_t(it.slot) * kRowsF32 * (kShared ? PS : D + 2);
+      float* const st = kShared ? pp + my_row * PS + D : pp + kRowsF32 * D + my_row * 2;
       if (half == 0) {
         st[0] = m_run;
         st[1] = l_run;
@@ -236,26 +239,14 @@ __global__ void __launch_bounds__(kWaves * 64, D == 64 ? 2 : 1) paged_rows_f32_k
       store(static_cast<float*>(a.o) + (int64_t(token) * a.hq + head) * D + half * 4, 8, l_run > 0.0f ? 1.0f / l_run : 0.0f);
     }
   };
-  if constexpr (kShared) for_each_prefix_tile<kRows>(a, blockIdx.x, tile);
-  else for_each_row_tile<kRows>(a, s_mem.plan, tile);
-}
-
-template <int D, bool kShared>
-int launch_t(const PagedArgs& a, int64_t groups, void* stream) {
-  if (groups >= kMaxGrid) return kGridTooLarge;
-  PagedArgs copy = a;
-  void* args[] = {&copy};
-  return static_cast<int>(hipLaunchKernel(reinterpret_cast<const void*>(&paged_rows_f32_kernel<D, kShared>),
-                                          dim3(static_cast<unsigned>(groups)), dim3(kWaves * 64), args, 0,
-                                          static_cast<hipStream_t>(stream)));
+  if constexpr (kShared) {
+    const PagedItem it = uniform(prefix_item<kRowsF32>(a, w));
+    if (it.rows > 0) tile(it);
+  } else {
+    for_each_row_tile<kRowsF32>(a, w, lds.plan, tile);
+  }
 }
 
 }  // namespace
-
-int launch_paged_rows_f32(const PagedArgs& a, int head_dim, int64_t groups, void* stream) {
-  if (a.prefix_table != nullptr)
-    return head_dim == 128 ? launch_t<128, true>(a, groups, stream) : launch_t<64, true>(a, groups, stream);
-  return head_dim == 128 ? launch_t<128, false>(a, groups, stream) : launch_t<64, false>(a, groups, stream);
-}
 
 }  // namespace moa
