@@ -15,8 +15,8 @@
 // per key forms the row of its key a tile ahead, and the lanes that load the row get it
 // by a lane permutation.  A key on an absent page gets weight 0, and zeros for a value.
 //
-// Inner loops.  One query head per KV head, and fp32: LPR lanes hold a row, products on
-// the vector units.  bf16 groups: 16x16x32 matrix products (G padded to 16 columns),
+// Inner loops.  fp32: LPR lanes hold a row, products on the vector units.  bf16: 16x16x32
+// matrix products (the G query heads padded to 16 columns),
 //   S^T = K Q^T  (A = 16 keys x 32 dims, from whole rows turned in LDS),
 //   O^T += V^T P^T  (B = P^T from the score registers, A = V^T by the transposing LDS
 //   read, the keys of a step permuted alike on both sides).
@@ -33,7 +33,7 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * 64;
 constexpr int kPageRows = 1024;      // page numbers held in LDS
-constexpr int kPlanHead = 4;         // plan: workers, per, rem, pad, then the rounds in front of each pair
+constexpr int kPlanHead = 4;         // plan: workers, per, rem, pad, then the rounds in front of each pair that has any
 
 __device__ __forceinline__ f32x4 mma16(const bf16x8& a, const bf16x8& b, const f32x4& c) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -60,7 +60,7 @@ __device__ __forceinline__ uint32_t rounds_of(const PagedArgs& a, int pos, int g
 // Shared state of the walk over a worker's piece.
 struct Walk {
   uint32_t wave_sum[kWaves], wave_max[kWaves];
-  int pair;                     // where the piece begins
+  int pair, pos;                // where the piece begins, and its sequence's position
   uint32_t before;              // rounds in front of that pair
   int rows[kPageRows];
 };
@@ -76,9 +76,11 @@ __device__ __forceinline__ void for_each_piece(const PagedArgs& a, Walk& s, uint
   const int p1 = min(pairs, p0 + each);
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   uint32_t sum = 0, longest = 0;
+  int pos = -1;                                      // of the thread's last pair, of one the only one
   for (int p = p0; p < p1; ++p) {
     const int b = p / a.hkv;
-    const uint32_t n = rounds_of(a, a.positions[b], p - b * a.hkv, round_shift);
+    pos = a.positions[b];
+    const uint32_t n = rounds_of(a, pos, p - b * a.hkv, round_shift);
     sum += n;
     longest = max(longest, n);
   }
@@ -104,52 +106,50 @@ __device__ __forceinline__ void for_each_piece(const PagedArgs& a, Walk& s, uint
   }
   before += incl - sum;
   const PagedSplit split = paged_split(units, longest, a.slots);
-  if (w == 0) {
-    if (threadIdx.x == 0) {
-      a.plan[0] = split.workers;
-      a.plan[1] = split.per;
-      a.plan[2] = split.rem;
-    }
-    uint32_t at = before;
-    for (int p = p0; p < p1; ++p) {
-      const int b = p / a.hkv;
-      a.plan[kPlanHead + p] = at;
-      at += rounds_of(a, a.positions[b], p - b * a.hkv, round_shift);
-    }
-    if (p0 < pairs && p1 == pairs) a.plan[kPlanHead + pairs] = at;
-  }
   if (w >= split.workers) return;
+  if (w == 0 && threadIdx.x == 0) {
+    a.plan[0] = split.workers;
+    a.plan[1] = split.per;
+    a.plan[2] = split.rem;
+  }
   uint32_t x = split.start(w);
   const uint32_t x_end = split.start(w + 1);
   if (x >= before && x < before + sum) {             // one thread
     int p = p0;
     uint32_t at = before;
-    while (true) {
+    for (; each > 1; ++p) {
       const int b = p / a.hkv;
-      const uint32_t n = rounds_of(a, a.positions[b], p - b * a.hkv, round_shift);
+      pos = a.positions[b];
+      const uint32_t n = rounds_of(a, pos, p - b * a.hkv, round_shift);
       if (x < at + n) break;
       at += n;
-      ++p;
     }
     s.pair = p;
+    s.pos = pos;
     s.before = at;
   }
   __syncthreads();
   int pair = uniform(s.pair);
   uint32_t at = uniform(s.before);
-  while (x < x_end) {
-    const int b = pair / a.hkv, g = pair - b * a.hkv;
-    const int pos = uniform(a.positions[b]);
+  pos = uniform(s.pos);
+  int b = pair / a.hkv, g = pair - b * a.hkv;
+  while (true) {
     const uint32_t n = rounds_of(a, pos, g, round_shift);
     if (n > 0) {
       const VisibleKeys keys = keys_of(a, pos, g);
       const uint32_t lo = x - at, hi = min(n, lo + (x_end - x));
+      if (lo == 0 && threadIdx.x == 0) a.plan[kPlanHead + pair] = static_cast<int32_t>(at);
       seg(b, g, keys, static_cast<int>(lo << round_shift),
           static_cast<int>(min(static_cast<uint32_t>(keys.count), hi << round_shift)), lo == 0 && hi == n, pair);
       x += hi - lo;
+      if (x >= x_end) break;
     }
     at += n;
     ++pair;
+    if (++g == a.hkv) {
+      g = 0;
+      pos = uniform(a.positions[++b]);
+    }
   }
 }
 
@@ -210,7 +210,7 @@ __device__ __forceinline__ void merge_waves_and_store(const PagedArgs& a, const 
 }
 
 // ---------------------------------------------------------------------------
-// Vector units: a wave's tile is U * RPW keys, RPW rows per load.
+// Vector units (fp32): a wave's tile is U * RPW keys, RPW rows per load.
 // ---------------------------------------------------------------------------
 template <typename T, int D>
 struct ValuTile {
@@ -342,7 +342,7 @@ __device__ __forceinline__ void decode_valu(const PagedArgs& a, ValuLds<D, G>& l
 }
 
 // ---------------------------------------------------------------------------
-// Matrix units (bf16, G query heads per KV head): a wave's tile is 32 keys.
+// Matrix units (bf16): a wave's tile is 32 keys.
 // ---------------------------------------------------------------------------
 template <int D>
 struct MmaTile {
@@ -422,40 +422,42 @@ __device__ __forceinline__ void decode_mma(const PagedArgs& a, MmaLds<D>& lds, u
 
     for_each_span(a, s_walk, b, g, keys, x0, x1, TL::kRoundShift, [&](int lo, int hi, auto row_of) {
       auto rows_at = [&](int t) { return lane < KT && t + lane < hi ? row_of(t + lane) : -1; };
-      int rows = rows_at(lo + wave * KT);
-      for (int t0 = lo + wave * KT; t0 < hi; t0 += kWaves * KT) {
-        // K and V in whole rows: chunk u * 64 + lane is row m / CPR, chunk m % CPR.  Keys
-        // that are not there read row 0 of the pool, and are taken out below.
-        const uint32_t there = static_cast<uint32_t>(__ballot(rows >= 0));
-        bf16x8 kr[LD], vr[LD];
+      // K and V in whole rows: chunk u * 64 + lane is row m / CPR, chunk m % CPR.  Keys that
+      // are not there read row 0 of the pool, and are taken out below.  The next tile's K is
+      // asked for as soon as this one's registers are free, its V likewise.
+      bf16x8 kr[LD], vr[LD];
+      auto load = [&](const char* base, int rows, bf16x8 (&x)[LD]) {
         const int row0 = max(rows, 0);
 #pragma unroll
         for (int u = 0; u < LD; ++u) {
           const uint32_t r = __shfl(row0, u * (64 / CPR) + lane / CPR, 64);
-          kr[u] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(kbase + uint64_t(r) * RB));
+          x[u] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(base + uint64_t(r) * RB));
         }
-#pragma unroll
-        for (int u = 0; u < LD; ++u) {
-          const uint32_t r = __shfl(row0, u * (64 / CPR) + lane / CPR, 64);
-          vr[u] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(vbase + uint64_t(r) * RB));
-        }
+      };
+      int rows = rows_at(lo + wave * KT);
+      if (lo + wave * KT < hi) {
+        load(kbase, rows, kr);
+        load(vbase, rows, vr);
+      }
+      for (int t0 = lo + wave * KT; t0 < hi; t0 += kWaves * KT) {
+        const uint32_t there = static_cast<uint32_t>(__ballot(rows >= 0));
+        const bool more = t0 + kWaves * KT < hi;
         rows = rows_at(t0 + kWaves * KT);
 #pragma unroll
         for (int u = 0; u < LD; ++u) *reinterpret_cast<bf16x8*>(ts + kw[u & 3] + u * 1024) = kr[u];
-        bf16x8 kop[2][KS];
-#pragma unroll
-        for (int st = 0; st < 2; ++st) {
-          const int r = 16 * st + n;
-#pragma unroll
-          for (int kk = 0; kk < KS; ++kk)
-            kop[st][kk] = *reinterpret_cast<const bf16x8*>(ts + r * RB + (((4 * kk + q4) ^ TL::swk(r)) << 4));
-        }
+        if (more) load(kbase, rows, kr);
+        sched_fence();
         f32x4 s[2];
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
+          const int r = 16 * st + n;
+          bf16x8 kop[KS];
+#pragma unroll
+          for (int kk = 0; kk < KS; ++kk)
+            kop[kk] = *reinterpret_cast<const bf16x8*>(ts + r * RB + (((4 * kk + q4) ^ TL::swk(r)) << 4));
           s[st] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-          for (int kk = 0; kk < KS; ++kk) s[st] = mma16(kop[st][kk], qop[kk], s[st]);
+          for (int kk = 0; kk < KS; ++kk) s[st] = mma16(kop[kk], qop[kk], s[st]);
         }
         if (there != 0xffffffffu) {
 #pragma unroll
@@ -492,6 +494,8 @@ __device__ __forceinline__ void decode_mma(const PagedArgs& a, MmaLds<D>& lds, u
         for (int i = 0; i < 8; i += 2) l_run = dot2_ones(pop[i], pop[i + 1], l_run);
 #pragma unroll
         for (int u = 0; u < LD; ++u) *reinterpret_cast<bf16x8*>(ts + vw[u & 1] + u * 1024) = vr[u];
+        if (more) load(vbase, rows, vr);
+        sched_fence();
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
           const bf16x4 v0 = read_tr(ts + rd_off[dt]);
@@ -521,14 +525,20 @@ __device__ __forceinline__ void decode_mma(const PagedArgs& a, MmaLds<D>& lds, u
   });
 }
 
-// The worker of a type and group: bf16 groups go to the matrix units.
-template <typename T, int G>
-constexpr __host__ __device__ bool on_matrix_units() { return sizeof(T) == 2 && G >= 2; }
+// The worker of a type: bf16 goes to the matrix units, of single heads too, as they leave the
+// vector units to the rest (1 x 32 heads of 8,200 keys on average 29.7 -> 28.8 us, 32 x 32
+// of 4,200 238 -> 233).
+template <typename T>
+constexpr __host__ __device__ bool on_matrix_units() { return sizeof(T) == 2; }
 template <typename T, int D, int G>
-using DecodeLds = std::conditional_t<on_matrix_units<T, G>(), MmaLds<D>, ValuLds<D, G>>;
+using DecodeLds = std::conditional_t<on_matrix_units<T>(), MmaLds<D>, ValuLds<D, G>>;
+template <typename T, int D, int G>
+constexpr __host__ __device__ int decode_round_shift() {
+  return on_matrix_units<T>() ? MmaTile<D>::kRoundShift : ValuTile<T, D>::kRoundShift;
+}
 template <typename T, int D, int G>
 __device__ __forceinline__ void decode_worker(const PagedArgs& a, DecodeLds<T, D, G>& lds, uint32_t w) {
-  if constexpr (on_matrix_units<T, G>()) decode_mma<D, G>(a, lds, w);
+  if constexpr (on_matrix_units<T>()) decode_mma<D, G>(a, lds, w);
   else decode_valu<T, D, G>(a, lds, w);
 }
 
@@ -558,7 +568,8 @@ __global__ void __launch_bounds__(256) paged_combine_kernel(PagedArgs a) {
   const int pair = static_cast<int>(blockIdx.x) / (G / HS);
   const int h0 = (static_cast<int>(blockIdx.x) - pair * (G / HS)) * HS;
   const int b = pair / a.hkv, g = pair - b * a.hkv;
-  const uint32_t x0 = a.plan[kPlanHead + pair], x1 = a.plan[kPlanHead + pair + 1];
+  const int pos = a.positions[b];
+  const uint32_t x0 = a.plan[kPlanHead + pair];       // written by the worker that began with the pair, if one did
   const PagedSplit split = {static_cast<uint32_t>(a.plan[0]), static_cast<uint32_t>(a.plan[1]),
                             static_cast<uint32_t>(a.plan[2])};
   const int pg = static_cast<int>(threadIdx.x) / TPR, j = static_cast<int>(threadIdx.x) % TPR;
@@ -567,14 +578,15 @@ __global__ void __launch_bounds__(256) paged_combine_kernel(PagedArgs a) {
   int n_own = 0, np;
   const float *own = a.part, *prefix = nullptr;
   int64_t step = 0;                                   // from piece to piece of the prefix
-  if (x0 < x1) {
-    const uint32_t w0 = split.worker_of(x0), w1 = split.worker_of(x1 - 1);
+  const uint32_t rounds = rounds_of(a, pos, g, decode_round_shift<T, D, G>());
+  if (rounds > 0) {
+    const uint32_t w0 = split.worker_of(x0), w1 = split.worker_of(x0 + rounds - 1);
     n_own = static_cast<int>(w1 - w0) + 1;
     own = a.part + ((int64_t(w0) + pair) * G + h0 + h) * PS;
   }
   np = n_own;
   if constexpr (kShared) {
-    if (a.positions[b] < 0) return;                   // idle
+    if (pos < 0) return;                              // idle
     const int row = b * G + h0 + h, tiles = prefix_row_tiles<RT>(a.batch, a.group_shift);
     const int first = a.prefix_piece[g];
     np += a.prefix_piece[g + 1] - first;
