@@ -118,7 +118,7 @@ constexpr int kPagedPrefixItems = 256;
 MOA_PAGED_FN int paged_tile_rows(int dtype) { return dtype == MOA_BF16 ? 128 : 64; }
 
 // groups: no fewer than there are row tiles, nor than a.slots.
-int launch_paged_rows(const PagedArgs& a, int dtype, int head_dim, int64_t groups, void* stream);
+int launch_paged_rows(const PagedArgs& a, int dtype, int head_dim, int key_groups, int64_t groups, void* stream);
 int launch_paged_merge(const PagedArgs& a, int dtype, int head_dim, void* stream);
 int launch_paged_shared(const PagedArgs& a, int dtype, int head_dim, int group, void* stream);
 int launch_paged_decode(const PagedArgs& a, int dtype, int head_dim, int group, void* stream);

@@ -261,15 +261,27 @@ moa_status_t moa_paged_prefill(const moa_plan_t* plan, const moa_pages_t* pages,
   char* ws = static_cast<char*>(workspace);
   a.rows_part = static_cast<float*>(workspace);
   a.plan = reinterpret_cast<int32_t*>(ws + prefill_space(*plan).plan);
+  int64_t widest = 0;
+  for (int h = 0; h < d.num_kv_heads; ++h) {
+    a.window_in_order[h] = a.window[a.kv_order[h]];
+    widest = std::max(widest, int64_t(a.window[h]) << a.band_shift);
+  }
+  const int rows = paged_tile_rows(d.dtype);
+  const int64_t longest = pair_cost(n_tokens, pages->max_pages * pages->page_size - 1, static_cast<int>(widest >> a.band_shift),
+                                    a.band_shift, d.num_sink, a.group_shift, rows,
+                                    int64_t(pages->max_pages) * pages->page_size).longest();
+  const bool bf16 = d.dtype == MOA_BF16;
+  const bool whole = longest <= (bf16 ? kShortRowCost : kShortRowCostF32);   // nothing is cut: no merge
+  const int key_groups = bf16 && whole && tiles <= kKeyGroupTiles ? 2 : 1;
+  if (whole) a.plan = nullptr;
   a.slots = kPagedRowGroups;
   a.log_slots = kPagedLogRowGroups;
   a.least_cost = kLeastRowCost;
-  a.whole_cost = kWholeRowCost;
-  for (int h = 0; h < d.num_kv_heads; ++h) a.window_in_order[h] = a.window[a.kv_order[h]];
+  a.whole_cost = bf16 ? kWholeRowCost : kWholeRowCostF32;
   // a work-group per row tile, dealt to the dies in whole rounds, or per piece
-  const int64_t groups = std::max<int64_t>((tiles + 127) / 128 * 128, kPagedRowGroups);
-  int err = launch_paged_rows(a, d.dtype, d.head_dim, groups, hip_stream);
-  if (!err) err = launch_paged_merge(a, d.dtype, d.head_dim, hip_stream);
+  const int64_t groups = std::max<int64_t>((tiles + 127) / 128 * 128, whole ? 0 : kPagedRowGroups);
+  int err = launch_paged_rows(a, d.dtype, d.head_dim, key_groups, groups, hip_stream);
+  if (!err && !whole) err = launch_paged_merge(a, d.dtype, d.head_dim, hip_stream);
   return launched(who, err);
 }
 

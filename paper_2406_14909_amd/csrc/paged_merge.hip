@@ -36,7 +36,8 @@ __global__ void __launch_bounds__(kThreads) paged_merge_kernel(PagedArgs a) {
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int w = thread * PER + i;
-    const PagedSeg seg = reinterpret_cast<const PagedSeg*>(a.plan)[w];
+    PagedSeg seg = {0, 0, 0, 0};
+    if (w < a.slots) seg = reinterpret_cast<const PagedSeg*>(a.plan)[w];
     s_seg[w] = seg;
     sum += seg.rows <= 0 ? 0 : (seg.rows + 31) / 32 * (seg.pieces > kMany ? BLOCKS : BLOCKS / kWaves);
     n[i] = sum;

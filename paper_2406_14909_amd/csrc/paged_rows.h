@@ -62,8 +62,8 @@ struct RowPair {
   PairCost cost;
 };
 struct RowPlanLds {
-  int64_t cost[4], longest[4];
-  uint32_t tiles[4];
+  int64_t cost[8], longest[8];     // of each wave
+  uint32_t tiles[8];
   // where this work-group begins
   int index, tile;
   int64_t before;                // cost in front of the pair
@@ -88,11 +88,11 @@ __device__ __forceinline__ RowPair row_pair(const PagedArgs& a, int pair) {
   return p;
 }
 
-// Calls tile(item) for each row tile that work-group `block` has a part in (256 threads).
+// Calls tile(item) for each row tile that work-group `block` of WAVES waves has a part in.
 // Work-group uniform; `tile` ends with a barrier where LDS is used again.
-template <int ROWS, class Tile>
+template <int ROWS, int WAVES, class Tile>
 __device__ __forceinline__ void for_each_row_tile(const PagedArgs& a, int block, RowPlanLds& s, Tile&& tile) {
-  constexpr int kThreads = 256;
+  constexpr int kThreads = WAVES * 64;
   const int pairs = a.batch * a.hkv;
   const int each = (pairs + kThreads - 1) / kThreads;
   const int p0 = static_cast<int>(threadIdx.x) * each;
@@ -128,7 +128,7 @@ __device__ __forceinline__ void for_each_row_tile(const PagedArgs& a, int block,
   uint32_t all = 0, tiles_before = tiles_to - tiles;
   longest = 0;
 #pragma unroll
-  for (int v = 0; v < 4; ++v) {
+  for (int v = 0; v < WAVES; ++v) {
     before += v < wave ? s.cost[v] : 0;
     tiles_before += v < wave ? s.tiles[v] : 0;
     units += s.cost[v];
@@ -155,11 +155,10 @@ __device__ __forceinline__ void for_each_row_tile(const PagedArgs& a, int block,
     return it;
   };
 
-  // Whole row tiles: where the longest is not worth cutting, or short beside what each of the
-  // resident work-groups has to do.
+  // Whole row tiles, where the longest takes little more than an equal share of the work.
   PagedSeg* const segs = reinterpret_cast<PagedSeg*>(a.plan);
-  if (longest <= a.whole_cost || 2 * longest * a.slots <= units) {
-    if (block < a.slots && threadIdx.x == 0) segs[block].rows = 0;
+  if (a.plan == nullptr || (longest - a.whole_cost) * a.slots <= units) {
+    if (a.plan != nullptr && block < a.slots && threadIdx.x == 0) segs[block].rows = 0;
     // Dealt to the dies in units of 16 neighbours, one unit to each die in turn and back
     // again; few singly.  Of a pair the last first: theirs are the most keys.
     const uint32_t unit = all >= 16 * kNumXcd * 4 ? 16 : 1;

@@ -66,23 +66,29 @@ struct RowTiles {
   __device__ __forceinline__ static int swz_v(int r) { return CPR >= 16 ? 4 * (r & 3) : 4 * ((r >> 1) & 1); }
 };
 
-template <int D>
+// Of each key group K stages, then V stages; at first the plan.
+template <int D, int KG>
 struct RowsBf16Lds {
-  char tiles[(RowTiles<D>::KSTAGES + 2) * RowTiles<D>::TILE_BYTES];    // K stages, V stages; at first the plan
+  static constexpr int GROUP = (RowTiles<D>::KSTAGES + 2) * RowTiles<D>::TILE_BYTES;
+  char tiles[KG * GROUP];
 };
 
-// Work-group w of a launch over ragged chunks, or (kShared) over a shared prefix.
-template <int D, bool kShared>
-__device__ __forceinline__ void rows_bf16(const PagedArgs& a, RowsBf16Lds<D>& lds, int w) {
+// Work-group w of a launch over ragged chunks, or (kShared) over a shared prefix.  KG groups
+// of 4 waves share its rows: group kg takes key tiles kg, kg + KG, ... through LDS stages of
+// its own, and their states meet in LDS at the end.
+template <int D, bool kShared, int KG>
+__device__ __forceinline__ void rows_bf16(const PagedArgs& a, RowsBf16Lds<D, KG>& lds, int w) {
   using TL = RowTiles<D>;
   constexpr int KS = D / 16;              // steps over the head dimension
   constexpr int RB = TL::RB, CPR = TL::CPR, KST = TL::KSTAGES, DPW = TL::DPW;
   constexpr int PS = D + kPagedPartPad;
-  char* const sK = lds.tiles;
+  const int wave_id = uniform(threadIdx.x >> 6);
+  const int wave = KG == 1 ? wave_id : wave_id % 4;    // of the key group: rows
+  const int kg = KG == 1 ? 0 : wave_id / 4;
+  char* const sK = lds.tiles + kg * RowsBf16Lds<D, KG>::GROUP;
   char* const sV = sK + KST * TL::TILE_BYTES;
 
   const int lane = threadIdx.x & 63;
-  const int wave = uniform(threadIdx.x >> 6);
   const int lrow = lane & 31;
   const int half = lane >> 5;
   const int gs = a.group_shift;
@@ -235,22 +241,23 @@ __device__ __forceinline__ void rows_bf16(const PagedArgs& a, RowsBf16Lds<D>& ld
     float m_run = kNegBig, l_run = 0.0f;
     const float c2 = a.scale_log2;
 
-    // During tile t V(t+1) and then K(t+2) stream in, and the page numbers of t+3 are read.
+    // During a group's tile t its V(t+1) and then K(t+2) stream in, and t+3's page numbers are read.
     int jt = 0, j1 = 0, j2 = 0;
     Pages pt = {}, p1 = {}, p2 = {};
-    if (t0 < t1) {
-      jt = tile_j0(t0);
+    const int ts = t0 + kg;               // the group's first
+    if (ts < t1) {
+      jt = tile_j0(ts);
       pt = fetch(jt);
       tile_dma(a.vp, v_src, jt, pt, sV);
       tile_dma(a.kp, k_src, jt, pt, sK);
     }
-    if (t0 + 1 < t1) {
-      j1 = tile_j0(t0 + 1);
+    if (ts + KG < t1) {
+      j1 = tile_j0(ts + KG);
       p1 = fetch(j1);
       tile_dma(a.kp, k_src, j1, p1, sK + TL::TILE_BYTES);
     }
-    if (t0 + 2 < t1) {
-      j2 = tile_j0(t0 + 2);
+    if (ts + 2 * KG < t1) {
+      j2 = tile_j0(ts + 2 * KG);
       p2 = fetch(j2);
     }
     bf16x8 qf[KS];
@@ -266,28 +273,28 @@ __device__ __forceinline__ void rows_bf16(const PagedArgs& a, RowsBf16Lds<D>& ld
     // Wait for Q (and the first tiles) here, once: the compiler does not count the direct
     // loads and would otherwise wait for everything in flight inside the loop.
     __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
-    for (int t = t0; t < t1; ++t) {
+    for (int t = ts; t < t1 + kg; t += KG) {            // as many rounds for every group
       const int j0 = jt;
       const int ok = present(pt);
-      if (t + 1 < t1) __builtin_amdgcn_s_waitcnt(0x0F70 | DPW);   // K(t+1) may be in flight
+      if (t + KG < t1) __builtin_amdgcn_s_waitcnt(0x0F70 | DPW);  // the next K may be in flight
       else __builtin_amdgcn_s_waitcnt(0x0F70);
       __syncthreads();                      // K(t), V(t) are there for every wave; K(t-1), V(t-1) are free
       Pages p3 = {};
       int j3 = 0;
-      if (t + 3 < t1) {
-        j3 = tile_j0(t + 3);
+      if (t + 3 * KG < t1) {
+        j3 = tile_j0(t + 3 * KG);
         p3 = fetch(j3);
       }
 
       // Does any (row, key) pair of this wave fall inside the mask?
-      const bool any_vis = j0 <= w_last && (j0 < s || band_start(w_first) <= j0 + BN - 1);
+      const bool any_vis = t < t1 && j0 <= w_last && (j0 < s || band_start(w_first) <= j0 + BN - 1);
       // At head_dim 128 the next tiles' loads go between the S products; issued at once they
       // would queue for the address unit with the waves standing still.
       constexpr bool kSpread = D == 128;
-      const bool spread = kSpread && any_vis && t + 2 < t1 && group_full(j1 + 16 * wave) && group_full(j2 + 16 * wave);
+      const bool spread = kSpread && any_vis && t + 2 * KG < t1 && group_full(j1 + 16 * wave) && group_full(j2 + 16 * wave);
       if (!spread) {
-        if (t + 1 < t1) tile_dma(a.vp, v_src, j1, p1, sV + (v_now ^ TL::TILE_BYTES));
-        if (t + 2 < t1) tile_dma(a.kp, k_src, j2, p2, sK + k_next);
+        if (t + KG < t1) tile_dma(a.vp, v_src, j1, p1, sV + (v_now ^ TL::TILE_BYTES));
+        if (t + 2 * KG < t1) tile_dma(a.kp, k_src, j2, p2, sK + k_next);
       }
       if (any_vis) {
         const bool all_vis = wave_full && ok == 15 && j0 + BN - 1 <= w_first && j0 + BN <= key_end &&
@@ -412,6 +419,37 @@ __device__ __forceinline__ void rows_bf16(const PagedArgs& a, RowsBf16Lds<D>& ld
       v_now ^= TL::TILE_BYTES;
     }
     l_run = sum_xor<32>(l_run);
+    if constexpr (KG > 1) {
+      // The groups' states of the same rows sit in the same lanes of waves 4 apart.
+      constexpr int kRegs = D / 2 + 2;
+      static_assert((KG - 1) * 4 * kRegs * 256 <= sizeof(lds.tiles), "the states fit the tiles' LDS");
+      float* const st = reinterpret_cast<float*>(lds.tiles) + lane;
+      __syncthreads();                    // every tile has been read
+      if (kg > 0) {
+        float* p = st + ((kg - 1) * 4 + wave) * kRegs * 64;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) p[(dt * 16 + r) * 64] = oacc[dt][r];
+        p[(kRegs - 2) * 64] = m_run;
+        p[(kRegs - 1) * 64] = l_run;
+      }
+      __syncthreads();
+      if (kg > 0) return;
+#pragma unroll 1
+      for (int v = 0; v < KG - 1; ++v) {
+        const float* p = st + (v * 4 + wave) * kRegs * 64;
+        const float m2 = p[(kRegs - 2) * 64];
+        const float m_new = fmaxf(m_run, m2);
+        const float f1 = fast_exp2(m_run - m_new), f2 = fast_exp2(m2 - m_new);
+        m_run = m_new;
+        l_run = l_run * f1 + p[(kRegs - 1) * 64] * f2;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) oacc[dt][r] = oacc[dt][r] * f1 + p[(dt * 16 + r) * 64] * f2;
+      }
+    }
 
     if constexpr (kShared) {
       // By rows, for the merge of single tokens: turned in LDS, so that a store is whole rows.
@@ -480,7 +518,7 @@ __device__ __forceinline__ void rows_bf16(const PagedArgs& a, RowsBf16Lds<D>& ld
     const PagedItem it = uniform(prefix_item<kRowsBf16>(a, w));
     if (it.rows > 0) tile(it);
   } else {
-    for_each_row_tile<kRowsBf16>(a, w, *reinterpret_cast<RowPlanLds*>(lds.tiles), tile);
+    for_each_row_tile<kRowsBf16, 4 * KG>(a, w, *reinterpret_cast<RowPlanLds*>(lds.tiles), tile);
   }
 }
 

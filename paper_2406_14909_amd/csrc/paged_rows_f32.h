@@ -243,7 +243,7 @@ __device__ __forceinline__ void rows_f32(const PagedArgs& a, RowsF32Lds<D>& lds,
     const PagedItem it = uniform(prefix_item<kRowsF32>(a, w));
     if (it.rows > 0) tile(it);
   } else {
-    for_each_row_tile<kRowsF32>(a, w, lds.plan, tile);
+    for_each_row_tile<kRowsF32, kRowWaves>(a, w, lds.plan, tile);
   }
 }
 

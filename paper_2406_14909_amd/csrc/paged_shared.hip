@@ -16,7 +16,7 @@ namespace {
 
 template <typename T, int D, int G>
 __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 && D == 128 ? 1 : 2) paged_shared_kernel(PagedArgs a) {
-  using RowsLds = std::conditional_t<sizeof(T) == 2, RowsBf16Lds<D>, RowsF32Lds<D>>;
+  using RowsLds = std::conditional_t<sizeof(T) == 2, RowsBf16Lds<D, 1>, RowsF32Lds<D>>;
   __shared__ __attribute__((aligned(1024))) union {
     DecodeLds<T, D, G> decode;
     RowsLds rows;
@@ -29,7 +29,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 && D == 128 ? 1 : 2) 
   // Neighbours of the prefix's items share a die.
   const int w = is_prefix ? die * prefix + nth : nth * kNumXcd + die;
   if (is_prefix) {
-    if constexpr (sizeof(T) == 2) rows_bf16<D, true>(a, lds.rows, w);
+    if constexpr (sizeof(T) == 2) rows_bf16<D, true, 1>(a, lds.rows, w);
     else rows_f32<D, true>(a, lds.rows, w);
   } else {
     decode_worker<T, D, G>(a, lds.decode, w);

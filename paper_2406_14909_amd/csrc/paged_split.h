@@ -64,13 +64,22 @@ struct VisiblePages {
 // ---------------------------------------------------------------------------
 constexpr int kTileCost = 96;        // keys: what a row tile's start and end cost, about
 
-// A piece costs two partial results of 128 rows on their way out and back (67 KB each) and a
-// start, so it has kLeastRowCost at least, and a call whose row tiles all cost no more than
-// kWholeRowCost is not cut (8 heads x 4 query heads: 512 tokens, tiles of up to 608: whole
-// 22 us, cut 43; 1,500 tokens, up to 1,596: 63 and 61; 64 tokens behind 8,000: 36, 33, 38 and
-// 54 us in pieces of 128, 256, 512 and 1,024).
+// A piece costs a start and partial results of 128 rows on their way out and back (67 KB
+// each way), so it has kLeastRowCost at least (8 heads x 4 query heads, 64 tokens behind
+// 8,000: 36, 33, 38 and 54 us in pieces of 128, 256, 512 and 1,024), and a call is cut only
+// where the longest row tile costs kWholeRowCost more than an equal share of all (the same
+// heads, whole and cut: 3,000 tokens 93 and 130 us, 2,048 67 and 82, 1,500 63 and 61; fp32,
+// where a key takes longer, 16 heads of 64 x 1,501 tokens 90 and 72).
 constexpr int kLeastRowCost = 256;
-constexpr int kWholeRowCost = 1024;
+constexpr int kWholeRowCost = 1200;
+constexpr int kWholeRowCostF32 = 600;
+// Where the table has no room for longer row tiles than these, nothing is cut, and the merge
+// is left out (512 tokens 21.9 -> 18.7 us); and so few that each work-group can have a compute
+// unit for itself are walked by two groups of waves (1,500 tokens, 376 tiles, 61 -> 53 us; 504
+// tiles 45 -> 58).
+constexpr int kShortRowCost = 2200;
+constexpr int kShortRowCostF32 = 600;
+constexpr int kKeyGroupTiles = 400;
 
 // Cost of the row tiles of one (sequence, KV head) pair: tile i ends at key
 // min(first + step * (i + 1), most), step being its tokens.
