@@ -271,7 +271,8 @@ moa_status_t moa_paged_prefill(const moa_plan_t* plan, const moa_pages_t* pages,
                                     a.band_shift, d.num_sink, a.group_shift, rows,
                                     int64_t(pages->max_pages) * pages->page_size).longest();
   const bool bf16 = d.dtype == MOA_BF16;
-  const bool whole = longest <= (bf16 ? kShortRowCost : kShortRowCostF32);   // nothing is cut: no merge
+  const int64_t most = bf16 ? kShortRowCost : kShortRowCostF32;
+  const bool whole = longest <= (tiles >= kFewRowTiles ? most : most / 3);   // nothing is cut: no merge
   const int key_groups = bf16 && whole && tiles <= kKeyGroupTiles ? 2 : 1;
   if (whole) a.plan = nullptr;
   a.slots = kPagedRowGroups;

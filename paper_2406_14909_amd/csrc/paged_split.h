@@ -76,10 +76,12 @@ constexpr int kWholeRowCostF32 = 600;
 // Where the table has no room for longer row tiles than these, nothing is cut, and the merge
 // is left out (512 tokens 21.9 -> 18.7 us); and so few that each work-group can have a compute
 // unit for itself are walked by two groups of waves (1,500 tokens, 376 tiles, 61 -> 53 us; 504
-// tiles 45 -> 58).
+// tiles 45 -> 58).  Very few are worth cutting all the same, unless they are shorter still (30
+// tokens behind 1,900, 8 tiles: whole 47 us).
 constexpr int kShortRowCost = 2200;
 constexpr int kShortRowCostF32 = 600;
 constexpr int kKeyGroupTiles = 400;
+constexpr int kFewRowTiles = 128;
 
 // Cost of the row tiles of one (sequence, KV head) pair: tile i ends at key
 // min(first + step * (i + 1), most), step being its tokens.
