@@ -62,6 +62,7 @@ struct PagedArgs {
   int32_t* plan;                 // workspace: the split, from the first kernel of a call to the merge
   float* rows_part;              // workspace: partial results of row tiles (decode: of the shared prefix, or null)
   int32_t slots;                 // work-groups that the keys are cut for
+  int32_t most_tiles;            // rows: as many row tiles as there can be
   int32_t least_cost;            // rows: keys of a piece, at least
   int32_t whole_cost;            // rows: keys of a row tile that is not worth cutting
   int32_t log_slots;             // rows: log2(slots)

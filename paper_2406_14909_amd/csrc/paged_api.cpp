@@ -255,9 +255,6 @@ moa_status_t moa_paged_prefill(const moa_plan_t* plan, const moa_pages_t* pages,
     for (int h = 0; h < d.num_kv_heads; ++h) a.window[h] = (a.window[h] + MOA_BAND_BLOCK - 1) / MOA_BAND_BLOCK;
   }
   const int64_t tiles = row_tiles(*plan, n_tokens, batch) * d.num_kv_heads;
-  if (tiles >= kMaxGrid || tiles * (std::min<int64_t>(int64_t(pages->max_pages) * pages->page_size, kMaxPosition) + kTileCost) >=
-                               (int64_t(1) << 53))    // the cost of a call is cut in 64 bits
-    return launched(who, kGridTooLarge);
   char* ws = static_cast<char*>(workspace);
   a.rows_part = static_cast<float*>(workspace);
   a.plan = reinterpret_cast<int32_t*>(ws + prefill_space(*plan).plan);
@@ -266,17 +263,22 @@ moa_status_t moa_paged_prefill(const moa_plan_t* plan, const moa_pages_t* pages,
     a.window_in_order[h] = a.window[a.kv_order[h]];
     widest = std::max(widest, int64_t(a.window[h]) << a.band_shift);
   }
+  const bool bf16 = d.dtype == MOA_BF16;
   const int rows = paged_tile_rows(d.dtype);
   const int64_t longest = pair_cost(n_tokens, pages->max_pages * pages->page_size - 1, static_cast<int>(widest >> a.band_shift),
                                     a.band_shift, d.num_sink, a.group_shift, rows,
                                     int64_t(pages->max_pages) * pages->page_size).longest();
-  const bool bf16 = d.dtype == MOA_BF16;
+  // The cost of a call is added up in 64 bits, whatever seq_start holds, and cut in 53.
+  const double one = double(n_tokens) * plan->group / rows + 1;
+  if (tiles >= kMaxGrid || double(tiles) * longest >= 9.0e15 || one * batch * d.num_kv_heads * longest >= 4.0e18)
+    return launched(who, kGridTooLarge);
   const int64_t most = bf16 ? kShortRowCost : kShortRowCostF32;
   const bool whole = longest <= (tiles >= kFewRowTiles ? most : most / 3);   // nothing is cut: no merge
   const int key_groups = bf16 && whole && tiles <= kKeyGroupTiles ? 2 : 1;
   if (whole) a.plan = nullptr;
   a.slots = kPagedRowGroups;
   a.log_slots = kPagedLogRowGroups;
+  a.most_tiles = static_cast<int32_t>(tiles);
   a.least_cost = kLeastRowCost;
   a.whole_cost = bf16 ? kWholeRowCost : kWholeRowCostF32;
   // a work-group per row tile, dealt to the dies in whole rounds, or per piece

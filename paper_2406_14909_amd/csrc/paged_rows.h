@@ -63,7 +63,7 @@ struct RowPair {
 };
 struct RowPlanLds {
   int64_t cost[8], longest[8];     // of each wave
-  uint32_t tiles[8];
+  int64_t tiles[8];
   // where this work-group begins
   int index, tile;
   int64_t before;                // cost in front of the pair
@@ -98,8 +98,7 @@ __device__ __forceinline__ void for_each_row_tile(const PagedArgs& a, int block,
   const int p0 = static_cast<int>(threadIdx.x) * each;
   const int p1 = min(pairs, p0 + each);
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-  int64_t cost = 0, longest = 0;
-  uint32_t tiles = 0;
+  int64_t cost = 0, longest = 0, tiles = 0;
   RowPair mine = {};                                 // the thread's last pair, of one the only one
   for (int p = p0; p < p1; ++p) {
     mine = row_pair<ROWS>(a, p);
@@ -108,12 +107,11 @@ __device__ __forceinline__ void for_each_row_tile(const PagedArgs& a, int block,
     longest = max(longest, c.longest());
     tiles += c.tiles;
   }
-  int64_t cost_to = cost;
-  uint32_t tiles_to = tiles;
+  int64_t cost_to = cost, tiles_to = tiles;
 #pragma unroll
   for (int off = 1; off < 64; off *= 2) {
     const int64_t c = __shfl_up(cost_to, off, 64);
-    const uint32_t t = __shfl_up(tiles_to, off, 64);
+    const int64_t t = __shfl_up(tiles_to, off, 64);
     cost_to += lane >= off ? c : 0;
     tiles_to += lane >= off ? t : 0;
     longest = max(longest, static_cast<int64_t>(__shfl_xor(longest, off, 64)));
@@ -124,8 +122,7 @@ __device__ __forceinline__ void for_each_row_tile(const PagedArgs& a, int block,
     s.tiles[wave] = tiles_to;
   }
   __syncthreads();
-  int64_t units = 0, before = cost_to - cost;
-  uint32_t all = 0, tiles_before = tiles_to - tiles;
+  int64_t units = 0, before = cost_to - cost, all = 0, tiles_before = tiles_to - tiles;
   longest = 0;
 #pragma unroll
   for (int v = 0; v < WAVES; ++v) {
@@ -137,7 +134,7 @@ __device__ __forceinline__ void for_each_row_tile(const PagedArgs& a, int block,
   }
   units = uniform64(units);
   longest = uniform64(longest);
-  all = uniform(all);
+  all = uniform64(all);
 
   // A row tile of a pair, whole or in part.
   auto item_of = [&](const RowPair& p, int i, int64_t num0, int64_t num1, int64_t den, int slot) {
@@ -155,6 +152,13 @@ __device__ __forceinline__ void for_each_row_tile(const PagedArgs& a, int block,
     return it;
   };
 
+  // More row tiles than n_tokens rows can have: seq_start is no packing of them, and nothing
+  // is done (all sums below rest on there being no more).
+  if (all > a.most_tiles) {
+    if (a.plan != nullptr && block < a.slots && threadIdx.x == 0) reinterpret_cast<PagedSeg*>(a.plan)[block].rows = 0;
+    return;
+  }
+
   // Whole row tiles, where the longest takes little more than an equal share of the work.
   PagedSeg* const segs = reinterpret_cast<PagedSeg*>(a.plan);
   if (a.plan == nullptr || (longest - a.whole_cost) * a.slots <= units) {
@@ -167,7 +171,7 @@ __device__ __forceinline__ void for_each_row_tile(const PagedArgs& a, int block,
     const uint32_t n = (round * kNumXcd + (round & 1 ? kNumXcd - 1 - die : die)) * unit + local % unit;
     if (n >= all) return;
     if (n >= tiles_before && n < tiles_before + tiles) {     // one thread
-      uint32_t at = tiles_before;
+      int64_t at = tiles_before;
       for (int p = p0; each > 1; ++p) {
         mine = row_pair<ROWS>(a, p);
         if (n < at + mine.cost.tiles) break;
