@@ -76,6 +76,7 @@ __device__ __forceinline__ void rows_f32(const PagedArgs& a, RowsF32Lds<D>& lds,
     }
     p_first = uniform(p_first);
     p_last = uniform(p_last);
+    const bool full = __ballot(my_pos >= 0) == ~0ull;
 
     // Keys that some row sees: [0, sinks) and [band_lo, key_end); 64-key tiles of this piece.
     const int cap = a.max_pages << a.page_shift;
@@ -95,17 +96,19 @@ __device__ __forceinline__ void rows_f32(const PagedArgs& a, RowsF32Lds<D>& lds,
       const int t = t0 + (u >> 1);
       return (t < ta ? t : tb + (t - ta)) * 64 + 32 * (u & 1);
     };
-    auto row_of = [&](int j0) {
+    auto page_of = [&](int j0) {          // as the table has it
       const int j = j0 + lrow;
-      if (j >= key_end || (j >= sinks && j < band_lo)) return -1;
-      const int r = page_row(table[j >> a.page_shift], a.num_pages, a.page_shift);
-      return r < 0 ? -1 : r + (j & ((1 << a.page_shift) - 1));
+      return j >= key_end || (j >= sinks && j < band_lo) ? -1 : table[j >> a.page_shift];
+    };
+    auto row_of = [&](int j0, int page) {
+      const int r = page_row(page, a.num_pages, a.page_shift);
+      return r < 0 ? -1 : r + ((j0 + lrow) & ((1 << a.page_shift) - 1));
     };
 
     const int end = 2 * (t1 - t0);
     int u = kg;
-    auto row_at = [&](int v) { return v < end ? row_of(tile_j0(v)) : -1; };
-    int row = row_at(u);
+    auto page_at = [&](int v) { return v < end ? page_of(tile_j0(v)) : -1; };
+    int row = row_of(tile_j0(u), page_at(u));
     // K of a tile is asked for behind the scores of the one before, V in front of its own
     // scores: each has a product's time to arrive, in one set of registers.
     f32x4 kf[H / 4];
@@ -115,7 +118,7 @@ __device__ __forceinline__ void rows_f32(const PagedArgs& a, RowsF32Lds<D>& lds,
       for (int i = 0; i < H / 4; ++i) kf[i] = *reinterpret_cast<const f32x4*>(p + 8 * i);
     };
     if (u < end) load_k(row);
-    int row_next = row_at(u + groups);
+    int row_next = row_of(tile_j0(u + groups), page_at(u + groups));
     float qf[H];
 #pragma unroll
     for (int i = 0; i < H; i += 4) {
@@ -134,6 +137,9 @@ __device__ __forceinline__ void rows_f32(const PagedArgs& a, RowsF32Lds<D>& lds,
     for (; u < end; u += groups) {
       const int j0 = tile_j0(u);
       const uint32_t there = static_cast<uint32_t>(__ballot(row >= 0));
+      // Asked for in front of V and used behind it: a wait for it is none for K.
+      const int page_after = page_at(u + 2 * groups);
+      sched_fence();
       float vf[16][DT];
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
@@ -150,8 +156,6 @@ __device__ __forceinline__ void rows_f32(const PagedArgs& a, RowsF32Lds<D>& lds,
         for (int e = 0; e < 4; ++e) sacc = mma32f(kf[i][e], qf[4 * i + e], sacc);
       sched_fence();
       if (u + groups < end) load_k(row_next);
-      row = row_next;
-      row_next = row_at(u + 2 * groups);
       sched_fence();
       if (there != 0xffffffffu) {
 #pragma unroll
@@ -161,16 +165,22 @@ __device__ __forceinline__ void rows_f32(const PagedArgs& a, RowsF32Lds<D>& lds,
             vf[r][dt] = there >> ((r >> 2) * 8 + half * 4 + (r & 3)) & 1 ? vf[r][dt] : 0.0f;
       }
 
-      const int jl = j0 + half * 4;                           // key of register 0 of this lane
-      const int hi = min(my_pos, key_end - 1) - jl, band = band_start(my_pos) - jl, sink = s - jl;
+      const bool all_vis = full && there == 0xffffffffu && j0 + 31 <= p_first && j0 + 32 <= key_end &&
+                           (j0 + 32 <= s || band_start(p_last) <= j0);
+      if (!all_vis) {
+        const int jl = j0 + half * 4;                       // key of register 0 of this lane
+        const int hi = min(my_pos, key_end - 1) - jl, band = band_start(my_pos) - jl, sink = s - jl;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int dj = (r >> 2) * 8 + (r & 3);
+          const bool vis = (dj <= hi) & ((dj < sink) | (dj >= band)) & ((there >> (dj + half * 4) & 1) != 0);
+          sacc[r] = vis ? sacc[r] : -INFINITY;
+        }
+      }
       float tmax = -INFINITY;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int dj = (r >> 2) * 8 + (r & 3);
-        const bool vis = (dj <= hi) & ((dj < sink) | (dj >= band)) & ((there >> (dj + half * 4) & 1) != 0);
-        sacc[r] = vis ? sacc[r] * c2 : -INFINITY;
-        tmax = fmaxf(tmax, sacc[r]);
-      }
+      for (int r = 0; r < 16; ++r) tmax = fmaxf(tmax, sacc[r]);
+      tmax *= c2;
       if (__any(tmax > m_run + kRescaleSlack)) {
         const float m_new = fmaxf(m_run, max_xor<32>(tmax));
         const float alpha = fast_exp2(m_run - m_new);
@@ -181,11 +191,13 @@ __device__ __forceinline__ void rows_f32(const PagedArgs& a, RowsF32Lds<D>& lds,
       }
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const float p = fast_exp2(sacc[r] - m_run);
+        const float p = fast_exp2(__builtin_fmaf(sacc[r], c2, -m_run));
         l_run += p;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) oacc[dt] = mma32f(vf[r][dt], p, oacc[dt]);
       }
+      row = row_next;
+      row_next = row_of(tile_j0(u + 2 * groups), page_after);
     }
     l_run = sum_xor<32>(l_run);
 
