@@ -305,7 +305,8 @@ moa_status_t moa_rule_loss(const float* ebar, int32_t num_heads, int64_t n, int3
  * token-exact in the two decode calls and, with MOA_BLOCK_BAND, in blocks in
  * moa_paged_prefill, as in moa_prefill.  A query that sees no key (all its pages
  * are absent) gets zeros.  What lies in rows that no query of the call sees is
- * not looked at; a value row that some query sees has to be finite.
+ * not looked at; a key or value that is not finite reaches the queries that see
+ * its position, and no other.
  * ----------------------------------------------------------------------- */
 typedef struct {
   void* k_pages;             /* device [num_pages, page_size, head_dim], the plan's type, 16-byte aligned */

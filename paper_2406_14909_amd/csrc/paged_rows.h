@@ -19,6 +19,7 @@
 
 namespace moa {
 
+__device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
 
 constexpr float kRescaleSlack = 8.0f;   // log2 headroom before a running maximum is raised
 

@@ -236,30 +236,8 @@ __device__ __forceinline__ void rows_bf16(const PagedArgs& a, RowsBf16Lds<D, KG>
     }
 
     f32x16 oacc[D / 32];
-#pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt) oacc[dt] = f32x16{};
-    float m_run = kNegBig, l_run = 0.0f;
+    float m_run, l_run;
     const float c2 = a.scale_log2;
-
-    // During a group's tile t its V(t+1) and then K(t+2) stream in, and t+3's page numbers are read.
-    int jt = 0, j1 = 0, j2 = 0;
-    Pages pt = {}, p1 = {}, p2 = {};
-    const int ts = t0 + kg;               // the group's first
-    if (ts < t1) {
-      jt = tile_j0(ts);
-      pt = fetch(jt);
-      tile_dma(a.vp, v_src, jt, pt, sV);
-      tile_dma(a.kp, k_src, jt, pt, sK);
-    }
-    if (ts + KG < t1) {
-      j1 = tile_j0(ts + KG);
-      p1 = fetch(j1);
-      tile_dma(a.kp, k_src, j1, p1, sK + TL::TILE_BYTES);
-    }
-    if (ts + 2 * KG < t1) {
-      j2 = tile_j0(ts + 2 * KG);
-      p2 = fetch(j2);
-    }
     bf16x8 qf[KS];
     if (active) {
       const bf16* qrow = static_cast<const bf16*>(a.q) + (int64_t(token) * a.hq + head) * D + 8 * half;
@@ -269,154 +247,244 @@ __device__ __forceinline__ void rows_bf16(const PagedArgs& a, RowsBf16Lds<D, KG>
 #pragma unroll
       for (int kk = 0; kk < KS; ++kk) qf[kk] = bf16x8{};
     }
-    int k_now = 0, k_next = (KST - 1) * TL::TILE_BYTES, v_now = 0;      // byte offsets of stages
-    // Wait for Q (and the first tiles) here, once: the compiler does not count the direct
-    // loads and would otherwise wait for everything in flight inside the loop.
-    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
-    for (int t = ts; t < t1 + kg; t += KG) {            // as many rounds for every group
-      const int j0 = jt;
-      const int ok = present(pt);
-      if (t + KG < t1) __builtin_amdgcn_s_waitcnt(0x0F70 | DPW);  // the next K may be in flight
-      else __builtin_amdgcn_s_waitcnt(0x0F70);
-      __syncthreads();                      // K(t), V(t) are there for every wave; K(t-1), V(t-1) are free
-      Pages p3 = {};
-      int j3 = 0;
-      if (t + 3 * KG < t1) {
-        j3 = tile_j0(t + 3 * KG);
-        p3 = fetch(j3);
-      }
-
-      // Does any (row, key) pair of this wave fall inside the mask?
-      const bool any_vis = t < t1 && j0 <= w_last && (j0 < s || band_start(w_first) <= j0 + BN - 1);
-      // At head_dim 128 the next tiles' loads go between the S products; issued at once they
-      // would queue for the address unit with the waves standing still.
-      constexpr bool kSpread = D == 128;
-      const bool spread = kSpread && any_vis && t + 2 * KG < t1 && group_full(j1 + 16 * wave) && group_full(j2 + 16 * wave);
-      if (!spread) {
-        if (t + KG < t1) tile_dma(a.vp, v_src, j1, p1, sV + (v_now ^ TL::TILE_BYTES));
-        if (t + 2 * KG < t1) tile_dma(a.kp, k_src, j2, p2, sK + k_next);
-      }
-      if (any_vis) {
-        const bool all_vis = wave_full && ok == 15 && j0 + BN - 1 <= w_first && j0 + BN <= key_end &&
-                             (j0 + BN <= s || band_start(w_last) <= j0);
-        const char* kb = sK + k_now;
-        auto kfrag = [&](int kk, int sub) {
-          return *reinterpret_cast<const bf16x8*>(kb + sub * 32 * RB + k_off[kk]);
-        };
-        f32x16 sacc[2] = {f32x16{}, f32x16{}};
-        bf16x8 kf[3][2];                    // read two steps ahead; the fence keeps that order
+    for (bool careful = false;; careful = true) {
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-          kf[kk][0] = kfrag(kk, 0);
-          kf[kk][1] = kfrag(kk, 1);
-        }
-        auto products = [&](auto with_loads) {
-          i32x4 rv = {}, rk = {};
-          if constexpr (decltype(with_loads)::value) {
-            rv = group_desc(a.vp, mine(p1), j1 + 16 * wave);
-            rk = group_desc(a.kp, mine(p2), j2 + 16 * wave);
+      for (int dt = 0; dt < D / 32; ++dt) oacc[dt] = f32x16{};
+      m_run = kNegBig;
+      l_run = 0.0f;
+      // During a group's tile t its V(t+1) and then K(t+2) stream in, and t+3's page numbers are read.
+      int jt = 0, j1 = 0, j2 = 0;
+      Pages pt = {}, p1 = {}, p2 = {};
+      const int ts = t0 + kg;               // the group's first
+      if (ts < t1) {
+        jt = tile_j0(ts);
+        pt = fetch(jt);
+        tile_dma(a.vp, v_src, jt, pt, sV);
+        tile_dma(a.kp, k_src, jt, pt, sK);
+      }
+      if (ts + KG < t1) {
+        j1 = tile_j0(ts + KG);
+        p1 = fetch(j1);
+        tile_dma(a.kp, k_src, j1, p1, sK + TL::TILE_BYTES);
+      }
+      if (ts + 2 * KG < t1) {
+        j2 = tile_j0(ts + 2 * KG);
+        p2 = fetch(j2);
+      }
+      int k_now = 0, k_next = (KST - 1) * TL::TILE_BYTES, v_now = 0;      // byte offsets of stages
+      // Wait for Q (and the first tiles) here, once: the compiler does not count the direct
+      // loads and would otherwise wait for everything in flight inside the loop.
+      __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
+      for (int t = ts; t < t1 + kg; t += KG) {            // as many rounds for every group
+        const int j0 = jt;
+        const int ok = present(pt);
+        if (t + KG < t1) __builtin_amdgcn_s_waitcnt(0x0F70 | DPW);  // the next K may be in flight
+        else __builtin_amdgcn_s_waitcnt(0x0F70);
+        if (careful && t < t1) {                // this wave's values of the tile: 0 in place of what is not finite
+#pragma unroll 1
+          for (int i = 0; i < DPW; ++i) {
+            bf16x8* const at = reinterpret_cast<bf16x8*>(sV + v_now + (wave * DPW + i) * 1024 + lane * 16);
+            bf16x8 v = *at;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = finite(static_cast<float>(v[e])) ? v[e] : static_cast<bf16>(0.0f);
+            *at = v;
           }
+        }
+        __syncthreads();                      // K(t), V(t) are there for every wave; K(t-1), V(t-1) are free
+        Pages p3 = {};
+        int j3 = 0;
+        if (t + 3 * KG < t1) {
+          j3 = tile_j0(t + 3 * KG);
+          p3 = fetch(j3);
+        }
+
+        // Does any (row, key) pair of this wave fall inside the mask?
+        const bool any_vis = t < t1 && j0 <= w_last && (j0 < s || band_start(w_first) <= j0 + BN - 1);
+        // At head_dim 128 the next tiles' loads go between the S products; issued at once they
+        // would queue for the address unit with the waves standing still.
+        constexpr bool kSpread = D == 128;
+        const bool spread = kSpread && any_vis && t + 2 * KG < t1 && group_full(j1 + 16 * wave) && group_full(j2 + 16 * wave);
+        if (!spread) {
+          if (t + KG < t1) tile_dma(a.vp, v_src, j1, p1, sV + (v_now ^ TL::TILE_BYTES));
+          if (t + 2 * KG < t1) tile_dma(a.kp, k_src, j2, p2, sK + k_next);
+        }
+        if (any_vis) {
+          const bool all_vis = wave_full && ok == 15 && j0 + BN - 1 <= w_first && j0 + BN <= key_end &&
+                               (j0 + BN <= s || band_start(w_last) <= j0);
+          const char* kb = sK + k_now;
+          auto kfrag = [&](int kk, int sub) {
+            return *reinterpret_cast<const bf16x8*>(kb + sub * 32 * RB + k_off[kk]);
+          };
+          f32x16 sacc[2] = {f32x16{}, f32x16{}};
+          bf16x8 kf[3][2];                    // read two steps ahead; the fence keeps that order
 #pragma unroll
-          for (int kk = 0; kk < KS; ++kk) {
-            if (kk + 2 < KS) {
-              kf[(kk + 2) % 3][0] = kfrag(kk + 2, 0);
-              kf[(kk + 2) % 3][1] = kfrag(kk + 2, 1);
-            }
-            sacc[0] = mma32(kf[kk % 3][0], qf[kk], sacc[0]);
-            sacc[1] = mma32(kf[kk % 3][1], qf[kk], sacc[1]);
+          for (int kk = 0; kk < 2; ++kk) {
+            kf[kk][0] = kfrag(kk, 0);
+            kf[kk][1] = kfrag(kk, 1);
+          }
+          auto products = [&](auto with_loads) {
+            i32x4 rv = {}, rk = {};
             if constexpr (decltype(with_loads)::value) {
-              constexpr int kPerStep = 2 * DPW / KS;     // V(t+1) first: only K may be in flight at the next tile
+              rv = group_desc(a.vp, mine(p1), j1 + 16 * wave);
+              rk = group_desc(a.kp, mine(p2), j2 + 16 * wave);
+            }
 #pragma unroll
-              for (int e = 0; e < kPerStep; ++e) {
-                const int m = kk * kPerStep + e;
-                if (m < DPW) dma16_async(rv, v_src[m % DPW], sV + (v_now ^ TL::TILE_BYTES) + (wave * DPW + m) * 1024);
-                else dma16_async(rk, k_src[m % DPW], sK + k_next + (wave * DPW + m - DPW) * 1024);
+            for (int kk = 0; kk < KS; ++kk) {
+              if (kk + 2 < KS) {
+                kf[(kk + 2) % 3][0] = kfrag(kk + 2, 0);
+                kf[(kk + 2) % 3][1] = kfrag(kk + 2, 1);
+              }
+              sacc[0] = mma32(kf[kk % 3][0], qf[kk], sacc[0]);
+              sacc[1] = mma32(kf[kk % 3][1], qf[kk], sacc[1]);
+              if constexpr (decltype(with_loads)::value) {
+                constexpr int kPerStep = 2 * DPW / KS;     // V(t+1) first: only K may be in flight at the next tile
+#pragma unroll
+                for (int e = 0; e < kPerStep; ++e) {
+                  const int m = kk * kPerStep + e;
+                  if (m < DPW) dma16_async(rv, v_src[m % DPW], sV + (v_now ^ TL::TILE_BYTES) + (wave * DPW + m) * 1024);
+                  else dma16_async(rk, k_src[m % DPW], sK + k_next + (wave * DPW + m - DPW) * 1024);
+                }
+              }
+              sched_fence();
+            }
+          };
+          if constexpr (kSpread) {
+            if (spread) products(std::true_type{});
+            else products(std::false_type{});
+          } else {
+            products(std::false_type{});
+          }
+
+          const char* vb = sV + v_now;
+          auto vfrag = [&](int step, int dt) {
+            const int kb0 = (step >> 1) * 32 + 16 * (step & 1);
+            const bf16x4 lo4 = read_tr(vb + kb0 * RB + v_off[dt]);
+            const bf16x4 hi4 = read_tr(vb + (kb0 + 8) * RB + v_off[dt]);
+            return __builtin_shufflevector(lo4, hi4, 0, 1, 2, 3, 4, 5, 6, 7);
+          };
+          bf16x8 vf[2][D / 32];
+#pragma unroll
+          for (int dt = 0; dt < D / 32; ++dt) vf[0][dt] = vfrag(0, dt);
+          sched_fence();
+
+          if (!all_vis) {
+            const int jl = j0 + half * 4;                       // key of register 0 of this lane
+            const int hi = min(my_pos, key_end - 1) - jl;       // key offset <= hi (none for an idle row)
+            const int band = band_start(my_pos) - jl;           // >= band
+            const int sink = s - jl;                            // or < sink
+#pragma unroll
+            for (int sub = 0; sub < 2; ++sub) {
+#pragma unroll
+              for (int r = 0; r < 16; ++r) {
+                const int dj = sub * 32 + (r >> 2) * 8 + (r & 3);
+                const bool vis = (dj <= hi) & ((dj < sink) | (dj >= band)) & ((ok >> (sub * 2 + (r >> 3)) & 1) != 0);
+                sacc[sub][r] = vis ? sacc[sub][r] : -INFINITY;
               }
             }
-            sched_fence();
           }
-        };
-        if constexpr (kSpread) {
-          if (spread) products(std::true_type{});
-          else products(std::false_type{});
-        } else {
-          products(std::false_type{});
-        }
-
-        const char* vb = sV + v_now;
-        auto vfrag = [&](int step, int dt) {
-          const int kb0 = (step >> 1) * 32 + 16 * (step & 1);
-          const bf16x4 lo4 = read_tr(vb + kb0 * RB + v_off[dt]);
-          const bf16x4 hi4 = read_tr(vb + (kb0 + 8) * RB + v_off[dt]);
-          return __builtin_shufflevector(lo4, hi4, 0, 1, 2, 3, 4, 5, 6, 7);
-        };
-        bf16x8 vf[2][D / 32];
+          float tmax = -INFINITY;
 #pragma unroll
-        for (int dt = 0; dt < D / 32; ++dt) vf[0][dt] = vfrag(0, dt);
-        sched_fence();
-
-        if (!all_vis) {
-          const int jl = j0 + half * 4;                       // key of register 0 of this lane
-          const int hi = min(my_pos, key_end - 1) - jl;       // key offset <= hi (none for an idle row)
-          const int band = band_start(my_pos) - jl;           // >= band
-          const int sink = s - jl;                            // or < sink
+          for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) tmax = fmaxf(tmax, sacc[sub][r]);
+          tmax *= c2;
+          if (__any(tmax > m_run + kRescaleSlack)) {
+            const float m_new = fmaxf(m_run, max_xor<32>(tmax));
+            const float alpha = fast_exp2(m_run - m_new);
+            m_run = m_new;
+            l_run *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < D / 32; ++dt) oacc[dt] *= alpha;
+          }
+          bf16x8 pf[2][2];
+          float psum = 0.0f;
 #pragma unroll
           for (int sub = 0; sub < 2; ++sub) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const int dj = sub * 32 + (r >> 2) * 8 + (r & 3);
-              const bool vis = (dj <= hi) & ((dj < sink) | (dj >= band)) & ((ok >> (sub * 2 + (r >> 3)) & 1) != 0);
-              sacc[sub][r] = vis ? sacc[sub][r] : -INFINITY;
+            for (int c = 0; c < 2; ++c) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                pf[sub][c][e] = static_cast<bf16>(fast_exp2(__builtin_fmaf(sacc[sub][8 * c + e], c2, -m_run)));
+#pragma unroll
+              for (int e = 0; e < 8; e += 2) psum = dot2_ones(pf[sub][c][e], pf[sub][c][e + 1], psum);
+            }
+          }
+          l_run += psum;
+#pragma unroll
+          for (int step = 0; step < 4; ++step) {
+            if (step + 1 < 4) {
+#pragma unroll
+              for (int dt = 0; dt < D / 32; ++dt) vf[(step + 1) & 1][dt] = vfrag(step + 1, dt);
+            }
+#pragma unroll
+            for (int dt = 0; dt < D / 32; ++dt) oacc[dt] = mma32(vf[step & 1][dt], pf[step >> 1][step & 1], oacc[dt]);
+          }
+        }
+        jt = j1;
+        j1 = j2;
+        j2 = j3;
+        pt = p1;
+        p1 = p2;
+        p2 = p3;
+        k_now = k_now == (KST - 1) * TL::TILE_BYTES ? 0 : k_now + TL::TILE_BYTES;
+        k_next = k_next == (KST - 1) * TL::TILE_BYTES ? 0 : k_next + TL::TILE_BYTES;
+        v_now ^= TL::TILE_BYTES;
+      }
+      if (careful) {
+        // What is not finite goes to the rows that see its key.  16 keys, in one page, are
+        // looked through at once.
+#pragma unroll 1
+        for (int i = 0; i < (t1 - ts + KG - 1) / KG * 4; ++i) {
+          const int kb = tile_j0(ts + (i >> 2) * KG) + (i & 3) * 16;
+          if (kb >= key_end) continue;
+          const int r = page_row(scalar_read(table, uniform(kb >> a.page_shift)), a.num_pages, a.page_shift);
+          if (r < 0) continue;
+          const bf16* const rows = static_cast<const bf16*>(a.vp) + int64_t(r + (kb & ps_mask)) * D;
+          uint32_t odd = 0;                   // keys with such a value
+#pragma unroll
+          for (int k = 0; k < 16; k += 64 / CPR) {
+            const bf16x8 v = *reinterpret_cast<const bf16x8*>(rows + k * D + lane * 8);
+            bool all = true;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) all &= finite(static_cast<float>(v[e]));
+#pragma unroll
+            for (int h = 0; h < 64 / CPR; ++h) odd |= (__ballot(!all) >> (h * CPR) & ((uint64_t(1) << CPR) - 1)) ? 1u << (k + h) : 0;
+          }
+          while (odd != 0) {
+            const int k = __builtin_ctz(odd), j = kb + k;
+            odd &= odd - 1;
+            const bool vis = (j <= min(my_pos, key_end - 1)) & ((j < s) | (j >= band_start(my_pos)));
+#pragma unroll
+            for (int c = 0; c < D / 8; ++c) {
+              const bf16x4 v = *reinterpret_cast<const bf16x4*>(rows + k * D + c * 8 + half * 4);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float x = static_cast<float>(v[e]);
+                oacc[c / 4][c % 4 * 4 + e] += vis && !finite(x) ? x : 0.0f;
+              }
             }
           }
         }
-        float tmax = -INFINITY;
-#pragma unroll
-        for (int sub = 0; sub < 2; ++sub)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) tmax = fmaxf(tmax, sacc[sub][r]);
-        tmax *= c2;
-        if (__any(tmax > m_run + kRescaleSlack)) {
-          const float m_new = fmaxf(m_run, max_xor<32>(tmax));
-          const float alpha = fast_exp2(m_run - m_new);
-          m_run = m_new;
-          l_run *= alpha;
-#pragma unroll
-          for (int dt = 0; dt < D / 32; ++dt) oacc[dt] *= alpha;
-        }
-        bf16x8 pf[2][2];
-        float psum = 0.0f;
-#pragma unroll
-        for (int sub = 0; sub < 2; ++sub) {
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              pf[sub][c][e] = static_cast<bf16>(fast_exp2(__builtin_fmaf(sacc[sub][8 * c + e], c2, -m_run)));
-#pragma unroll
-            for (int e = 0; e < 8; e += 2) psum = dot2_ones(pf[sub][c][e], pf[sub][c][e + 1], psum);
-          }
-        }
-        l_run += psum;
-#pragma unroll
-        for (int step = 0; step < 4; ++step) {
-          if (step + 1 < 4) {
-#pragma unroll
-            for (int dt = 0; dt < D / 32; ++dt) vf[(step + 1) & 1][dt] = vfrag(step + 1, dt);
-          }
-#pragma unroll
-          for (int dt = 0; dt < D / 32; ++dt) oacc[dt] = mma32(vf[step & 1][dt], pf[step >> 1][step & 1], oacc[dt]);
-        }
+        break;
       }
-      jt = j1;
-      j1 = j2;
-      j2 = j3;
-      pt = p1;
-      p1 = p2;
-      p2 = p3;
-      k_now = k_now == (KST - 1) * TL::TILE_BYTES ? 0 : k_now + TL::TILE_BYTES;
-      k_next = k_next == (KST - 1) * TL::TILE_BYTES ? 0 : k_next + TL::TILE_BYTES;
-      v_now ^= TL::TILE_BYTES;
+      // A weight of 0 times a value that is not finite is NaN, in a row that may not see it:
+      // the sums of every row are looked at once, and the tile is taken again if need be (2 % of
+      // 6 chunks behind 16,384, 1 us of a batch of 16 over 8,001 shared keys).
+      float zero = 0.0f;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) zero = __builtin_fmaf(oacc[dt][r], 0.0f, zero);
+      int* const bad = reinterpret_cast<int*>(lds.tiles);
+      const int mine_bad = __any(zero != 0.0f);
+      __syncthreads();                    // every tile has been read
+      if (lane == 0) bad[wave_id] = mine_bad;
+      __syncthreads();
+      int any_bad = 0;
+#pragma unroll
+      for (int v = 0; v < 4 * KG; ++v) any_bad |= bad[v];
+      if (!uniform(any_bad)) break;
+      __syncthreads();                    // before the tiles are loaded again
     }
     l_run = sum_xor<32>(l_run);
     if constexpr (KG > 1) {

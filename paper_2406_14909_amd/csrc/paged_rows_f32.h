@@ -14,6 +14,8 @@
 // absent pages read the pool's first row instead, and count as zeros with weight 0.
 #pragma once
 
+#include <type_traits>
+
 #include "paged_rows.h"
 
 namespace moa {
@@ -106,19 +108,6 @@ __device__ __forceinline__ void rows_f32(const PagedArgs& a, RowsF32Lds<D>& lds,
     };
 
     const int end = 2 * (t1 - t0);
-    int u = kg;
-    auto page_at = [&](int v) { return v < end ? page_of(tile_j0(v)) : -1; };
-    int row = row_of(tile_j0(u), page_at(u));
-    // K of a tile is asked for behind the scores of the one before, V in front of its own
-    // scores: each has a product's time to arrive, in one set of registers.
-    f32x4 kf[H / 4];
-    auto load_k = [&](int r) {
-      const float* p = static_cast<const float*>(a.kp) + int64_t(max(r, 0)) * D + half * 4;
-#pragma unroll
-      for (int i = 0; i < H / 4; ++i) kf[i] = *reinterpret_cast<const f32x4*>(p + 8 * i);
-    };
-    if (u < end) load_k(row);
-    int row_next = row_of(tile_j0(u + groups), page_at(u + groups));
     float qf[H];
 #pragma unroll
     for (int i = 0; i < H; i += 4) {
@@ -129,76 +118,126 @@ __device__ __forceinline__ void rows_f32(const PagedArgs& a, RowsF32Lds<D>& lds,
       for (int e = 0; e < 4; ++e) qf[i + e] = x[e];
     }
     f32x16 oacc[DT];
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) oacc[dt] = f32x16{};
-    float m_run = kNegBig, l_run = 0.0f;
+    float m_run, l_run;
     const float c2 = a.scale_log2;
 
-    for (; u < end; u += groups) {
-      const int j0 = tile_j0(u);
-      const uint32_t there = static_cast<uint32_t>(__ballot(row >= 0));
-      // Asked for in front of V and used behind it: a wait for it is none for K.
-      const int page_after = page_at(u + 2 * groups);
-      sched_fence();
-      float vf[16][DT];
+    // Over the piece's keys.  `careful`: the second time, for values that are not finite.
+    auto walk = [&](auto careful) {
+      constexpr bool kCareful = decltype(careful)::value;
+      int u = kg;
+      auto page_at = [&](int v) { return v < end ? page_of(tile_j0(v)) : -1; };
+      int row = row_of(tile_j0(u), page_at(u));
+      // K of a tile is asked for behind the scores of the one before, V in front of its own
+      // scores: each has a product's time to arrive, in one set of registers.
+      f32x4 kf[H / 4];
+      auto load_k = [&](int r) {
+        const float* p = static_cast<const float*>(a.kp) + int64_t(max(r, 0)) * D + half * 4;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int vrow = max(__shfl(row, (r >> 2) * 8 + half * 4 + (r & 3), 64), 0);
-        const float* p = static_cast<const float*>(a.vp) + int64_t(vrow) * D + lrow;
+        for (int i = 0; i < H / 4; ++i) kf[i] = *reinterpret_cast<const f32x4*>(p + 8 * i);
+      };
+      if (u < end) load_k(row);
+      int row_next = row_of(tile_j0(u + groups), page_at(u + groups));
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) vf[r][dt] = p[dt * 32];
-      }
-      sched_fence();
-      f32x16 sacc = f32x16{};
-#pragma unroll
-      for (int i = 0; i < H / 4; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sacc = mma32f(kf[i][e], qf[4 * i + e], sacc);
-      sched_fence();
-      if (u + groups < end) load_k(row_next);
-      sched_fence();
-      if (there != 0xffffffffu) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt)
-            vf[r][dt] = there >> ((r >> 2) * 8 + half * 4 + (r & 3)) & 1 ? vf[r][dt] : 0.0f;
-      }
-
-      const bool all_vis = full && there == 0xffffffffu && j0 + 31 <= p_first && j0 + 32 <= key_end &&
-                           (j0 + 32 <= s || band_start(p_last) <= j0);
-      if (!all_vis) {
-        const int jl = j0 + half * 4;                       // key of register 0 of this lane
-        const int hi = min(my_pos, key_end - 1) - jl, band = band_start(my_pos) - jl, sink = s - jl;
+      for (int dt = 0; dt < DT; ++dt) oacc[dt] = f32x16{};
+      m_run = kNegBig;
+      l_run = 0.0f;
+      for (; u < end; u += groups) {
+        const int j0 = tile_j0(u);
+        const uint32_t there = static_cast<uint32_t>(__ballot(row >= 0));
+        // Asked for in front of V and used behind it: a wait for it is none for K.
+        const int page_after = page_at(u + 2 * groups);
+        sched_fence();
+        float vf[16][DT];
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const int dj = (r >> 2) * 8 + (r & 3);
-          const bool vis = (dj <= hi) & ((dj < sink) | (dj >= band)) & ((there >> (dj + half * 4) & 1) != 0);
-          sacc[r] = vis ? sacc[r] : -INFINITY;
+          const int vrow = max(__shfl(row, (r >> 2) * 8 + half * 4 + (r & 3), 64), 0);
+          const float* p = static_cast<const float*>(a.vp) + int64_t(vrow) * D + lrow;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) vf[r][dt] = p[dt * 32];
         }
+        sched_fence();
+        f32x16 sacc = f32x16{};
+#pragma unroll
+        for (int i = 0; i < H / 4; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sacc = mma32f(kf[i][e], qf[4 * i + e], sacc);
+        sched_fence();
+        if (u + groups < end) load_k(row_next);
+        sched_fence();
+        if (there != 0xffffffffu) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+              vf[r][dt] = there >> ((r >> 2) * 8 + half * 4 + (r & 3)) & 1 ? vf[r][dt] : 0.0f;
+        }
+        if constexpr (kCareful) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) vf[r][dt] = finite(vf[r][dt]) ? vf[r][dt] : 0.0f;
+        }
+
+        const bool all_vis = full && there == 0xffffffffu && j0 + 31 <= p_first && j0 + 32 <= key_end &&
+                             (j0 + 32 <= s || band_start(p_last) <= j0);
+        if (!all_vis) {
+          const int jl = j0 + half * 4;                       // key of register 0 of this lane
+          const int hi = min(my_pos, key_end - 1) - jl, band = band_start(my_pos) - jl, sink = s - jl;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int dj = (r >> 2) * 8 + (r & 3);
+            const bool vis = (dj <= hi) & ((dj < sink) | (dj >= band)) & ((there >> (dj + half * 4) & 1) != 0);
+            sacc[r] = vis ? sacc[r] : -INFINITY;
+          }
+        }
+        float tmax = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) tmax = fmaxf(tmax, sacc[r]);
+        tmax *= c2;
+        if (__any(tmax > m_run + kRescaleSlack)) {
+          const float m_new = fmaxf(m_run, max_xor<32>(tmax));
+          const float alpha = fast_exp2(m_run - m_new);
+          m_run = m_new;
+          l_run *= alpha;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) oacc[dt] *= alpha;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float p = fast_exp2(__builtin_fmaf(sacc[r], c2, -m_run));
+          l_run += p;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) oacc[dt] = mma32f(vf[r][dt], p, oacc[dt]);
+        }
+        if constexpr (kCareful) {           // what is not finite goes to the rows that see its key
+#pragma unroll 1
+          for (int k = 0; k < 32; ++k) {
+            const int r = __builtin_amdgcn_readlane(row, k);
+            if (r < 0) continue;
+            const int j = j0 + k;
+            const bool vis = (j <= min(my_pos, key_end - 1)) & ((j < s) | (j >= band_start(my_pos)));
+            const float* p = static_cast<const float*>(a.vp) + int64_t(r) * D + half * 4;
+#pragma unroll
+            for (int c = 0; c < D / 8; ++c) {
+              const f32x4 x = *reinterpret_cast<const f32x4*>(p + c * 8);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) oacc[c / 4][c % 4 * 4 + e] += vis && !finite(x[e]) ? x[e] : 0.0f;
+            }
+          }
+        }
+        row = row_next;
+        row_next = row_of(tile_j0(u + 2 * groups), page_after);
       }
-      float tmax = -INFINITY;
+    };
+    walk(std::false_type{});
+    // A weight of 0 times a value that is not finite is NaN, in a row that may not see it: the
+    // sums of every row are looked at once, and the keys are taken again if need be.
+    float zero = 0.0f;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) tmax = fmaxf(tmax, sacc[r]);
-      tmax *= c2;
-      if (__any(tmax > m_run + kRescaleSlack)) {
-        const float m_new = fmaxf(m_run, max_xor<32>(tmax));
-        const float alpha = fast_exp2(m_run - m_new);
-        m_run = m_new;
-        l_run *= alpha;
+    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) oacc[dt] *= alpha;
-      }
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float p = fast_exp2(__builtin_fmaf(sacc[r], c2, -m_run));
-        l_run += p;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) oacc[dt] = mma32f(vf[r][dt], p, oacc[dt]);
-      }
-      row = row_next;
-      row_next = row_of(tile_j0(u + 2 * groups), page_after);
-    }
+      for (int r = 0; r < 16; ++r) zero = __builtin_fmaf(oacc[dt][r], 0.0f, zero);
+    if (__any(zero != 0.0f)) walk(std::true_type{});
     l_run = sum_xor<32>(l_run);
 
     // The waves' states of the same rows sit in the same lanes.
