@@ -49,7 +49,7 @@ __device__ __forceinline__ f32x4 mma16(const bf16x8& a, const bf16x8& b, const f
 // its keys read here, all of them, so that those that a tile of sequences reads of the
 // prefix are one run without holes.
 __device__ __forceinline__ VisibleKeys keys_of(const PagedArgs& a, int pos, int g) {
-  return visible_keys(pos, a.window[g], 0, a.num_sink, pos + 1 < a.prefix_len ? 0 : a.prefix_len,
+  return visible_keys(pos, a.window[g], 0, a.num_sink, pos < a.prefix_len - 1 ? 0 : a.prefix_len,
                       a.max_pages << a.page_shift);
 }
 

@@ -251,3 +251,20 @@ def test_scale_and_large_scores():
             c = Paged(4, 2, 64, 3, [60, 300], dt, [200], counts, page=32, scale=4.0, seed=11)
             c.q *= 0.25
             c.check("large scores")
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_positions_past_the_table(dt):
+    """Keys past the table are absent: a row there sees the sinks and what the table holds of its band."""
+    _say("past the table", dt)
+    far = [2 ** 31 - 1, 160, 2 ** 30, 139, 500]
+    for counts, prefix in ((None, 0), (None, 100), ([1, 40, 3, 9, 2], 0)):
+        c = Paged(4, 2, 64, 20, [50, 130], dt, [130, 120, 125, 110, 115], counts, page=16, prefix_len=prefix, seed=12)
+        c.width = 9                                # 144 positions, with all of which the pages are filled
+        c.table, c.prefix_table = c.table[:, :, :9].copy(), c.prefix_table[:, :9].copy()
+        c.table[:, :, :] = np.random.default_rng(13).integers(0, c.num_pages, c.table.shape)
+        c.prefix_table[:, :] = c.table[0]
+        gen = torch.Generator().manual_seed(14)
+        c.k, c.v = (torch.randn(c.k.shape, generator=gen).to(c.dtype) for _ in range(2))
+        c.positions = far
+        c.check(f"past the table {dt} {counts} {prefix}")
