@@ -280,7 +280,7 @@ __device__ __forceinline__ void rows_bf16(const PagedArgs& a, RowsBf16Lds<D, KG>
         const int ok = present(pt);
         if (t + KG < t1) __builtin_amdgcn_s_waitcnt(0x0F70 | DPW);  // the next K may be in flight
         else __builtin_amdgcn_s_waitcnt(0x0F70);
-        if (careful && t < t1) {                // this wave's values of the tile: 0 in place of what is not finite
+        if (__builtin_expect(careful && t < t1, 0)) {   // this wave's values of the tile: 0 in place of what is not finite
 #pragma unroll 1
           for (int i = 0; i < DPW; ++i) {
             bf16x8* const at = reinterpret_cast<bf16x8*>(sV + v_now + (wave * DPW + i) * 1024 + lane * 16);
