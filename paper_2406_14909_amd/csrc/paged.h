@@ -111,10 +111,12 @@ constexpr int kPagedMaxWorkers = 4096;   // decode workers (work-groups) per lau
 
 int launch_paged_append(const PagedAppendArgs& a, int dtype, int head_dim, void* stream);
 constexpr int kPagedLogRowGroups = 9;
-constexpr int kPagedRowGroups = 1 << kPagedLogRowGroups;   // work-groups that row tiles are cut for (two per compute unit)
+// Work-groups that row tiles are cut for, two per compute unit (twice as many: 6 chunks behind
+// 16,000 keys 262 -> 270 us, fp32, 2 x 16 heads of 64 x 1,501, 69 -> 81).
+constexpr int kPagedRowGroups = 1 << kPagedLogRowGroups;
 // Work-groups over a shared prefix, about, and over the keys behind it: one of each per
-// compute unit (16 x 8 x 4 heads on 8,001 keys and 48 x 8 x 8 on 32,700: 22.2 and 52.5 us; 384
-// for the prefix 26.6 and 58.6, 192 23.7 and 56.4; 512 behind it 24.6 and 57.8).
+// compute unit (16 x 8 x 4 heads on 8,001 keys and 48 x 8 x 8 on 32,700: 23.1 and 52.5 us; 384
+// for the prefix 27.4 and 59.7, 192 24.2 and 56.3; 512 behind it 25.1 and 57.8).
 constexpr int kPagedPrefixItems = 256;
 MOA_PAGED_FN int paged_tile_rows(int dtype) { return dtype == MOA_BF16 ? 128 : 64; }
 

@@ -526,8 +526,8 @@ __device__ __forceinline__ void decode_mma(const PagedArgs& a, MmaLds<D>& lds, u
 }
 
 // The worker of a type: bf16 goes to the matrix units, of single heads too, as they leave the
-// vector units to the rest (1 x 32 heads of 8,200 keys on average 29.7 -> 28.8 us, 32 x 32
-// of 4,200 238 -> 233).
+// vector units to the rest (1 x 32 heads of 8,200 keys on average 29.4 -> 28.5 us, 32 x 32
+// of 4,200 235 -> 232).
 template <typename T>
 constexpr __host__ __device__ bool on_matrix_units() { return sizeof(T) == 2; }
 template <typename T, int D, int G>

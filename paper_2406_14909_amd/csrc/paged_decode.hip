@@ -7,7 +7,7 @@ namespace {
 
 // Two work-groups per compute unit where the matrix units do the work: a wave then has a whole
 // tile on its way while it works on another (with three, in 168 registers, 16 sequences x 8 KV
-// heads x 4 query heads, 357 MB: 82.6 us, without the loads ahead 76.2; with two 63.1).
+// heads x 4 query heads, 357 MB: 82.2 us, without the loads ahead 76.2; with two 62.0).
 template <typename T, int D, int G>
 __global__ void __launch_bounds__(kThreads, (on_matrix_units<T>() ? 2 : 1)) paged_decode_kernel(PagedArgs a) {
   __shared__ __attribute__((aligned(1024))) DecodeLds<T, D, G> lds;

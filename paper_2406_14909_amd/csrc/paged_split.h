@@ -62,22 +62,24 @@ struct VisiblePages {
 // ---------------------------------------------------------------------------
 // Row tiles.
 // ---------------------------------------------------------------------------
-constexpr int kTileCost = 96;        // keys: what a row tile's start and end cost, about
+// Keys: what a row tile's start and end cost, about (8 heads x 4 query heads x 5,000 tokens: 239 us
+// with 96, 234 with 192 and 288; fp32, 2 x 16 heads of 64 x 1,501: 69.5, 68.8, 70.4).
+constexpr int kTileCost = 192;
 
 // A piece costs a start and partial results of 128 rows on their way out and back (67 KB
 // each way), so it has kLeastRowCost at least (8 heads x 4 query heads, 64 tokens behind
-// 8,000: 36, 33, 38 and 54 us in pieces of 128, 256, 512 and 1,024), and a call is cut only
+// 8,000: 37, 35, 36 and 47 us in pieces of 128, 256, 512 and 1,024), and a call is cut only
 // where the longest row tile costs kWholeRowCost more than an equal share of all (the same
-// heads, whole and cut: 3,000 tokens 93 and 130 us, 2,048 67 and 82, 1,500 63 and 61; fp32,
-// where a key takes longer, 16 heads of 64 x 1,501 tokens 90 and 72).
+// heads, whole and cut: 3,000 tokens 98 and 139 us, 2,048 68 and 87, 1,500 52 and 66; fp32,
+// where a key takes longer, 16 heads of 64 x 1,501 tokens 93 and 73).
 constexpr int kLeastRowCost = 256;
 constexpr int kWholeRowCost = 1200;
 constexpr int kWholeRowCostF32 = 600;
 // Where the table has no room for longer row tiles than these, nothing is cut, and the merge
-// is left out (512 tokens 21.9 -> 18.7 us); and so few that each work-group can have a compute
-// unit for itself are walked by two groups of waves (1,500 tokens, 376 tiles, 61 -> 53 us; 504
-// tiles 45 -> 58).  Very few are worth cutting all the same, unless they are shorter still (30
-// tokens behind 1,900, 8 tiles: whole 47 us).
+// is left out (512 tokens 22.3 -> 18.9 us); and so few that each work-group can have a compute
+// unit for itself are walked by two groups of waves (1,500 tokens, 376 tiles, 55 -> 47 us; 504
+// tiles 51 -> 59).  Very few are worth cutting all the same, unless they are shorter still (30
+// tokens behind 1,900, 8 tiles: whole 40 us, cut 29).
 constexpr int kShortRowCost = 2200;
 constexpr int kShortRowCostF32 = 600;
 constexpr int kKeyGroupTiles = 400;
