@@ -10,6 +10,8 @@
 // itself (a prefix sum over the pairs, one trip to memory), which costs less than a
 // launch of its own would.  Softmax statistics and sums are fp32 and kept relative to a
 // running maximum; a cache that is cut leaves partial results that a second kernel merges.
+// 16 sequences x 8 heads x 4 query heads, 0.36 GB: 62 us, 57 of them this kernel at
+// 6.3 TB/s; one sequence x 32 heads, 35 MB: 13.8 us, most of them the start and the merge.
 //
 // Page numbers of a piece are fetched in one go into LDS, as rows of the pool; one lane
 // per key forms the row of its key a tile ahead, and the lanes that load the row get it
