@@ -64,7 +64,8 @@ struct PagedArgs {
   int32_t slots;                 // work-groups that the keys are cut for
   int32_t most_tiles;            // rows: as many row tiles as there can be
   int32_t least_cost;            // rows: keys of a piece, at least
-  int32_t whole_cost;            // rows: keys of a row tile that is not worth cutting
+  int32_t whole_cost;            // rows: keys of a row tile that is not worth cutting,
+  int32_t full_cost;             // and with row tiles for most of the work-groups
   int32_t log_slots;             // rows: log2(slots)
   int32_t prefix_items;          // work-groups over a shared prefix
   int32_t n_tokens;

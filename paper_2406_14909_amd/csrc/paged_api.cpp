@@ -281,6 +281,7 @@ moa_status_t moa_paged_prefill(const moa_plan_t* plan, const moa_pages_t* pages,
   a.most_tiles = static_cast<int32_t>(tiles);
   a.least_cost = kLeastRowCost;
   a.whole_cost = bf16 ? kWholeRowCost : kWholeRowCostF32;
+  a.full_cost = bf16 ? kFullRowCost : kWholeRowCostF32;
   // a work-group per row tile, dealt to the dies in whole rounds, or per piece
   const int64_t groups = std::max<int64_t>((tiles + 127) / 128 * 128, whole ? 0 : kPagedRowGroups);
   int err = launch_paged_rows(a, d.dtype, d.head_dim, key_groups, groups, hip_stream);

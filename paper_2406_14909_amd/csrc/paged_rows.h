@@ -162,7 +162,8 @@ __device__ __forceinline__ void for_each_row_tile(const PagedArgs& a, int block,
 
   // Whole row tiles, where the longest takes little more than an equal share of the work.
   PagedSeg* const segs = reinterpret_cast<PagedSeg*>(a.plan);
-  if (a.plan == nullptr || (longest - a.whole_cost) * a.slots <= units) {
+  const int worth = 4 * all >= 3 * a.slots ? a.full_cost : a.whole_cost;
+  if (a.plan == nullptr || (longest - worth) * a.slots <= units) {
     if (a.plan != nullptr && block < a.slots && threadIdx.x == 0) segs[block].rows = 0;
     // Dealt to the dies in units of 16 neighbours, one unit to each die in turn and back
     // again; few singly.  Of a pair the last first: theirs are the most keys.

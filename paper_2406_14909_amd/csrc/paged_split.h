@@ -71,10 +71,14 @@ constexpr int kTileCost = 192;
 // 8,000: 37, 35, 36 and 47 us in pieces of 128, 256, 512 and 1,024), and a call is cut only
 // where the longest row tile costs kWholeRowCost more than an equal share of all (the same
 // heads, whole and cut: 3,000 tokens 98 and 139 us, 2,048 68 and 87, 1,500 52 and 66; fp32,
-// where a key takes longer, 16 heads of 64 x 1,501 tokens 93 and 73).
+// where a key takes longer, 16 heads of 64 x 1,501 tokens 93 and 73).  With row tiles for most
+// work-groups, whose pieces would nearly all be parts, it takes kFullRowCost in bf16 (8 heads x 4
+// query heads, 2,000 tokens behind 1,000 and 2,000, 1,426 and 1,647 more: whole 83 and 104 us, cut
+// 102 and 124; 32 heads, 1,513 and 1,959 more: 108 and 140, cut 106 and 130).
 constexpr int kLeastRowCost = 256;
 constexpr int kWholeRowCost = 1200;
 constexpr int kWholeRowCostF32 = 600;
+constexpr int kFullRowCost = 1700;
 // Where the table has no room for longer row tiles than these, nothing is cut, and the merge
 // is left out (512 tokens 22.3 -> 18.9 us); and so few that each work-group can have a compute
 // unit for itself are walked by two groups of waves (1,500 tokens, 376 tiles, 55 -> 47 us; 504
