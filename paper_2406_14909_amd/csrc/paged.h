@@ -112,7 +112,7 @@ constexpr int kPagedMaxWorkers = 4096;   // decode workers (work-groups) per lau
 
 int launch_paged_append(const PagedAppendArgs& a, int dtype, int head_dim, void* stream);
 constexpr int kPagedLogRowGroups = 9;
-// Work-groups that row tiles are cut for, two per compute unit (twice as many: 6 chunks behind
+// Work-groups that row tiles are cut for, at most, two per compute unit (twice as many: 6 chunks behind
 // 16,000 keys 262 -> 270 us, fp32, 2 x 16 heads of 64 x 1,501, 69 -> 81).
 constexpr int kPagedRowGroups = 1 << kPagedLogRowGroups;
 // Work-groups over a shared prefix, about, and over the keys behind it: one of each per
