@@ -328,13 +328,16 @@ moa_status_t moa_paged_decode_shared(const moa_plan_t* plan, const moa_pages_t* 
     a.rows_part = reinterpret_cast<float*>(ws + space.rows);
     const int rows = paged_tile_rows(d.dtype);
     const int64_t tiles = (int64_t(batch) * plan->group + rows - 1) / rows;
-    // Pieces of as few key tiles as give no more than kPagedPrefixItems work-groups.
+    // Pieces of as few key tiles as give no more than `most` work-groups.
     int64_t keys[MOA_MAX_KV_HEADS], sum = 0, pieces = 0;
     for (int h = 0; h < d.num_kv_heads; ++h) {
       keys[h] = (std::min<int64_t>(prefix_len, int64_t(d.num_sink) + plan->window[h] + 63) + 63) / 64;
       sum += keys[h];
     }
-    constexpr int64_t most = kPagedPrefixItems;
+    // fp32 at head_dim 128 has one work-group per compute unit, and half of them for each (16 x
+    // 32/8 heads over 8,001 keys 54.6 -> 46.2 us, 3 over 5,000 40.5 -> 29.7, 32 over 2,000 with
+    // up to 4,000 of their own 172.5 -> 175.8).
+    const int32_t most = d.dtype == MOA_BF16 || d.head_dim == 64 ? kPagedPrefixItems : kPagedPrefixItems / 2;
     int64_t longest = std::max<int64_t>(2, (sum * tiles + most - 1) / most);
     for (;; ++longest) {
       pieces = 0;
@@ -348,7 +351,7 @@ moa_status_t moa_paged_decode_shared(const moa_plan_t* plan, const moa_pages_t* 
     }
     a.prefix_piece[d.num_kv_heads] = static_cast<int32_t>(pieces);
     a.prefix_items = static_cast<int32_t>(pieces * tiles);
-    a.slots = kPagedPrefixItems;
+    a.slots = most;
     return launched(who, launch_paged_shared(a, d.dtype, d.head_dim, plan->group, hip_stream));
   }
   return launched(who, launch_paged_decode(a, d.dtype, d.head_dim, plan->group, hip_stream));
