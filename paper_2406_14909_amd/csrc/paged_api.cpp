@@ -329,20 +329,23 @@ moa_status_t moa_paged_decode_shared(const moa_plan_t* plan, const moa_pages_t* 
     const int rows = paged_tile_rows(d.dtype);
     const int64_t tiles = (int64_t(batch) * plan->group + rows - 1) / rows;
     // Pieces of as few key tiles as give no more than `most` work-groups.
-    int64_t keys[MOA_MAX_KV_HEADS], sum = 0, pieces = 0;
+    int64_t keys[MOA_MAX_KV_HEADS], sum = 0, pieces = 0, widest = 0;
     for (int h = 0; h < d.num_kv_heads; ++h) {
       keys[h] = (std::min<int64_t>(prefix_len, int64_t(d.num_sink) + plan->window[h] + 63) + 63) / 64;
       sum += keys[h];
+      widest = std::max(widest, keys[h]);
     }
     // fp32 at head_dim 128 has one work-group per compute unit, and half of them for each (16 x
     // 32/8 heads over 8,001 keys 54.6 -> 46.2 us, 3 over 5,000 40.5 -> 29.7, 32 over 2,000 with
     // up to 4,000 of their own 172.5 -> 175.8).
     const int32_t most = d.dtype == MOA_BF16 || d.head_dim == 64 ? kPagedPrefixItems : kPagedPrefixItems / 2;
     int64_t longest = std::max<int64_t>(2, (sum * tiles + most - 1) / most);
-    for (;; ++longest) {
+    for (int64_t end = widest; longest < end;) {      // at the widest head's keys there is one piece per head
+      const int64_t mid = (longest + end) / 2;
       pieces = 0;
-      for (int h = 0; h < d.num_kv_heads; ++h) pieces += (keys[h] + longest - 1) / longest;
-      if (pieces * tiles <= most || pieces == d.num_kv_heads) break;
+      for (int h = 0; h < d.num_kv_heads; ++h) pieces += (keys[h] + mid - 1) / mid;
+      if (pieces * tiles <= most) end = mid;
+      else longest = mid + 1;
     }
     pieces = 0;
     for (int h = 0; h < d.num_kv_heads; ++h) {
