@@ -199,7 +199,8 @@ __device__ __forceinline__ void merge_waves_and_store(const PagedArgs& a, const 
       asum += s_acc[(v * G + h) * D + d] * f;
     }
     if (whole) {
-      static_cast<T*>(a.o)[(int64_t(b) * a.hq + g * G + h) * D + d] = static_cast<T>(lsum > 0.0f ? asum / lsum : 0.0f);
+      // no key: zeros; a sum that is no number stays one, as in the merge of a cache that is cut
+      static_cast<T*>(a.o)[(int64_t(b) * a.hq + g * G + h) * D + d] = static_cast<T>(lsum == 0.0f ? 0.0f : asum / lsum);
     } else {
       float* pp = a.part + ((int64_t(w) + pair) * G + h) * PS;
       pp[d] = asum;
