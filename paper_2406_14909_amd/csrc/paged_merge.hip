@@ -102,9 +102,11 @@ __global__ void __launch_bounds__(kThreads) paged_merge_kernel(PagedArgs a) {
         m = mx;
 #pragma unroll
         for (int u = 0; u < kFlight; ++u) {
-          const float wgt = p0 + u * step < seg.pieces ? fast_exp2(mp[u] - mx) : 0.0f;
+          // past the last piece, which is read again there, sums count as zeros: they may be infinite
+          const bool more = p0 + u * step < seg.pieces;
+          const float wgt = more ? fast_exp2(mp[u] - mx) : 0.0f;
           l += wgt * lp[u];
-          acc += xp[u] * wgt;
+          acc += (more ? xp[u] : f32x4{0.0f, 0.0f, 0.0f, 0.0f}) * wgt;
         }
       }
     }

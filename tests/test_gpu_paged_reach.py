@@ -76,3 +76,21 @@ def test_decode_of_one_key(dt, hq):
         c = Paged(hq, 1, 64, 0, (1,), dt, (0, 17), page=16, seed=2)
         _put(c, kind, 0, 0, 0, 3)
         _check(c)
+
+
+# heads, windows, positions, counts: one row tile whole, and ones cut into few and into many pieces
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv,windows,positions,counts", [
+    (2, 2, (30, 100), (5,), (60,)), (8, 1, (1500,), (1700,), (24,)), (8, 2, (3000, 2000), (2900, 2500), (9, 30)),
+    (2, 1, (14000,), (14000,), (20,))])
+@pytest.mark.parametrize("kind", ["query nan", "key nan", "value inf"])
+def test_prefill(kind, dt, hq, hkv, windows, positions, counts):
+    print("[case]", kind, dt, hq, windows, flush=True)
+    c = Paged(hq, hkv, 128, 4, windows, dt, positions, counts, page=16, seed=3)
+    for i, (p, n) in enumerate(zip(positions, counts)):
+        for g in range(hkv):
+            _put(c, kind, i, g, p + n // 2, 5 + g)          # a key that some of the sequence's rows see
+            if kind == "value inf":
+                _put(c, kind, i, g, p + n - 1, 40, -1.0)     # the last key, in the last piece
+                _put(c, kind, i, g, max(0, p - 20), 77)      # one that all rows see
+    _check(c)
