@@ -21,7 +21,8 @@
 // matrix products (the G query heads padded to 16 columns),
 //   S^T = K Q^T  (A = 16 keys x 32 dims, from whole rows turned in LDS),
 //   O^T += V^T P^T  (B = P^T from the score registers, A = V^T by the transposing LDS
-//   read, the keys of a step permuted alike on both sides).
+//   read, the keys of a step permuted alike on both sides).  P^T is in bf16: of a single
+//   head in two columns, the second for what rounding left over, of groups in one each.
 #pragma once
 
 #include <type_traits>
@@ -180,24 +181,32 @@ __device__ __forceinline__ void for_each_span(const PagedArgs& a, Walk& s, int b
   }
 }
 
-// Merges the waves' states of one cache held in LDS (acc[w][h][d], ml[w][h] = (m, l)) and
-// writes either o (all keys) or the worker's partial.
-template <typename T, int D, int G>
+// Merges the waves' states of one cache held in LDS (acc[w][h][d], ml[w][h] = (m, l), and with
+// PARTS = 2 the sums of what the weights' rounding left over at h + G) and writes either o (all
+// keys) or the worker's partial.  An infinite value makes NaN of the small parts' sums, which
+// are left out there.
+template <typename T, int D, int G, int PARTS>
 __device__ __forceinline__ void merge_waves_and_store(const PagedArgs& a, const float* s_acc, const float* s_ml,
                                                       uint32_t w, int b, int g, int pair, bool whole) {
   constexpr int PS = D + kPagedPartPad;
+  constexpr int H = PARTS * G;
   for (int idx = threadIdx.x; idx < G * D; idx += kThreads) {
     const int h = idx / D, d = idx % D;
     float mx = kNegBig;
 #pragma unroll
-    for (int v = 0; v < kWaves; ++v) mx = fmaxf(mx, s_ml[(v * G + h) * 2]);
-    float lsum = 0.0f, asum = 0.0f;
+    for (int v = 0; v < kWaves; ++v) mx = fmaxf(mx, s_ml[(v * H + h) * 2]);
+    float lsum = 0.0f, asum = 0.0f, low = 0.0f;
 #pragma unroll
     for (int v = 0; v < kWaves; ++v) {
-      const float f = fast_exp2(s_ml[(v * G + h) * 2] - mx);
-      lsum += s_ml[(v * G + h) * 2 + 1] * f;
-      asum += s_acc[(v * G + h) * D + d] * f;
+      const float f = fast_exp2(s_ml[(v * H + h) * 2] - mx);
+      lsum += s_ml[(v * H + h) * 2 + 1] * f;
+      asum += s_acc[(v * H + h) * D + d] * f;
+      if constexpr (PARTS == 2) {
+        lsum += s_ml[(v * H + G + h) * 2 + 1] * f;
+        low += s_acc[(v * H + G + h) * D + d] * f;
+      }
     }
+    if constexpr (PARTS == 2) asum += finite(asum) ? low : 0.0f;
     if (whole) {
       // no key: zeros; a sum that is no number stays one, as in the merge of a cache that is cut
       static_cast<T*>(a.o)[(int64_t(b) * a.hq + g * G + h) * D + d] = static_cast<T>(lsum == 0.0f ? 0.0f : asum / lsum);
@@ -339,7 +348,7 @@ __device__ __forceinline__ void decode_valu(const PagedArgs& a, ValuLds<D, G>& l
       }
     }
     __syncthreads();
-    merge_waves_and_store<T, D, G>(a, s_acc, s_ml, w, b, g, pair, whole && a.rows_part == nullptr);
+    merge_waves_and_store<T, D, G, 1>(a, s_acc, s_ml, w, b, g, pair, whole && a.rows_part == nullptr);
     __syncthreads();                                // LDS is used by the next cache
   });
 }
@@ -373,15 +382,21 @@ template <int D, int G>
 __device__ __forceinline__ void decode_mma(const PagedArgs& a, MmaLds<D>& lds, uint32_t w) {
   using TL = MmaTile<D>;
   constexpr int KT = TL::KT, KS = TL::KS, DT = TL::DT, RB = TL::RB, CPR = TL::CPR, LD = TL::LD;
-  static_assert(G >= 1 && G <= 16, "query heads per KV head");
-  static_assert((G * D + 2 * G) * 4 <= KT * RB, "the waves' states fit the tiles' LDS");
+  // Parts of a weight, each with columns of its own of the 16.  Of single heads, whose other
+  // columns are empty anyway, a weight keeps 16 bits (is within 2^-16 of itself), so that a sum over
+  // many keys is as good as moa_decode's, which keeps 32 (32 heads, 2,100 keys each 13.5 -> 13.7 us;
+  // 32 x 32, 4,180 each, 320 -> 321).  Of groups it keeps 8, as in moa_decode (with 16, 23 x 8 KV
+  // heads x 8 query heads 37.0 -> 38.4 us).
+  constexpr int PARTS = G == 1 ? 2 : 1;
+  static_assert(G >= 1 && PARTS * G <= 16, "query heads per KV head");
+  static_assert((PARTS * G * D + PARTS * 2 * G) * 4 <= KT * RB, "the waves' states fit the tiles' LDS");
   Walk& s_walk = lds.walk;
   float* s_acc = reinterpret_cast<float*>(&lds.tile[0][0]);
-  float* s_ml = s_acc + kWaves * G * D;
+  float* s_ml = s_acc + kWaves * PARTS * G * D;
 
   const int lane = threadIdx.x & 63;
   const int wave = uniform(threadIdx.x >> 6);
-  const int n = lane & 15;        // query head
+  const int n = lane & 15;        // column: query head n % G of part n / G
   const int q4 = lane >> 4;       // 16-lane group
   char* ts = &lds.tile[wave][0];
 
@@ -405,10 +420,10 @@ __device__ __forceinline__ void decode_mma(const PagedArgs& a, MmaLds<D>& lds, u
   }
 
   for_each_piece(a, s_walk, w, TL::kRoundShift, [&](int b, int g, const VisibleKeys& keys, int x0, int x1, bool whole, int pair) {
-    // B = Q^T: lane holds query head n, dims 32*kk + 8*q4 .. +7 (zero past G).
+    // B = Q^T: lane holds column n, dims 32*kk + 8*q4 .. +7 (zero past the last part).
     bf16x8 qop[KS];
-    if (n < G) {
-      const bf16* qp = static_cast<const bf16*>(a.q) + (int64_t(b) * a.hq + g * G + n) * D + 8 * q4;
+    if (n < PARTS * G) {
+      const bf16* qp = static_cast<const bf16*>(a.q) + (int64_t(b) * a.hq + g * G + n % G) * D + 8 * q4;
 #pragma unroll
       for (int kk = 0; kk < KS; ++kk) qop[kk] = *reinterpret_cast<const bf16x8*>(qp + 32 * kk);
     } else {
@@ -486,12 +501,14 @@ __device__ __forceinline__ void decode_mma(const PagedArgs& a, MmaLds<D>& lds, u
         for (int dt = 0; dt < DT; ++dt) oacc[dt] *= alpha;
 
         // P^T: score tiles 0 (keys 4*q4 + i) and 1 (keys 16 + 4*q4 + i).  Weights are rounded
-        // to bf16 for the product; the sum is taken over the rounded ones.
+        // to bf16 for the product, and what that leaves over, in the second part's columns, once
+        // more; the sum is taken over the same parts.
         bf16x8 pop;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          pop[i] = static_cast<bf16>(fast_exp2(__builtin_fmaf(s[0][i], c2, -m_new)));
-          pop[4 + i] = static_cast<bf16>(fast_exp2(__builtin_fmaf(s[1][i], c2, -m_new)));
+        for (int i = 0; i < 8; ++i) {
+          const float p = fast_exp2(__builtin_fmaf(s[i >> 2][i & 3], c2, -m_new));
+          pop[i] = static_cast<bf16>(p);
+          if constexpr (PARTS == 2) pop[i] = n < G ? pop[i] : static_cast<bf16>(p - static_cast<float>(pop[i]));
         }
 #pragma unroll
         for (int i = 0; i < 8; i += 2) l_run = dot2_ones(pop[i], pop[i + 1], l_run);
@@ -513,24 +530,25 @@ __device__ __forceinline__ void decode_mma(const PagedArgs& a, MmaLds<D>& lds, u
     l_run = sum_xor<16>(l_run);
     l_run = sum_xor<32>(l_run);
     __syncthreads();                                // every wave is done with its tile
-    if (n < G) {
-      float* sa = s_acc + (wave * G + n) * D + 4 * q4;   // lane holds O^T rows 16*dt + 4*q4 + i
+    if (n < PARTS * G) {
+      const int at = wave * PARTS * G + n;
+      float* sa = s_acc + at * D + 4 * q4;               // lane holds O^T rows 16*dt + 4*q4 + i
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4*>(sa + 16 * dt) = oacc[dt];
       if (q4 == 0) {
-        s_ml[(wave * G + n) * 2] = m_run;
-        s_ml[(wave * G + n) * 2 + 1] = l_run;
+        s_ml[at * 2] = m_run;
+        s_ml[at * 2 + 1] = l_run;
       }
     }
     __syncthreads();
-    merge_waves_and_store<bf16, D, G>(a, s_acc, s_ml, w, b, g, pair, whole && a.rows_part == nullptr);
+    merge_waves_and_store<bf16, D, G, PARTS>(a, s_acc, s_ml, w, b, g, pair, whole && a.rows_part == nullptr);
     __syncthreads();                                // LDS is used by the next cache
   });
 }
 
 // The worker of a type: bf16 goes to the matrix units, of single heads too, as they leave the
-// vector units to the rest (1 x 32 heads of 8,200 keys on average 29.4 -> 28.5 us, 32 x 32
-// of 4,200 235 -> 232).
+// vector units to the rest (32 heads of 8,260 keys on average 29.0 -> 28.3 us, 32 x 32 of 4,180
+// 326 -> 321).
 template <typename T>
 constexpr __host__ __device__ bool on_matrix_units() { return sizeof(T) == 2; }
 template <typename T, int D, int G>
