@@ -236,6 +236,14 @@ def _stream(t, stream) -> ctypes.c_void_p:
     return ctypes.c_void_p(stream.cuda_stream)
 
 
+def _new(shape, dtype, device, stream):
+    """A call's output, from the memory of the stream that writes it: a block of the current stream's may
+    still be read or written there by earlier work."""
+    import torch
+    with torch.cuda.stream(stream):                  # None: the current one
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _one_device(**tensors):
     """The GPU that every tensor of a call lives on; the call runs with it as
     the current device (raises if the tensors are spread over devices)."""
@@ -270,7 +278,7 @@ def moa_prefill(plan: Plan, q, k, v, o=None, stream=None):
     _need(k, (bsz, n, plan.num_kv_heads, plan.head_dim), dt, "k")
     _need(v, (bsz, n, plan.num_kv_heads, plan.head_dim), dt, "v")
     if o is None:
-        o = torch.empty_like(q)
+        o = _new(q.shape, dt, q.device, stream)
     _need(o, q.shape, dt, "o")
     with torch.cuda.device(_one_device(q=q, k=k, v=v, o=o)):
         _check(load_library().moa_prefill(plan.handle, q.data_ptr(), k.data_ptr(), v.data_ptr(),
@@ -331,7 +339,7 @@ def moa_decode(plan: Plan, q, k_cache, v_cache, pos: int, workspace, o=None, str
     _need(k_cache, (bsz, plan.cache_rows, plan.head_dim), dt, "k_cache")
     _need(v_cache, (bsz, plan.cache_rows, plan.head_dim), dt, "v_cache")
     if o is None:
-        o = torch.empty_like(q)
+        o = _new(q.shape, dt, q.device, stream)
     _need(o, q.shape, dt, "o")
     if workspace.device.type != "cuda" or not workspace.is_contiguous():
         raise MoaError(MOA_ERR_WORKSPACE, "workspace must be a contiguous GPU tensor")
@@ -411,7 +419,7 @@ def moa_decode_ragged(plan: Plan, q, k_cache, v_cache, positions, workspace, o=N
     _need(v_cache, (bsz, plan.cache_rows, plan.head_dim), dt, "v_cache")
     _positions(positions, bsz)
     if o is None:
-        o = torch.empty_like(q)
+        o = _new(q.shape, dt, q.device, stream)
     _need(o, q.shape, dt, "o")
     if workspace.device.type != "cuda" or not workspace.is_contiguous():
         raise MoaError(MOA_ERR_WORKSPACE, "workspace must be a contiguous GPU tensor")
@@ -441,7 +449,7 @@ def moa_influence(q, k, v, dout, ebar=None, softmax_scale: float = 0.0, stream=N
         _need(t, shape, torch.bfloat16, name)
     nb = -(-n // 64)
     if ebar is None:
-        ebar = torch.empty((hq, nb, nb), dtype=torch.float32, device=q.device)
+        ebar = _new((hq, nb, nb), torch.float32, q.device, stream)
     _need(ebar, (hq, nb, nb), torch.float32, "ebar")
     desc = moa_desc_t(hq, hkv, d, 0, n, MOA_BF16, float(softmax_scale), 0, 0)
     with torch.cuda.device(_one_device(q=q, k=k, v=v, dout=dout, ebar=ebar)):
@@ -468,8 +476,8 @@ def moa_rule_loss(ebar, n: int, num_sink: int, alpha, beta, flags: int = 0, stre
     if a.shape != b.shape or a.ndim != 1:
         raise MoaError(MOA_ERR_INVALID_ARG, "alpha and beta must be 1-D arrays of the same length")
     r = int(a.shape[0])
-    dl = torch.empty((h, r), dtype=torch.float64, device=ebar.device)
-    dens = torch.empty((r,), dtype=torch.float64, device=ebar.device)
+    dl = _new((h, r), torch.float64, ebar.device, stream)
+    dens = _new((r,), torch.float64, ebar.device, stream)
     with torch.cuda.device(_one_device(ebar=ebar, dl=dl, density=dens)):
         _check(load_library().moa_rule_loss(ebar.data_ptr(), h, int(n), int(num_sink), int(flags),
                                             a.ctypes.data_as(ctypes.POINTER(ctypes.c_double)),
@@ -569,7 +577,7 @@ def moa_paged_append(plan: Plan, k_pages, v_pages, table, q, k_new, v_new, posit
         shape = (n, plan.num_q_heads, plan.head_dim)
         q_stride = _token_stride(q, shape, dt, "q")
         if q_out is None:
-            q_out = torch.empty(shape, dtype=dt, device=q.device)
+            q_out = _new(shape, dt, q.device, stream)
         _need(q_out, shape, dt, "q_out")
         tensors.update(q=q, q_out=q_out)
     elif q_out is not None:
@@ -602,7 +610,7 @@ def _paged_attention(plan, q, k_pages, v_pages, table, positions, workspace, o, 
     pages = _pages(plan, k_pages, v_pages, table, bsz)
     _positions(positions, bsz)
     if o is None:
-        o = torch.empty_like(q)
+        o = _new(q.shape, dt, q.device, stream)
     _need(o, q.shape, dt, "o")
     if workspace.device.type != "cuda" or not workspace.is_contiguous():
         raise MoaError(MOA_ERR_WORKSPACE, "workspace must be a contiguous GPU tensor")
