@@ -294,7 +294,7 @@ moa_status_t moa_rule_loss(const float* ebar, int32_t num_heads, int64_t n, int3
  *
  * The tokens of a call are packed: rows seq_start[b] .. seq_start[b + 1] - 1 of
  * q, k_new, v_new, o and q_out are sequence b's, at positions positions[b],
- * positions[b] + 1, ...; a sequence may have none.  seq_start (device int32
+ * positions[b] + 1, ..., below 2^31; a sequence may have none.  seq_start (device int32
  * [batch + 1]) is non-decreasing; rows in front of seq_start[0] and from
  * seq_start[batch] on belong to no sequence and are left as they were in o and
  * q_out.  A sequence whose rows are not all within [0, n_tokens) has none in
@@ -305,9 +305,14 @@ moa_status_t moa_rule_loss(const float* ebar, int32_t num_heads, int64_t n, int3
  * A query at position p of head g sees the keys j <= p with j < s or in its band,
  * token-exact in the two decode calls and, with MOA_BLOCK_BAND, in blocks in
  * moa_paged_prefill, as in moa_prefill.  A query that sees no key (all its pages
- * are absent) gets zeros.  What lies in rows that no query of the call sees is
- * not looked at; a key or value that is not finite reaches the queries that see
- * its position, and no other.
+ * are absent), or only keys of score minus infinity, gets zeros.  What lies in rows
+ * that no query of the call sees is not looked at; a key or value that is not finite
+ * reaches the queries that see its position, and no other.
+ *
+ * Scores, weights and sums are fp32.  With MOA_BF16 the weights enter the product
+ * with the values rounded to bf16 (each within 2^-8 of itself), as in moa_prefill and
+ * in moa_decode of grouped heads; of single heads they keep 16 bits in
+ * moa_paged_decode, and in moa_paged_decode_shared behind the prefix.
  * ----------------------------------------------------------------------- */
 typedef struct {
   void* k_pages;             /* device [num_pages, page_size, head_dim], the plan's type, 16-byte aligned */
@@ -345,7 +350,9 @@ moa_status_t moa_paged_append(const moa_plan_t* plan, const moa_pages_t* pages, 
 
 /* Bytes of device workspace that any of the three calls below needs for `batch`
  * sequences with n_tokens packed tokens in all (batch of them in the decode
- * calls).  Returns 0 for a NULL plan, batch < 1 or n_tokens < 1. */
+ * calls).  It is what moa_paged_prefill's cut row tiles take (69 MB for bf16 at
+ * head_dim 128, 35 MB for fp32, half at 64) or, for large batches, the decode calls'
+ * partial results.  Returns 0 for a NULL plan, batch < 1 or n_tokens < 1. */
 size_t moa_paged_workspace_bytes(const moa_plan_t* plan, int32_t batch, int64_t n_tokens);
 
 /* Attention of n_tokens packed new tokens over the pages, which already hold them

@@ -113,11 +113,17 @@ constexpr int kPagedMaxWorkers = 4096;   // decode workers (work-groups) per lau
 int launch_paged_append(const PagedAppendArgs& a, int dtype, int head_dim, void* stream);
 constexpr int kPagedLogRowGroups = 9;
 // Work-groups that row tiles are cut for, at most, two per compute unit (twice as many: 6 chunks behind
-// 16,000 keys 262 -> 270 us, fp32, 2 x 16 heads of 64 x 1,501, 69 -> 81).
+// 16,000 keys 258 -> 263 us; fp32, 16 heads of 64, 1,501 tokens of 2 sequences, 69 -> 82).
 constexpr int kPagedRowGroups = 1 << kPagedLogRowGroups;
 // Work-groups over a shared prefix, about, and over the keys behind it: one of each per
-// compute unit (16 x 8 x 4 heads on 8,001 keys and 48 x 8 x 8 on 32,700: 23.1 and 52.5 us; 384
-// for the prefix 27.4 and 59.7, 192 24.2 and 56.3; 512 behind it 25.1 and 57.8).
+// compute unit, whatever the two have to read.  Sequences x KV heads x query heads of each on a
+// prefix, with up to so many keys of their own (us):
+//                                     256 + 256   384 + 256   192 + 256   256 + 512
+//   16 x 8 x 4 on 8,001, 500               22.7        27.2        24.2        24.7
+//   48 x 8 x 8 on 32,700, 1,000            50.8        58.7        55.3        57.1
+//   16 x 32 x 1 on 8,001, 500              39.5        47.2        44.9        45.3
+//   48 x 32 x 1 on 8,001, 1,500             166         172         166         146
+// Most keys of the last are the sequences' own: there more work-groups for them pay.
 constexpr int kPagedPrefixItems = 256;
 MOA_PAGED_FN int paged_tile_rows(int dtype) { return dtype == MOA_BF16 ? 128 : 64; }
 

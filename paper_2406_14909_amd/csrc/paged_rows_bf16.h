@@ -4,9 +4,9 @@
 //
 // Rows are (token, query head) pairs of one KV head, so that a key tile is read once for all
 // the query heads that use it, and a short chunk or a batch of single tokens fills a tile of
-// 128 rows.  What bounds it: in long prompts the matrix units and the board's power (2 x 32
-// heads x 16,384 tokens: 849 us, 890 TFLOP/s, matrix units busy 41 % at 1.8 GHz; 6 chunks of
-// 8 x 4 heads behind 16,000: 259 us, 652 TFLOP/s), memory and the chain of tiles where rows are few.
+// 128 rows.  What bounds it: in long prompts the matrix units and the board's power (32 heads,
+// 16,384 tokens of 2 sequences: 849 us, 890 TFLOP/s, matrix units busy 41 % at 1.8 GHz; 6 chunks of
+// 8 x 4 heads behind up to 16,000: 259 us, 652 TFLOP/s), memory and the chain of tiles where rows are few.
 // Key tiles of few row tiles are cut into pieces for other work-groups (paged_rows.h).
 //
 // One work-group = 4 waves of 32 rows over the same 64-key tiles, which it stages in LDS by
@@ -21,7 +21,8 @@
 //   O^T += V^T P^T: B = P^T straight from the score registers, rounded to bf16, A = V^T by
 //   the transposing LDS read; the keys of a step are permuted alike on both sides.
 // Softmax in base 2, relative to a running maximum that is raised only where a row would see
-// exponents above 2^8; sums in fp32, of the rounded weights.
+// exponents above 2^8; sums in fp32, of the rounded weights.  A weight is rounded to bf16, to within
+// 2^-8 of itself, as in moa_prefill: what is left over would take a second product for V.
 #pragma once
 
 #include <type_traits>

@@ -2,7 +2,7 @@
 // fp32 plans, in tiles of 64 rows.
 //
 // Bound by the fp32 matrix units (32x32x2, a sixteenth of the bf16 rate; 32 heads of 64 x
-// 2,048 tokens behind 333: 192 us, 72 TFLOP/s, matrix units busy 48 %): operands come
+// 2,048 tokens of one sequence behind 333: 192 us, 72 TFLOP/s, matrix units busy 48 %): operands come
 // straight from memory, a tile's keys once per 32 rows.  Two waves share each 32 rows, and
 // all four the rows of a tile that has no more: they take the 32-key tiles of the rows' span
 // in turn and meet in LDS at the end.

@@ -6,8 +6,10 @@
 // launch, as both wait for memory much of the time: work-groups of the one kind and the
 // other alternate, in eights, so that every die and most compute units have both.  All leave
 // partial results, which one merge joins.  48 sequences x 8 heads x 8 query heads over 32,700
-// shared keys and up to 1,000 of their own, 138 MB: 49 us, 43 of them this kernel at 3.4 TB/s,
-// matrix units busy 12 %: row tiles take a piece's key tiles one after the other.
+// shared keys (34 MB of those seen) and up to 1,000 of their own (103 MB): 50 us, 43 of them this
+// kernel at 3.2 TB/s, matrix units busy 12 %.  Either part takes most of it alone: with one key of their
+// own 42 us, as row tiles take a piece's key tiles one after the other; behind a prefix of 64 keys
+// 39, as one work-group per compute unit reads what moa_paged_decode reads with two.
 #include "paged_decode.h"
 #include "paged_rows_bf16.h"
 #include "paged_rows_f32.h"

@@ -63,7 +63,8 @@ struct VisiblePages {
 // Row tiles.
 // ---------------------------------------------------------------------------
 // Keys: what a row tile's start and end cost, about (8 heads x 4 query heads x 5,000 tokens: 239 us
-// with 96, 234 with 192 and 288; fp32, 2 x 16 heads of 64 x 1,501: 69.5, 68.8, 70.4).
+// with 96, 234 with 192 and 288; fp32, 16 heads of 64, 1,501
+// tokens of 2 sequences: 69.6, 69.1, 70.7).
 constexpr int kTileCost = 192;
 
 // A piece costs a start and partial results of 128 rows on their way out and back (67 KB
@@ -71,7 +72,7 @@ constexpr int kTileCost = 192;
 // 8,000: 37, 35, 36 and 47 us in pieces of 128, 256, 512 and 1,024), and a call is cut only
 // where the longest row tile costs kWholeRowCost more than an equal share of all (the same
 // heads, whole and cut: 3,000 tokens 98 and 139 us, 2,048 68 and 87, 1,500 52 and 66; fp32,
-// where a key takes longer, 16 heads of 64 x 1,501 tokens 93 and 73).  With row tiles for most
+// where a key takes longer, 16 heads of 64, 1,501 tokens of 2 sequences 91 and 69).  With row tiles for most
 // work-groups, whose pieces would nearly all be parts, it takes kFullRowCost in bf16 (8 heads x 4
 // query heads, 2,000 tokens behind 1,000 and 2,000, 1,426 and 1,647 more: whole 83 and 104 us, cut
 // 102 and 124; 32 heads, 1,513 and 1,959 more: 108 and 140, cut 106 and 130).

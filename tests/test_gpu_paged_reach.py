@@ -94,3 +94,29 @@ def test_prefill(kind, dt, hq, hkv, windows, positions, counts):
                 _put(c, kind, i, g, p + n - 1, 40, -1.0)     # the last key, in the last piece
                 _put(c, kind, i, g, max(0, p - 20), 77)      # one that all rows see
     _check(c)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv", [(2, 2), (8, 2)])
+@pytest.mark.parametrize("counts,prefix", [(None, 0), (None, 51), ((3, 2), 0)])
+def test_scores_of_minus_infinity(dt, hq, hkv, counts, prefix):
+    """A key of that score weighs nothing; a query with no other gets zeros."""
+    print("[case]", dt, hq, counts, prefix, flush=True)
+    c = Paged(hq, hkv, 64, 0, (1, 5), dt, (50, 60), counts, page=16, prefix_len=prefix, seed=4)
+    heads = c.q[:, :hq // hkv, 7]
+    heads.copy_(heads.abs() + 0.25)                             # those of KV head 0, whose window is 1
+    c.k[_slot(c, 0, 0, 50)][7] = -INF                           # all that sequence 0's first row sees there
+    c.k[_slot(c, 0, 1, 49)][3] = -INF                           # of KV head 1 one of five keys
+    c.q[0, hq // hkv:, 3] = c.q[0, hq // hkv:, 3].abs() + 0.25
+    if counts is not None:
+        c.q[:3, hq // hkv:, 3] = c.q[:3, hq // hkv:, 3].abs() + 0.25
+    got = c.run().double().cpu().numpy()
+    with np.errstate(invalid="ignore"):
+        ref, a, _ = oracle.paged_attention_ref(c.q.double().numpy(), c.k.double().numpy(), c.v.double().numpy(), c.table,
+                                               c.positions, c.seq_start, c.windows, c.s, None, 0, c.prefix_table,
+                                               c.prefix_len)
+    assert np.isnan(ref[0, :hq // hkv]).all() and (got[0, :hq // hkv] == 0.0).all()
+    ref[0, :hq // hkv] = 0.0
+    # fp32: scores are below 50 in magnitude, of 64 terms; see attention_bound, with 2^-8 for bf16's two roundings
+    slack = 8 * 2.0 ** -24 * (12 * 50 + 7) * a + (2.0 ** -8 * (a + 2 * np.abs(ref)) if dt == "bf16" else 2.0 ** -24 * np.abs(ref))
+    assert np.isfinite(ref).all() and (np.abs(got - ref) <= slack)[np.isfinite(a)].all()
