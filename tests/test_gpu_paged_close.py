@@ -81,6 +81,21 @@ def test_a_whole_prompt(dt, n, flags):
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("counts,prefix", [(None, 0), (None, 150), ((130, 1, 40), 0), ((700, 5, 3), 0)])
+def test_tables_made_for_longer_sequences(dt, counts, prefix):
+    """A table is as wide as the longest sequence that a server takes; the split goes by its width, too."""
+    print("[case]", dt, counts, prefix, flush=True)
+    for hq, hkv, d in ((8, 2, 128), (2, 2, 64)):
+        c = Paged(hq, hkv, d, 4, [100, 600], dt, [200, 160, 333], counts, page=16, prefix_len=prefix, seed=7, pad=2 if counts else 0)
+        c.check("narrow")
+        more = 4096 // 16 - c.width
+        odd = np.random.default_rng(1).choice(np.array([-1, 0, c.num_pages, 2 ** 31 - 1]), (len(c.positions), hkv, more))
+        c.table = np.concatenate([c.table, odd.astype(np.int32)], 2)
+        c.prefix_table = np.concatenate([c.prefix_table, odd[0].astype(np.int32)], 1)
+        c.check("wide")                  # whose bound is that of the keys there are
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
 def test_a_prefix_of_no_keys(dt):
     """The same bits as the call without one, and the oracle's values."""
     print("[case]", dt, flush=True)

@@ -67,6 +67,20 @@ def test_decode(kind, dt, hq, hkv, d, windows, prefix):
     _check(c)
 
 
+@pytest.mark.parametrize("kind", ["query nan", "key nan", "value inf"])
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv,d", [(2, 2, 64), (8, 2, 128)])
+def test_shared_prefix(kind, dt, hq, hkv, d):
+    """In the part that is read once for all: it reaches the sequences whose windows go back to it."""
+    print("[case]", kind, dt, hq, hkv, d, flush=True)
+    where = (3100, 3030, -1, 3003, 2999, 1500)                  # the last two: at the prefix's end, and inside it
+    c = Paged(hq, hkv, d, 3, (60, 2500), dt, where, page=32, prefix_len=3000, seed=5)
+    _put(c, kind, 3, 0, 2960, 5)
+    _put(c, kind, 0, 1, 2999, 9, -1.0)
+    _put(c, kind, 1, 1, 1, 11)                                  # a sink
+    _check(c)
+
+
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
 @pytest.mark.parametrize("hq", [1, 8])
 def test_decode_of_one_key(dt, hq):
