@@ -7,12 +7,12 @@ Kinds of cases:
              back to the free list, new tokens get pages, and each token's row
              per head is written down (``moa_paged_assign``).
 ``append``   new tokens enter the pages: queries and keys are rotated by their
-             positions, keys and values stored in 8 bits (``moa_paged8_append``).
+             positions, keys and values stored in 8 bits (``moa_quant_append``).
 ``prefill``  ragged chunks of new tokens attend to all that their sequences'
-             pages hold (``moa_paged8_prefill``).
-``decode``   one token per sequence (``moa_paged8_decode``).
+             pages hold (``moa_quant_prefill``).
+``decode``   one token per sequence (``moa_quant_decode``).
 ``shared``   the same for a batch whose sequences begin with one long prefix,
-             which is read once for all (``moa_paged8_decode_shared``).
+             which is read once for all (``moa_quant_decode_shared``).
 
 A page holds ``page`` consecutive positions of one KV head; ``table[b, g, i]`` is the
 page of positions ``i * page ..`` of head g of sequence b, negative where there is
@@ -428,16 +428,16 @@ def _run_own(x):
         return {"table": x["table"], "free": x["free"], "counts": x["counts"], "slots": x["slots"]}
     cache = (x["k_pages"], x["v_pages"], x["scales"])
     if kind == "append":
-        q = moa.moa_paged8_append(plan, *cache, x["table"], x["q"], x["k_new"], x["v_new"], x["positions"],
+        q = moa.moa_quant_append(plan, *cache, x["table"], x["q"], x["k_new"], x["v_new"], x["positions"],
                                   x["seq_start"], x["inv_freq"], case["interleaved"], q_out=x["out"])
         return {"q": q, "k_pages": cache[0], "v_pages": cache[1], "scales": cache[2]}
     if kind == "prefill":
-        o = moa.moa_paged8_prefill(plan, x["q"], *cache, x["table"], x["positions"], x["seq_start"], x["workspace"],
+        o = moa.moa_quant_prefill(plan, x["q"], *cache, x["table"], x["positions"], x["seq_start"], x["workspace"],
                                    o=x["out"])
     elif kind == "decode":
-        o = moa.moa_paged8_decode(plan, x["q"], *cache, x["table"], x["positions"], x["workspace"], o=x["out"])
+        o = moa.moa_quant_decode(plan, x["q"], *cache, x["table"], x["positions"], x["workspace"], o=x["out"])
     else:
-        o = moa.moa_paged8_decode_shared(plan, x["q"], *cache, x["prefix_table"], case["prefix"], x["table"],
+        o = moa.moa_quant_decode_shared(plan, x["q"], *cache, x["prefix_table"], case["prefix"], x["table"],
                                          x["positions"], x["workspace"], o=x["out"])
     return {"o": o}
 
