@@ -37,6 +37,14 @@
  *                  narrow window gives back what it no longer sees, prompts
  *                  enter in chunks of any length, and sequences share the
  *                  pages of a common prefix.
+ *   moa_paged_assign
+ *                  the page tables of that cache kept on the device: pages that
+ *                  no later query sees go back to a free list, new tokens get
+ *                  pages from it.
+ *   moa_quant_append, moa_quant_prefill, moa_quant_decode,
+ *   moa_quant_decode_shared
+ *                  the paged cache in 8 bits per element, with a scale for every
+ *                  16 positions of a head, and the same attention over it.
  *
  * Definitions used throughout (s = num_sink, w_g = window of KV head g):
  *   window    w_g = min(max(floor(alpha_g + beta_g * N), 1), N), evaluated
@@ -378,6 +386,93 @@ moa_status_t moa_paged_decode(const moa_plan_t* plan, const moa_pages_t* pages, 
  * table, whose entries in front of that page are not looked at.  A page across the
  * border is looked up in both.  0 <= prefix_len <= max_pages * page_size. */
 moa_status_t moa_paged_decode_shared(const moa_plan_t* plan, const moa_pages_t* pages, const int32_t* prefix_table,
+                                     int64_t prefix_len, const void* q, void* o, const int32_t* positions,
+                                     int32_t batch, void* workspace, size_t ws_bytes, void* hip_stream);
+
+/* --------------------------------------------------------------------------
+ * Page tables on the device.
+ * ----------------------------------------------------------------------- */
+typedef struct {
+  int32_t* table;            /* device [batch, num_kv_heads, max_pages]: page numbers, or an absent page (-1 in new tables) */
+  int32_t* free_pages;       /* device [num_pages]: the first counts[0] are the free pages, the last of them given out first */
+  int32_t* counts;           /* device [2]: free pages; pages that the last call lacked */
+  int64_t num_pages;         /* >= 1; num_pages * page_size <= 2^31 */
+  int32_t page_size;         /* 16, 32, 64, 128 or 256 */
+  int32_t max_pages;         /* pages per (sequence, head) in the table; max_pages * page_size <= 2^30 */
+} moa_page_tables_t;
+
+/* Brings the tables up to a call of the paged attention, in two steps.
+ *  1. Pages go back to the free list, behind the others, in the order of the table
+ *     (sequence, head, entry): all pages of a sequence b with fresh[b] != 0 (it ended, and
+ *     what stands in its place starts anew), and of the others, where positions[b] >= 0, the
+ *     entries wholly at positions >= num_sink and in front of the band of positions[b], which
+ *     no query at positions[b] or later sees (with MOA_BLOCK_BAND the band in blocks as well as
+ *     the token-exact one).  Their entries become -1.
+ *  2. Absent entries of the positions of new tokens get pages, in the order of the table:
+ *     each the last page of the free list.  Where the list runs out the remaining ones
+ *     stay absent (moa_paged_append does not store their tokens), counts[0] is 0 and counts[1] the
+ *     number of pages lacked, otherwise counts[1] is 0.
+ * positions and seq_start are as in moa_paged_append (seq_start NULL: one token per
+ * sequence); a negative positions[b] has no new tokens, nor has a sequence whose rows are
+ * not all within [0, n_tokens).  fresh (device int32 [batch]) may be NULL: none.
+ * slots (device int32 [n_tokens, num_kv_heads], or NULL): the row of the pool of each new token
+ * and head, page * page_size + row in the page, or -1 where its page is absent; rows of no sequence are
+ * left as they were.
+ * A page may stand in one entry only: pages of a shared prefix belong in prefix tables
+ * (moa_paged_decode_shared), which this call does not touch.  The workspace is as in
+ * the attention calls (moa_paged_workspace_bytes).  The result does not depend on the
+ * launch order.  1 <= batch <= 65535, 0 <= n_tokens < 2^30. */
+moa_status_t moa_paged_assign(const moa_plan_t* plan, const moa_page_tables_t* tables, const int32_t* positions,
+                              const int32_t* seq_start, const int32_t* fresh, int32_t* slots, int32_t batch,
+                              int64_t n_tokens, void* workspace, size_t ws_bytes, void* hip_stream);
+
+/* --------------------------------------------------------------------------
+ * Paged cache in 8 bits.
+ *
+ * The paged cache with keys and values as e4m3 numbers (OCP 8-bit floating point: 4 exponent and
+ * 3 mantissa bits, largest 448, no infinities) times a scale of their block of 16
+ * positions: half the memory, and half of what a decode call reads.  Tables,
+ * packed tokens, masks, workspaces and the treatment of what no query sees are those of the paged
+ * cache; plans are MOA_BF16 ones.  Products and sums are as there: the 8-bit numbers times
+ * their scales are bf16 numbers, without rounding.
+ *
+ * A scale is a power of two 2^e, -117 <= e <= 119: the exponent bits of the stored fp32
+ * are read and nothing else.  A block stores x as the e4m3 number nearest to x / 2^e (ties to
+ * even), so that x is kept to within 2^-4 of itself, or 2^(e - 10); what is past 448 * 2^119 in
+ * magnitude is stored as that, and what is not finite as NaN.
+ * ----------------------------------------------------------------------- */
+#define MOA_QUANT_BLOCK 16
+typedef struct {
+  void* k_pages;             /* device [num_pages, page_size, head_dim], e4m3, 16-byte aligned */
+  void* v_pages;
+  float* scales;             /* device [num_pages, page_size / 16, 2]: of the keys and the values of each block; 8-byte aligned */
+  const int32_t* table;      /* device [batch, num_kv_heads, max_pages] */
+  int64_t num_pages;         /* >= 1; num_pages * page_size <= 2^31 */
+  int32_t page_size;         /* 16, 32, 64, 128 or 256 */
+  int32_t max_pages;         /* pages per (sequence, head) in the table; max_pages * page_size <= 2^30 */
+} moa_quant_pages_t;
+
+/* moa_paged_append into an 8-bit cache.  A block whose first position is among the new
+ * tokens gets the smallest scale that keeps the largest finite magnitude of its new tokens (keys:
+ * after rotation, in fp32) within 448.  Of a block that is entered behind its first position, the
+ * scale is the larger of that and the stored one, and where it grows the rows in front of the
+ * new tokens are rounded once more, to the new scale.  Rows behind the new tokens of a block
+ * mean nothing afterwards.  Two sequences of one append must not write to the same block.
+ * Values, keys and queries are otherwise as in moa_paged_append; q_out is bf16. */
+moa_status_t moa_quant_append(const moa_plan_t* plan, const moa_quant_pages_t* pages, const void* q, int64_t q_stride,
+                              const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, void* q_out,
+                              const moa_rope_t* rope, const int32_t* positions, const int32_t* seq_start,
+                              int32_t batch, int64_t n_tokens, void* hip_stream);
+
+/* moa_paged_prefill, moa_paged_decode and moa_paged_decode_shared over an 8-bit cache;
+ * workspaces are those of moa_paged_workspace_bytes. */
+moa_status_t moa_quant_prefill(const moa_plan_t* plan, const moa_quant_pages_t* pages, const void* q, void* o,
+                               const int32_t* positions, const int32_t* seq_start, int32_t batch, int64_t n_tokens,
+                               void* workspace, size_t ws_bytes, void* hip_stream);
+moa_status_t moa_quant_decode(const moa_plan_t* plan, const moa_quant_pages_t* pages, const void* q, void* o,
+                              const int32_t* positions, int32_t batch, void* workspace, size_t ws_bytes,
+                              void* hip_stream);
+moa_status_t moa_quant_decode_shared(const moa_plan_t* plan, const moa_quant_pages_t* pages, const int32_t* prefix_table,
                                      int64_t prefix_len, const void* q, void* o, const int32_t* positions,
                                      int32_t batch, void* workspace, size_t ws_bytes, void* hip_stream);
 

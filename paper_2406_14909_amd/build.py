@@ -26,7 +26,8 @@ BINDING_PATH = os.path.join(PKG_DIR, "_binding.so")
 PROBES = ["stream_read", "mfma_loop"]
 
 HIP_SOURCES = ["kv_append.hip", "decode.hip", "prefill.hip", "prefill_f32.hip", "influence.hip", "rule_loss.hip",
-               "paged_append.hip", "paged_decode.hip", "paged_prefill.hip", "paged_shared.hip", "paged_merge.hip"]
+               "paged_append.hip", "paged_decode.hip", "paged_prefill.hip", "paged_shared.hip", "paged_merge.hip",
+               "paged_assign.hip", "quant_append.hip", "quant_prefill.hip", "quant_decode.hip", "quant_shared.hip"]
 HOST_SOURCES = ["moa_api.cpp", "paged_api.cpp"]
 
 ARCH = "gfx950"

@@ -44,6 +44,11 @@ struct Api {
   decltype(&moa_paged_prefill) paged_prefill;
   decltype(&moa_paged_decode) paged_decode;
   decltype(&moa_paged_decode_shared) paged_decode_shared;
+  decltype(&moa_paged_assign) paged_assign;
+  decltype(&moa_quant_append) quant_append;
+  decltype(&moa_quant_prefill) quant_prefill;
+  decltype(&moa_quant_decode) quant_decode;
+  decltype(&moa_quant_decode_shared) quant_decode_shared;
 };
 
 // What the checks need of a library and a plan; held by a capsule.
@@ -383,88 +388,108 @@ PyObject* rule_loss(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   MOA_LEAVE
 }
 
-// k_pages, v_pages and table of a paged call of `bsz` sequences.
-moa_pages_t pages_of(const Bound& b, Check& c, PyObject* kp, PyObject* vp, PyObject* table, int64_t bsz) {
+// k_pages, v_pages and table of a paged call of `bsz` sequences: of the plan's type, or, with scales, in 8 bits.
+struct Pages {
   moa_pages_t p = {};
+  float* scales = nullptr;
+  moa_quant_pages_t quant() const {
+    return {p.k_pages, p.v_pages, scales, p.table, p.num_pages, p.page_size, p.max_pages};
+  }
+};
+Pages pages_of(const Bound& b, Check& c, PyObject* kp, PyObject* vp, PyObject* sc, PyObject* table, int64_t bsz) {
+  Pages r;
+  moa_pages_t& p = r.p;
   const at::Tensor* k = c.any(kp);
   const at::Tensor* t = c.any(table);
   if (!b.plan || !k || !t || k->dim() != 3 || t->dim() != 3) {
     c.ok = false;
-    return p;
+    return r;
   }
   const int64_t np = k->size(0), ps = k->size(1), mp = t->size(2);
-  c(kp, b.dtype, {np, ps, b.d});
-  const at::Tensor* v = c(vp, b.dtype, {np, ps, b.d});
+  const at::ScalarType type = sc ? at::kFloat8_e4m3fn : b.dtype;
+  c(kp, type, {np, ps, b.d});
+  const at::Tensor* v = c(vp, type, {np, ps, b.d});
+  const at::Tensor* s = sc ? c(sc, at::kFloat, {np, ps / MOA_QUANT_BLOCK, 2}) : nullptr;
   c(table, at::kInt, {bsz, b.hkv, mp});
   if (!c.ok || ps > INT32_MAX || mp > INT32_MAX || bsz > INT32_MAX) {
     c.ok = false;
-    return p;
+    return r;
   }
   p.k_pages = k->data_ptr();
   p.v_pages = v->data_ptr();
+  if (s) r.scales = static_cast<float*>(s->data_ptr());
   p.table = static_cast<const int32_t*>(t->data_ptr());
   p.num_pages = np;
   p.page_size = static_cast<int32_t>(ps);
   p.max_pages = static_cast<int32_t>(mp);
-  return p;
+  return r;
 }
 
-// paged_append(bound, k_pages, v_pages, table, q, k_new, v_new, positions, seq_start, inv_freq, interleaved, q_out)
-PyObject* paged_append(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
-  MOA_ENTER(12)
-  const at::Tensor* at_ = c.any(args[7]);
-  const at::Tensor* k0 = plain(args[5]);
-  if (!b->plan || !at_ || at_->dim() != 1 || !k0 || k0->dim() != 3 || !PyBool_Check(args[10])) return none();
+// (bound, k_pages, v_pages, [scales,] table, q, k_new, v_new, positions, seq_start, inv_freq, interleaved, q_out)
+template <bool kQuant>
+PyObject* append(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  MOA_ENTER(kQuant ? 13 : 12)
+  PyObject* const sc = kQuant ? args[3] : nullptr;
+  PyObject* const* a = args + (kQuant ? 4 : 3);           // from the table on
+  const at::Tensor* at_ = c.any(a[4]);
+  const at::Tensor* k0 = plain(a[2]);
+  if (!b->plan || !at_ || at_->dim() != 1 || !k0 || k0->dim() != 3 || !PyBool_Check(a[7])) return none();
   const int64_t bsz = at_->size(0), n = k0->size(0);
-  c(args[7], at::kInt, {bsz});
-  const moa_pages_t pages = pages_of(*b, c, args[1], args[2], args[3], bsz);
+  c(a[4], at::kInt, {bsz});
+  const Pages pages = pages_of(*b, c, args[1], args[2], sc, a[0], bsz);
   int64_t qs = 0, ks = 0, vs = 0;
-  const at::Tensor* k = c.tokens(args[5], b->dtype, {n, b->hkv, b->d}, &ks);
-  const at::Tensor* v = c.tokens(args[6], b->dtype, {n, b->hkv, b->d}, &vs);
-  const bool with_q = args[4] != Py_None;
-  const at::Tensor* q = with_q ? c.tokens(args[4], b->dtype, {n, b->hq, b->d}, &qs) : nullptr;
-  const at::Tensor* ss = args[8] != Py_None ? c(args[8], at::kInt, {bsz + 1}) : nullptr;
-  const at::Tensor* f = args[9] != Py_None ? c.any(args[9]) : nullptr;
+  const at::Tensor* k = c.tokens(a[2], b->dtype, {n, b->hkv, b->d}, &ks);
+  const at::Tensor* v = c.tokens(a[3], b->dtype, {n, b->hkv, b->d}, &vs);
+  const bool with_q = a[1] != Py_None;
+  const at::Tensor* q = with_q ? c.tokens(a[1], b->dtype, {n, b->hq, b->d}, &qs) : nullptr;
+  const at::Tensor* ss = a[5] != Py_None ? c(a[5], at::kInt, {bsz + 1}) : nullptr;
+  const at::Tensor* f = a[6] != Py_None ? c.any(a[6]) : nullptr;
   if (!c.done() || (f && (f->dim() != 1 || f->scalar_type() != at::kFloat || f->size(0) > INT32_MAX / 2)))
     return none();
   at::Tensor fresh;
   const at::Tensor* out = &fresh;
   if (!with_q) {
-    if (args[11] != Py_None) return none();
-  } else if (args[11] == Py_None) {
+    if (a[8] != Py_None) return none();
+  } else if (a[8] == Py_None) {
     fresh = at::empty({n, b->hq, b->d}, q->options());
   } else {
-    out = c(args[11], b->dtype, {n, b->hq, b->d});
+    out = c(a[8], b->dtype, {n, b->hq, b->d});
   }
   if (!c.done()) return none();
   moa_rope_t rope = {};
   if (f) {
     rope.inv_freq = static_cast<const float*>(f->data_ptr());
     rope.rotary_dim = static_cast<int32_t>(2 * f->size(0));
-    rope.interleaved = args[10] == Py_True;
+    rope.interleaved = a[7] == Py_True;
   }
   void *pq = with_q ? q->data_ptr() : nullptr, *po = with_q ? out->data_ptr() : nullptr;
   void *pk = k->data_ptr(), *pv = v->data_ptr(), *s = c.stream();
   const int32_t* pp = static_cast<const int32_t*>(at_->data_ptr());
   const int32_t* ps = ss ? static_cast<const int32_t*>(ss->data_ptr()) : nullptr;
+  const moa_quant_pages_t quant = pages.quant();
   if (!call(*b, [&] {
-        return b->api.paged_append(b->plan, &pages, pq, qs, pk, ks, pv, vs, po, f ? &rope : nullptr, pp, ps,
-                                   static_cast<int32_t>(bsz), n, s);
+        const int32_t batch = static_cast<int32_t>(bsz);
+        if constexpr (kQuant)
+          return b->api.quant_append(b->plan, &quant, pq, qs, pk, ks, pv, vs, po, f ? &rope : nullptr, pp, ps, batch, n, s);
+        else
+          return b->api.paged_append(b->plan, &pages.p, pq, qs, pk, ks, pv, vs, po, f ? &rope : nullptr, pp, ps, batch, n, s);
       }))
     return nullptr;
   if (!with_q) Py_RETURN_TRUE;
-  return args[11] == Py_None ? THPVariable_Wrap(fresh) : same(args[11]);
+  return a[8] == Py_None ? THPVariable_Wrap(fresh) : same(a[8]);
   MOA_LEAVE
 }
+constexpr auto paged_append = append<false>, quant_append = append<true>;
 
 // q, pages, positions, workspace and o of a paged attention call
 struct PagedTensors {
   const at::Tensor *q, *ps = nullptr, *w = nullptr;
-  moa_pages_t pages = {};
+  Pages pages;
+  moa_quant_pages_t quant = {};
   int64_t n = 0, bsz = 0;
   // one_each: one token per sequence
-  PagedTensors(const Bound& b, Check& c, PyObject* oq, PyObject* kp, PyObject* vp, PyObject* table, PyObject* pos,
-               PyObject* work, bool one_each)
+  PagedTensors(const Bound& b, Check& c, PyObject* oq, PyObject* kp, PyObject* vp, PyObject* sc, PyObject* table,
+               PyObject* pos, PyObject* work, bool one_each)
       : q(c.any(oq)) {
     ps = c.any(pos);
     if (!b.plan || !q || !ps || q->dim() != 3 || ps->dim() != 1) {
@@ -475,64 +500,119 @@ struct PagedTensors {
     bsz = ps->size(0);
     c(oq, b.dtype, {one_each ? bsz : n, b.hq, b.d});
     c(pos, at::kInt, {bsz});
-    pages = pages_of(b, c, kp, vp, table, bsz);
+    pages = pages_of(b, c, kp, vp, sc, table, bsz);
+    quant = pages.quant();
     w = c.any(work);
   }
   const int32_t* positions() const { return static_cast<const int32_t*>(ps->data_ptr()); }
 };
 
-// paged_prefill(bound, q, k_pages, v_pages, table, positions, seq_start, workspace, o)
-PyObject* paged_prefill(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
-  MOA_ENTER(9)
-  const PagedTensors t(*b, c, args[1], args[2], args[3], args[4], args[5], args[7], false);
-  const at::Tensor* ss = c(args[6], at::kInt, {t.bsz + 1});
-  Out o(args[8], t.q, c);
+// (bound, q, k_pages, v_pages, [scales,] table, positions, seq_start, workspace, o)
+template <bool kQuant>
+PyObject* packed_prefill(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  MOA_ENTER(kQuant ? 10 : 9)
+  PyObject* const* a = args + (kQuant ? 5 : 4);           // from the table on
+  const PagedTensors t(*b, c, args[1], args[2], args[3], kQuant ? args[4] : nullptr, a[0], a[1], a[3], false);
+  const at::Tensor* ss = c(a[2], at::kInt, {t.bsz + 1});
+  Out o(a[4], t.q, c);
   if (!c.done() || !o.t) return none();
   void *pq = t.q->data_ptr(), *po = o.t->data_ptr(), *pw = t.w->data_ptr(), *s = c.stream();
   const int32_t* ps = static_cast<const int32_t*>(ss->data_ptr());
   const size_t nw = t.w->nbytes();
   if (!call(*b, [&] {
-        return b->api.paged_prefill(b->plan, &t.pages, pq, po, t.positions(), ps, static_cast<int32_t>(t.bsz), t.n, pw, nw, s);
+        const int32_t batch = static_cast<int32_t>(t.bsz);
+        if constexpr (kQuant)
+          return b->api.quant_prefill(b->plan, &t.quant, pq, po, t.positions(), ps, batch, t.n, pw, nw, s);
+        else
+          return b->api.paged_prefill(b->plan, &t.pages.p, pq, po, t.positions(), ps, batch, t.n, pw, nw, s);
       }))
     return nullptr;
   return o.answer();
   MOA_LEAVE
 }
+constexpr auto paged_prefill = packed_prefill<false>, quant_prefill = packed_prefill<true>;
 
-// paged_decode(bound, q, k_pages, v_pages, table, positions, workspace, o)
-PyObject* paged_decode(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
-  MOA_ENTER(8)
-  const PagedTensors t(*b, c, args[1], args[2], args[3], args[4], args[5], args[6], true);
-  Out o(args[7], t.q, c);
+// (bound, q, k_pages, v_pages, [scales,] table, positions, workspace, o)
+template <bool kQuant>
+PyObject* pages_decode(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  MOA_ENTER(kQuant ? 9 : 8)
+  PyObject* const* a = args + (kQuant ? 5 : 4);           // from the table on
+  const PagedTensors t(*b, c, args[1], args[2], args[3], kQuant ? args[4] : nullptr, a[0], a[1], a[2], true);
+  Out o(a[3], t.q, c);
   if (!c.done() || !o.t) return none();
   void *pq = t.q->data_ptr(), *po = o.t->data_ptr(), *pw = t.w->data_ptr(), *s = c.stream();
   const size_t nw = t.w->nbytes();
   if (!call(*b, [&] {
-        return b->api.paged_decode(b->plan, &t.pages, pq, po, t.positions(), static_cast<int32_t>(t.bsz), pw, nw, s);
+        const int32_t batch = static_cast<int32_t>(t.bsz);
+        if constexpr (kQuant) return b->api.quant_decode(b->plan, &t.quant, pq, po, t.positions(), batch, pw, nw, s);
+        else return b->api.paged_decode(b->plan, &t.pages.p, pq, po, t.positions(), batch, pw, nw, s);
       }))
     return nullptr;
   return o.answer();
   MOA_LEAVE
 }
+constexpr auto paged_decode = pages_decode<false>, quant_decode = pages_decode<true>;
 
-// paged_decode_shared(bound, q, k_pages, v_pages, prefix_table, prefix_len, table, positions, workspace, o)
-PyObject* paged_decode_shared(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
-  MOA_ENTER(10)
+// (bound, q, k_pages, v_pages, [scales,] prefix_table, prefix_len, table, positions, workspace, o)
+template <bool kQuant>
+PyObject* pages_decode_shared(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  MOA_ENTER(kQuant ? 11 : 10)
+  PyObject* const* a = args + (kQuant ? 5 : 4);           // from the prefix's table on
   int64_t len;
-  if (!as_int(args[5], &len)) return none();
-  const PagedTensors t(*b, c, args[1], args[2], args[3], args[6], args[7], args[8], true);
-  const at::Tensor* pre = c(args[4], at::kInt, {b->hkv, int64_t(t.pages.max_pages)});
-  Out o(args[9], t.q, c);
+  if (!as_int(a[1], &len)) return none();
+  const PagedTensors t(*b, c, args[1], args[2], args[3], kQuant ? args[4] : nullptr, a[2], a[3], a[4], true);
+  const at::Tensor* pre = c(a[0], at::kInt, {b->hkv, int64_t(t.pages.p.max_pages)});
+  Out o(a[5], t.q, c);
   if (!c.done() || !o.t) return none();
   void *pq = t.q->data_ptr(), *po = o.t->data_ptr(), *pw = t.w->data_ptr(), *s = c.stream();
   const int32_t* pp = static_cast<const int32_t*>(pre->data_ptr());
   const size_t nw = t.w->nbytes();
   if (!call(*b, [&] {
-        return b->api.paged_decode_shared(b->plan, &t.pages, pp, len, pq, po, t.positions(), static_cast<int32_t>(t.bsz), pw,
-                                          nw, s);
+        const int32_t batch = static_cast<int32_t>(t.bsz);
+        if constexpr (kQuant)
+          return b->api.quant_decode_shared(b->plan, &t.quant, pp, len, pq, po, t.positions(), batch, pw, nw, s);
+        else
+          return b->api.paged_decode_shared(b->plan, &t.pages.p, pp, len, pq, po, t.positions(), batch, pw, nw, s);
       }))
     return nullptr;
   return o.answer();
+  MOA_LEAVE
+}
+constexpr auto paged_decode_shared = pages_decode_shared<false>, quant_decode_shared = pages_decode_shared<true>;
+
+// paged_assign(bound, table, free_pages, counts, page_size, positions, workspace, seq_start, fresh, slots)
+PyObject* paged_assign(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  MOA_ENTER(10)
+  int64_t page;
+  const at::Tensor* t = c.any(args[1]);
+  const at::Tensor* f = c.any(args[2]);
+  const at::Tensor* ps = c.any(args[5]);
+  if (!b->plan || !t || !f || !ps || t->dim() != 3 || f->dim() != 1 || ps->dim() != 1 || !as_int(args[4], &page) ||
+      page < 0 || page > INT32_MAX)
+    return none();
+  const int64_t bsz = ps->size(0), mp = t->size(2);
+  c(args[1], at::kInt, {bsz, b->hkv, mp});
+  c(args[2], at::kInt, {f->size(0)});
+  const at::Tensor* n2 = c(args[3], at::kInt, {2});
+  c(args[5], at::kInt, {bsz});
+  const at::Tensor* w = c.any(args[6]);
+  const at::Tensor* ss = args[7] != Py_None ? c(args[7], at::kInt, {bsz + 1}) : nullptr;
+  const at::Tensor* fr = args[8] != Py_None ? c(args[8], at::kInt, {bsz}) : nullptr;
+  const at::Tensor* sl = args[9] != Py_None ? c.any(args[9]) : nullptr;
+  if (sl && (sl->dim() != 2 || sl->scalar_type() != at::kInt || sl->size(1) != b->hkv)) return none();
+  if (!c.done() || bsz > INT32_MAX || mp > INT32_MAX) return none();
+  auto at_ = [](const at::Tensor* x) { return x ? static_cast<int32_t*>(x->data_ptr()) : nullptr; };
+  const moa_page_tables_t tables = {at_(t), at_(f), at_(n2), f->size(0), static_cast<int32_t>(page), static_cast<int32_t>(mp)};
+  const int64_t n = sl ? sl->size(0) : (int64_t(1) << 30) - 1;
+  void *pw = w->data_ptr(), *s = c.stream();
+  const size_t nw = w->nbytes();
+  const int32_t *pp = at_(ps), *pss = at_(ss), *pf = at_(fr);
+  int32_t* psl = at_(sl);
+  if (!call(*b, [&] {
+        return b->api.paged_assign(b->plan, &tables, pp, pss, pf, psl, static_cast<int32_t>(bsz), n, pw, nw, s);
+      }))
+    return nullptr;
+  Py_RETURN_TRUE;
   MOA_LEAVE
 }
 
@@ -577,7 +657,8 @@ PyObject* bind(PyObject*, PyObject* args) {
 PyMethodDef kMethods[] = {
     MOA_FAST(prefill), MOA_FAST(kv_append), MOA_FAST(kv_append_ragged), MOA_FAST(decode), MOA_FAST(decode_noalloc),
     MOA_FAST(decode_ragged), MOA_FAST(influence), MOA_FAST(rule_loss), MOA_FAST(paged_append), MOA_FAST(paged_prefill),
-    MOA_FAST(paged_decode), MOA_FAST(paged_decode_shared), {"bind", bind, METH_VARARGS, nullptr},
+    MOA_FAST(paged_decode), MOA_FAST(paged_decode_shared), MOA_FAST(paged_assign), MOA_FAST(quant_append),
+    MOA_FAST(quant_prefill), MOA_FAST(quant_decode), MOA_FAST(quant_decode_shared), {"bind", bind, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

@@ -21,6 +21,7 @@ constexpr int kMinPageShift = 4;         // 16 positions: the rows that a wave o
 constexpr int kMaxPageShift = 8;
 constexpr int64_t kMaxPosition = int64_t(1) << 30;
 constexpr int64_t kMaxPageRows = int64_t(1) << 31;   // rows of a page pool
+constexpr int kQuantBlock = MOA_QUANT_BLOCK;         // positions of one scale; a page holds whole blocks
 
 // New tokens into the pages, rotated on the way.
 struct PagedAppendArgs {
@@ -46,6 +47,33 @@ struct PagedAppendArgs {
   int32_t max_pages;
   int32_t rotary;            // 0: nothing is rotated
   int32_t interleaved;
+};
+
+// The same into an 8-bit cache.
+struct QuantAppendArgs {
+  PagedAppendArgs a;
+  float* scales;             // [num_pages * page_size / 16][2]: of keys, of values
+};
+
+// Page tables from lengths.
+struct AssignArgs {
+  int32_t* table;            // [batch, hkv, max_pages]
+  int32_t* free_pages;       // [num_pages]
+  int32_t* counts;           // [2]: free pages, pages lacked
+  const int32_t* positions;
+  const int32_t* seq_start;  // null: one token per sequence
+  const int32_t* fresh;      // null: none
+  int32_t* slots;            // [n_tokens, hkv], or null
+  int64_t* plan;             // workspace: the list's length before step 2, then per pair the pages in front of its own
+  int32_t n_tokens;
+  int32_t batch;
+  int32_t hkv;
+  int32_t num_pages;
+  int32_t page_shift;
+  int32_t max_pages;
+  int32_t num_sink;
+  int32_t block_band;        // the band in blocks counts too
+  int32_t window[MOA_MAX_KV_HEADS];
 };
 
 // Attention over the pages.
@@ -84,6 +112,7 @@ struct PagedArgs {
   int32_t window_in_order[MOA_MAX_KV_HEADS];   // and the same, widest first,
   int16_t kv_order[MOA_MAX_KV_HEADS];          // of these KV heads
   int32_t prefix_piece[MOA_MAX_KV_HEADS + 1];  // first piece of each head's keys of a shared prefix
+  const float* scales;           // 8-bit pages: of keys and values of every 16 rows of the pool; null: pages of the plan's type
 };
 
 // Keys of one query position, as a run of sinks and a band behind them, both cut at
@@ -132,5 +161,12 @@ int launch_paged_rows(const PagedArgs& a, int dtype, int head_dim, int key_group
 int launch_paged_merge(const PagedArgs& a, int dtype, int head_dim, void* stream);
 int launch_paged_shared(const PagedArgs& a, int dtype, int head_dim, int group, void* stream);
 int launch_paged_decode(const PagedArgs& a, int dtype, int head_dim, int group, void* stream);
+
+int launch_paged_assign(const AssignArgs& a, void* stream);
+// 8-bit pages, bf16 queries and outputs.
+int launch_quant_append(const QuantAppendArgs& a, int head_dim, void* stream);
+int launch_quant_rows(const PagedArgs& a, int head_dim, int key_groups, int64_t groups, void* stream);
+int launch_quant_shared(const PagedArgs& a, int head_dim, int group, void* stream);
+int launch_quant_decode(const PagedArgs& a, int head_dim, int group, void* stream);
 
 }  // namespace moa

@@ -19,31 +19,71 @@ moa_status_t invalid(const char* who, const char* what) {
 
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
-size_t pool_bytes(const moa_plan_s& p, const moa_pages_t& pages) {
-  return elem_size(p) * static_cast<size_t>(pages.num_pages) * pages.page_size * p.desc.head_dim;
+bool aligned8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
+
+// Pages of either kind: of the plan's type, or in 8 bits with scales.
+struct Pool : moa_pages_t {
+  bool quant;
+  float* scales;
+};
+const Pool* pool_of(const moa_pages_t* pages, Pool* pool) {
+  if (!pages) return nullptr;
+  static_cast<moa_pages_t&>(*pool) = *pages;
+  pool->quant = false;
+  pool->scales = nullptr;
+  return pool;
+}
+const Pool* pool_of(const moa_quant_pages_t* pages, Pool* pool) {
+  if (!pages) return nullptr;
+  static_cast<moa_pages_t&>(*pool) = {pages->k_pages, pages->v_pages, pages->table, pages->num_pages, pages->page_size,
+                                      pages->max_pages};
+  pool->quant = true;
+  pool->scales = pages->scales;
+  return pool;
+}
+
+size_t pool_bytes(const moa_plan_s& p, const Pool& pages) {
+  return (pages.quant ? 1 : elem_size(p)) * static_cast<size_t>(pages.num_pages) * pages.page_size * p.desc.head_dim;
+}
+
+size_t scale_bytes(const Pool& pages) {
+  return pages.quant ? sizeof(float) * 2 * static_cast<size_t>(pages.num_pages) * (pages.page_size / kQuantBlock) : 0;
 }
 
 size_t rows_bytes(const moa_plan_s& p, int64_t n, int heads) {
   return elem_size(p) * static_cast<size_t>(n) * heads * p.desc.head_dim;
 }
 
-moa_status_t check_pages(const char* who, const moa_plan_t* plan, const moa_pages_t* pages, const int32_t* positions,
+moa_status_t check_sizes(const char* who, int32_t ps, int64_t num_pages, int32_t max_pages, int32_t batch,
+                         int64_t n_tokens) {
+  if (ps < (1 << kMinPageShift) || ps > (1 << kMaxPageShift) || (ps & (ps - 1)) != 0)
+    return fail(MOA_ERR_UNSUPPORTED, std::string(who) + ": page_size must be 16, 32, 64, 128 or 256");
+  if (num_pages < 1 || num_pages > kMaxPageRows / ps)
+    return invalid(who, "need num_pages >= 1 and num_pages * page_size <= 2^31");
+  if (max_pages < 1 || max_pages > kMaxPosition / ps)
+    return invalid(who, "need max_pages >= 1 and max_pages * page_size <= 2^30");
+  if (batch < 1 || batch > kMaxBatch) return invalid(who, "batch must be in [1, 65535]");
+  if (n_tokens < 0 || n_tokens >= (int64_t(1) << 30)) return invalid(who, "n_tokens must be in [0, 2^30)");
+  return MOA_OK;
+}
+
+moa_status_t check_pages(const char* who, const moa_plan_t* plan, const Pool* pages, const int32_t* positions,
                          int32_t batch, int64_t n_tokens) {
   if (!plan || !pages) return invalid(who, "null plan or pages");
   if (!pages->k_pages || !pages->v_pages || !pages->table || !positions) return invalid(who, "null pointer");
   if (!aligned16(pages->k_pages) || !aligned16(pages->v_pages) || !aligned4(pages->table) || !aligned4(positions))
     return invalid(who, "pages must be 16-byte aligned, table and positions 4-byte");
-  const int32_t ps = pages->page_size;
-  if (ps < (1 << kMinPageShift) || ps > (1 << kMaxPageShift) || (ps & (ps - 1)) != 0)
-    return fail(MOA_ERR_UNSUPPORTED, std::string(who) + ": page_size must be 16, 32, 64, 128 or 256");
-  if (pages->num_pages < 1 || pages->num_pages > kMaxPageRows / ps)
-    return invalid(who, "need num_pages >= 1 and num_pages * page_size <= 2^31");
-  if (pages->max_pages < 1 || pages->max_pages > kMaxPosition / ps)
-    return invalid(who, "need max_pages >= 1 and max_pages * page_size <= 2^30");
-  if (batch < 1 || batch > kMaxBatch) return invalid(who, "batch must be in [1, 65535]");
-  if (n_tokens < 0 || n_tokens >= (int64_t(1) << 30)) return invalid(who, "n_tokens must be in [0, 2^30)");
+  if (pages->quant) {
+    if (plan->desc.dtype != MOA_BF16) return fail(MOA_ERR_UNSUPPORTED, std::string(who) + ": an 8-bit cache takes bf16 plans");
+    if (!pages->scales || !aligned8(pages->scales)) return invalid(who, "null or misaligned scales (8-byte aligned)");
+  }
+  const moa_status_t st = check_sizes(who, pages->page_size, pages->num_pages, pages->max_pages, batch, n_tokens);
+  if (st != MOA_OK) return st;
   const size_t pool = pool_bytes(*plan, *pages);
   if (overlaps(pages->k_pages, pool, pages->v_pages, pool)) return invalid(who, "k_pages overlaps v_pages");
+  if (const size_t sb = scale_bytes(*pages))
+    if (overlaps(pages->scales, sb, pages->k_pages, pool) || overlaps(pages->scales, sb, pages->v_pages, pool))
+      return invalid(who, "scales overlap the pages");
   return MOA_OK;
 }
 
@@ -51,7 +91,7 @@ int page_shift(const moa_pages_t& pages) { return __builtin_ctz(static_cast<unsi
 
 // Checks the arguments that the three attention calls have in common and fills in
 // those of the kernels.
-moa_status_t attention_args(const char* who, const moa_plan_t* plan, const moa_pages_t* pages, const void* q, void* o,
+moa_status_t attention_args(const char* who, const moa_plan_t* plan, const Pool* pages, const void* q, void* o,
                             const int32_t* positions, int32_t batch, int64_t n_tokens, void* workspace, size_t ws_bytes,
                             PagedArgs* a) {
   const moa_status_t st = check_pages(who, plan, pages, positions, batch, n_tokens);
@@ -69,13 +109,15 @@ moa_status_t attention_args(const char* who, const moa_plan_t* plan, const moa_p
   const size_t qb = rows_bytes(p, n_tokens, d.num_q_heads), pool = pool_bytes(p, *pages);
   const size_t tb = sizeof(int32_t) * static_cast<size_t>(batch) * d.num_kv_heads * pages->max_pages;
   const struct { const void* p; size_t n; } reads[] = {
-      {q, qb}, {pages->k_pages, pool}, {pages->v_pages, pool}, {pages->table, tb}, {positions, sizeof(int32_t) * batch}};
+      {q, qb}, {pages->k_pages, pool}, {pages->v_pages, pool}, {pages->table, tb}, {positions, sizeof(int32_t) * batch},
+      {pages->scales, scale_bytes(*pages)}};
   for (const auto& r : reads)
-    if (overlaps(o, qb, r.p, r.n) || overlaps(workspace, need, r.p, r.n))
+    if (r.n && (overlaps(o, qb, r.p, r.n) || overlaps(workspace, need, r.p, r.n)))
       return invalid(who, "o or the workspace overlaps another argument");
   if (overlaps(o, qb, workspace, need)) return invalid(who, "o overlaps the workspace");
   memset(a, 0, sizeof(*a));
   a->q = q; a->o = o; a->kp = pages->k_pages; a->vp = pages->v_pages;
+  a->scales = pages->scales;
   a->table = pages->table;
   a->positions = positions;
   a->part = static_cast<float*>(workspace);
@@ -133,7 +175,7 @@ PrefillSpace prefill_space(const moa_plan_s& p) {
 }
 
 // Rounds of all caches of a decode call are counted in 31 bits.
-bool countable(const moa_plan_s& p, const moa_pages_t& pages, int32_t batch) {
+bool countable(const moa_plan_s& p, const Pool& pages, int32_t batch) {
   int64_t keys = 0;
   for (int h = 0; h < p.desc.num_kv_heads; ++h)
     keys += std::min<int64_t>(p.capacity[h], int64_t(pages.max_pages) * pages.page_size) / 64 + 1;
@@ -146,19 +188,10 @@ moa_status_t launched(const char* who, int err) {
   return ok();
 }
 
-}  // namespace
-
-}  // namespace moa
-
-using namespace moa;
-
-extern "C" {
-
-moa_status_t moa_paged_append(const moa_plan_t* plan, const moa_pages_t* pages, const void* q, int64_t q_stride,
+moa_status_t paged_append(const char* who, const moa_plan_t* plan, const Pool* pages, const void* q, int64_t q_stride,
                               const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, void* q_out,
                               const moa_rope_t* rope, const int32_t* positions, const int32_t* seq_start,
                               int32_t batch, int64_t n_tokens, void* hip_stream) {
-  const char* who = "moa_paged_append";
   const moa_status_t st = check_pages(who, plan, pages, positions, batch, n_tokens);
   if (st != MOA_OK) return st;
   if (!seq_start && n_tokens != batch) return invalid(who, "without seq_start there is one token per sequence");
@@ -177,7 +210,7 @@ moa_status_t moa_paged_append(const moa_plan_t* plan, const moa_pages_t* pages, 
   if (rope) {
     if (!rope->inv_freq || !aligned4(rope->inv_freq)) return invalid(who, "null or misaligned inv_freq");
     if (rope->rotary_dim < 16 || rope->rotary_dim > d.head_dim || rope->rotary_dim % 16 != 0)
-      return fail(MOA_ERR_UNSUPPORTED, "moa_paged_append: rotary_dim must be a multiple of 16, at most head_dim");
+      return fail(MOA_ERR_UNSUPPORTED, std::string(who) + ": rotary_dim must be a multiple of 16, at most head_dim");
     if (rope->interleaved != 0 && rope->interleaved != 1) return invalid(who, "interleaved must be 0 or 1");
   }
   const size_t pool = pool_bytes(*plan, *pages);
@@ -190,10 +223,13 @@ moa_status_t moa_paged_append(const moa_plan_t* plan, const moa_pages_t* pages, 
       {k_new, kb}, {v_new, vb}, {pages->table, tb}, {positions, sizeof(int32_t) * batch},
       {seq_start, seq_start ? sizeof(int32_t) * (batch + 1) : 0},
       {rope ? rope->inv_freq : nullptr, rope ? sizeof(float) * (rope->rotary_dim / 2) : 0}};
-  for (const void* pages_of : {static_cast<const void*>(pages->k_pages), static_cast<const void*>(pages->v_pages)}) {
+  const struct { const void* p; size_t n; } written[] = {
+      {pages->k_pages, pool}, {pages->v_pages, pool}, {pages->scales, scale_bytes(*pages)}};
+  for (const auto& w : written) {
+    if (!w.n) continue;
     for (const auto& r : reads)
-      if (r.n && overlaps(pages_of, pool, r.p, r.n)) return invalid(who, "the pages overlap another argument");
-    if (q && (overlaps(pages_of, pool, q, qb) || overlaps(pages_of, pool, q_out, ob)))
+      if (r.n && overlaps(w.p, w.n, r.p, r.n)) return invalid(who, "the pages overlap another argument");
+    if (q && (overlaps(w.p, w.n, q, qb) || overlaps(w.p, w.n, q_out, ob)))
       return invalid(who, "the pages overlap another argument");
   }
   if (q) {
@@ -202,8 +238,10 @@ moa_status_t moa_paged_append(const moa_plan_t* plan, const moa_pages_t* pages, 
     if (overlaps(q_out, ob, q, qb) && !(q_out == q && q_stride == q_row))
       return invalid(who, "q_out overlaps q without being q");
   }
-  PagedAppendArgs a;
-  memset(&a, 0, sizeof(a));
+  QuantAppendArgs args;
+  memset(&args, 0, sizeof(args));
+  args.scales = pages->scales;
+  PagedAppendArgs& a = args.a;
   a.q = q; a.kn = k_new; a.vn = v_new; a.q_out = q_out;
   a.kp = pages->k_pages; a.vp = pages->v_pages; a.table = pages->table;
   a.positions = positions;
@@ -223,18 +261,13 @@ moa_status_t moa_paged_append(const moa_plan_t* plan, const moa_pages_t* pages, 
     a.rotary = rope->rotary_dim;
     a.interleaved = rope->interleaved;
   }
-  return launched(who, launch_paged_append(a, d.dtype, d.head_dim, hip_stream));
+  return launched(who, pages->quant ? launch_quant_append(args, d.head_dim, hip_stream)
+                                    : launch_paged_append(a, d.dtype, d.head_dim, hip_stream));
 }
 
-size_t moa_paged_workspace_bytes(const moa_plan_t* plan, int32_t batch, int64_t n_tokens) {
-  if (!plan || batch < 1 || n_tokens < 1) return 0;
-  return std::max(decode_space(*plan, batch).bytes, prefill_space(*plan).bytes);
-}
-
-moa_status_t moa_paged_prefill(const moa_plan_t* plan, const moa_pages_t* pages, const void* q, void* o,
+moa_status_t paged_prefill(const char* who, const moa_plan_t* plan, const Pool* pages, const void* q, void* o,
                                const int32_t* positions, const int32_t* seq_start, int32_t batch, int64_t n_tokens,
                                void* workspace, size_t ws_bytes, void* hip_stream) {
-  const char* who = "moa_paged_prefill";
   PagedArgs a;
   if (n_tokens == 0) {
     const moa_status_t none = check_pages(who, plan, pages, positions, batch, 0);
@@ -286,27 +319,31 @@ moa_status_t moa_paged_prefill(const moa_plan_t* plan, const moa_pages_t* pages,
   a.full_cost = bf16 ? kFullRowCost : kWholeRowCostF32;
   // a work-group per row tile, dealt to the dies in whole rounds, or per piece
   const int64_t groups = std::max<int64_t>((tiles + 127) / 128 * 128, whole ? 0 : a.slots);
-  int err = launch_paged_rows(a, d.dtype, d.head_dim, key_groups, groups, hip_stream);
+  int err = pages->quant ? launch_quant_rows(a, d.head_dim, key_groups, groups, hip_stream)
+                         : launch_paged_rows(a, d.dtype, d.head_dim, key_groups, groups, hip_stream);
   if (!err && !whole) err = launch_paged_merge(a, d.dtype, d.head_dim, hip_stream);
   return launched(who, err);
 }
 
-moa_status_t moa_paged_decode(const moa_plan_t* plan, const moa_pages_t* pages, const void* q, void* o,
+int run_decode(const moa_plan_s& p, const Pool& pages, const PagedArgs& a, void* hip_stream) {
+  return pages.quant ? launch_quant_decode(a, p.desc.head_dim, p.group, hip_stream)
+                     : launch_paged_decode(a, p.desc.dtype, p.desc.head_dim, p.group, hip_stream);
+}
+
+moa_status_t paged_decode(const char* who, const moa_plan_t* plan, const Pool* pages, const void* q, void* o,
                               const int32_t* positions, int32_t batch, void* workspace, size_t ws_bytes,
                               void* hip_stream) {
-  const char* who = "moa_paged_decode";
   PagedArgs a;
   const moa_status_t st = attention_args(who, plan, pages, q, o, positions, batch, batch, workspace, ws_bytes, &a);
   if (st != MOA_OK) return st;
   if (!countable(*plan, *pages, batch)) return launched(who, kGridTooLarge);
   a.plan = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + decode_space(*plan, batch).plan);
-  return launched(who, launch_paged_decode(a, plan->desc.dtype, plan->desc.head_dim, plan->group, hip_stream));
+  return launched(who, run_decode(*plan, *pages, a, hip_stream));
 }
 
-moa_status_t moa_paged_decode_shared(const moa_plan_t* plan, const moa_pages_t* pages, const int32_t* prefix_table,
+moa_status_t paged_decode_shared(const char* who, const moa_plan_t* plan, const Pool* pages, const int32_t* prefix_table,
                                      int64_t prefix_len, const void* q, void* o, const int32_t* positions,
                                      int32_t batch, void* workspace, size_t ws_bytes, void* hip_stream) {
-  const char* who = "moa_paged_decode_shared";
   PagedArgs a;
   const moa_status_t st = attention_args(who, plan, pages, q, o, positions, batch, batch, workspace, ws_bytes, &a);
   if (st != MOA_OK) return st;
@@ -355,9 +392,140 @@ moa_status_t moa_paged_decode_shared(const moa_plan_t* plan, const moa_pages_t* 
     a.prefix_piece[d.num_kv_heads] = static_cast<int32_t>(pieces);
     a.prefix_items = static_cast<int32_t>(pieces * tiles);
     a.slots = most;
-    return launched(who, launch_paged_shared(a, d.dtype, d.head_dim, plan->group, hip_stream));
+    return launched(who, pages->quant ? launch_quant_shared(a, d.head_dim, plan->group, hip_stream)
+                                      : launch_paged_shared(a, d.dtype, d.head_dim, plan->group, hip_stream));
   }
-  return launched(who, launch_paged_decode(a, d.dtype, d.head_dim, plan->group, hip_stream));
+  return launched(who, run_decode(*plan, *pages, a, hip_stream));
+}
+
+}  // namespace
+
+}  // namespace moa
+
+using namespace moa;
+
+extern "C" {
+
+moa_status_t moa_paged_append(const moa_plan_t* plan, const moa_pages_t* pages, const void* q, int64_t q_stride,
+                              const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, void* q_out,
+                              const moa_rope_t* rope, const int32_t* positions, const int32_t* seq_start,
+                              int32_t batch, int64_t n_tokens, void* hip_stream) {
+  Pool pool;
+  return paged_append("moa_paged_append", plan, pool_of(pages, &pool), q, q_stride, k_new, k_stride, v_new, v_stride,
+                      q_out, rope, positions, seq_start, batch, n_tokens, hip_stream);
+}
+
+moa_status_t moa_quant_append(const moa_plan_t* plan, const moa_quant_pages_t* pages, const void* q, int64_t q_stride,
+                              const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, void* q_out,
+                              const moa_rope_t* rope, const int32_t* positions, const int32_t* seq_start,
+                              int32_t batch, int64_t n_tokens, void* hip_stream) {
+  Pool pool;
+  return paged_append("moa_quant_append", plan, pool_of(pages, &pool), q, q_stride, k_new, k_stride, v_new, v_stride,
+                      q_out, rope, positions, seq_start, batch, n_tokens, hip_stream);
+}
+
+size_t moa_paged_workspace_bytes(const moa_plan_t* plan, int32_t batch, int64_t n_tokens) {
+  if (!plan || batch < 1 || n_tokens < 1) return 0;
+  return std::max(decode_space(*plan, batch).bytes, prefill_space(*plan).bytes);
+}
+
+moa_status_t moa_paged_prefill(const moa_plan_t* plan, const moa_pages_t* pages, const void* q, void* o,
+                               const int32_t* positions, const int32_t* seq_start, int32_t batch, int64_t n_tokens,
+                               void* workspace, size_t ws_bytes, void* hip_stream) {
+  Pool pool;
+  return paged_prefill("moa_paged_prefill", plan, pool_of(pages, &pool), q, o, positions, seq_start, batch, n_tokens,
+                       workspace, ws_bytes, hip_stream);
+}
+
+moa_status_t moa_quant_prefill(const moa_plan_t* plan, const moa_quant_pages_t* pages, const void* q, void* o,
+                               const int32_t* positions, const int32_t* seq_start, int32_t batch, int64_t n_tokens,
+                               void* workspace, size_t ws_bytes, void* hip_stream) {
+  Pool pool;
+  return paged_prefill("moa_quant_prefill", plan, pool_of(pages, &pool), q, o, positions, seq_start, batch, n_tokens,
+                       workspace, ws_bytes, hip_stream);
+}
+
+moa_status_t moa_paged_decode(const moa_plan_t* plan, const moa_pages_t* pages, const void* q, void* o,
+                              const int32_t* positions, int32_t batch, void* workspace, size_t ws_bytes,
+                              void* hip_stream) {
+  Pool pool;
+  return paged_decode("moa_paged_decode", plan, pool_of(pages, &pool), q, o, positions, batch, workspace, ws_bytes,
+                      hip_stream);
+}
+
+moa_status_t moa_quant_decode(const moa_plan_t* plan, const moa_quant_pages_t* pages, const void* q, void* o,
+                              const int32_t* positions, int32_t batch, void* workspace, size_t ws_bytes,
+                              void* hip_stream) {
+  Pool pool;
+  return paged_decode("moa_quant_decode", plan, pool_of(pages, &pool), q, o, positions, batch, workspace, ws_bytes,
+                      hip_stream);
+}
+
+moa_status_t moa_paged_decode_shared(const moa_plan_t* plan, const moa_pages_t* pages, const int32_t* prefix_table,
+                                     int64_t prefix_len, const void* q, void* o, const int32_t* positions,
+                                     int32_t batch, void* workspace, size_t ws_bytes, void* hip_stream) {
+  Pool pool;
+  return paged_decode_shared("moa_paged_decode_shared", plan, pool_of(pages, &pool), prefix_table, prefix_len, q, o,
+                             positions, batch, workspace, ws_bytes, hip_stream);
+}
+
+moa_status_t moa_quant_decode_shared(const moa_plan_t* plan, const moa_quant_pages_t* pages, const int32_t* prefix_table,
+                                     int64_t prefix_len, const void* q, void* o, const int32_t* positions,
+                                     int32_t batch, void* workspace, size_t ws_bytes, void* hip_stream) {
+  Pool pool;
+  return paged_decode_shared("moa_quant_decode_shared", plan, pool_of(pages, &pool), prefix_table, prefix_len, q, o,
+                             positions, batch, workspace, ws_bytes, hip_stream);
+}
+
+moa_status_t moa_paged_assign(const moa_plan_t* plan, const moa_page_tables_t* tables, const int32_t* positions,
+                              const int32_t* seq_start, const int32_t* fresh, int32_t* slots, int32_t batch,
+                              int64_t n_tokens, void* workspace, size_t ws_bytes, void* hip_stream) {
+  const char* who = "moa_paged_assign";
+  if (!plan || !tables) return invalid(who, "null plan or tables");
+  if (!tables->table || !tables->free_pages || !tables->counts || !positions) return invalid(who, "null pointer");
+  const void* const ints[] = {tables->table, tables->free_pages, tables->counts, positions, seq_start, fresh, slots};
+  for (const void* p : ints)
+    if (!aligned4(p)) return invalid(who, "tensors must be 4-byte aligned");
+  const moa_status_t st = check_sizes(who, tables->page_size, tables->num_pages, tables->max_pages, batch, n_tokens);
+  if (st != MOA_OK) return st;
+  if (!seq_start && slots && n_tokens != batch) return invalid(who, "without seq_start there is one token per sequence");
+  const moa_desc_t& d = plan->desc;
+  const size_t need = moa_paged_workspace_bytes(plan, batch, std::max<int64_t>(n_tokens, 1));
+  if (!workspace || ws_bytes < need)
+    return fail(MOA_ERR_WORKSPACE, std::string(who) + ": workspace missing or smaller than moa_paged_workspace_bytes (" +
+                                       std::to_string(need) + " bytes)");
+  if (reinterpret_cast<uintptr_t>(workspace) & 255u)
+    return fail(MOA_ERR_WORKSPACE, std::string(who) + ": workspace must be 256-byte aligned");
+  const size_t i4 = sizeof(int32_t), pairs = static_cast<size_t>(batch) * d.num_kv_heads;
+  const struct { const void* p; size_t n; } args[] = {     // the first five are written
+      {tables->table, i4 * pairs * tables->max_pages},
+      {tables->free_pages, i4 * static_cast<size_t>(tables->num_pages)},
+      {tables->counts, i4 * 2},
+      {slots, slots ? i4 * static_cast<size_t>(n_tokens) * d.num_kv_heads : 0},
+      {workspace, need},
+      {positions, i4 * batch},
+      {seq_start, seq_start ? i4 * (static_cast<size_t>(batch) + 1) : 0},
+      {fresh, fresh ? i4 * batch : 0}};
+  for (int i = 0; i < 5; ++i)
+    for (int j = i + 1; j < 8; ++j)
+      if (args[i].n && args[j].n && overlaps(args[i].p, args[i].n, args[j].p, args[j].n))
+        return invalid(who, "an argument that is written overlaps another one");
+  AssignArgs a;
+  memset(&a, 0, sizeof(a));
+  a.table = tables->table; a.free_pages = tables->free_pages; a.counts = tables->counts;
+  a.positions = positions; a.seq_start = seq_start; a.fresh = fresh; a.slots = slots;
+  a.plan = static_cast<int64_t*>(workspace);
+  static_assert(kPagedPartPad * sizeof(float) >= 2 * sizeof(int64_t), "a pair's share of the workspace holds its counts");
+  a.n_tokens = static_cast<int32_t>(n_tokens);
+  a.batch = batch;
+  a.hkv = d.num_kv_heads;
+  a.num_pages = static_cast<int32_t>(std::min<int64_t>(tables->num_pages, INT32_MAX));
+  a.page_shift = __builtin_ctz(static_cast<unsigned>(tables->page_size));
+  a.max_pages = tables->max_pages;
+  a.num_sink = d.num_sink;
+  a.block_band = (d.flags & MOA_BLOCK_BAND) != 0;
+  for (int h = 0; h < d.num_kv_heads; ++h) a.window[h] = plan->window[h];
+  return launched(who, launch_paged_assign(a, hip_stream));
 }
 
 }  // extern "C"

@@ -574,7 +574,7 @@ __device__ __forceinline__ void decode_worker(const PagedArgs& a, DecodeLds<T, D
 template <int G>
 constexpr int merge_heads() { return G <= 2 ? G : 2; }
 
-template <typename T, int D, int G, bool kShared>
+template <typename T, int D, int G, bool kShared, int kRoundShift = decode_round_shift<T, D, G>()>
 __global__ void __launch_bounds__(256) paged_combine_kernel(PagedArgs a) {
   constexpr int PS = D + kPagedPartPad;
   constexpr int V4 = D / 4;
@@ -599,7 +599,7 @@ __global__ void __launch_bounds__(256) paged_combine_kernel(PagedArgs a) {
   int n_own = 0, np;
   const float *own = a.part, *prefix = nullptr;
   int64_t step = 0;                                   // from piece to piece of the prefix
-  const uint32_t rounds = rounds_of(a, pos, g, decode_round_shift<T, D, G>());
+  const uint32_t rounds = rounds_of(a, pos, g, kRoundShift);
   if (rounds > 0) {
     const uint32_t w0 = split.worker_of(x0), w1 = split.worker_of(x0 + rounds - 1);
     n_own = static_cast<int>(w1 - w0) + 1;

@@ -11,10 +11,9 @@ namespace moa {
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-// The sequence of packed row t: the last b with seq_start[b] <= t, or -1 where no
-// sequence has the row.  All lanes of the wave search together, 64 probes per trip to
-// memory; whatever seq_start holds, only its batch + 1 entries are read.
-__device__ __forceinline__ int sequence_of(const int32_t* seq_start, int batch, int t) {
+// The last b with seq_start[b] <= t, or -1.  All lanes of the wave search together, 64
+// probes per trip to memory; whatever seq_start holds, only its batch + 1 entries are read.
+__device__ __forceinline__ int sequence_at(const int32_t* seq_start, int batch, int t) {
   const int lane = threadIdx.x & 63;
   int b = 0, n = batch;
   while (true) {
@@ -26,8 +25,13 @@ __device__ __forceinline__ int sequence_of(const int32_t* seq_start, int batch, 
     n = min(stride, n - (c - 1) * stride);
     if (stride == 1) break;
   }
-  b = uniform(b);
-  return t < seq_start[b + 1] ? b : -1;
+  return uniform(b);
+}
+
+// The sequence of packed row t, or -1 where no sequence has the row.
+__device__ __forceinline__ int sequence_of(const int32_t* seq_start, int batch, int t) {
+  const int b = sequence_at(seq_start, batch, t);
+  return b >= 0 && t < seq_start[b + 1] ? b : -1;
 }
 
 // Position of packed row t of sequence b, negative for an idle sequence.
@@ -68,6 +72,8 @@ __device__ __forceinline__ float dot2_ones(bf16 a, bf16 b, float acc) {
   return acc + float(a) + float(b);
 #endif
 }
+
+__device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
 
 // Resident work-groups of `kernel` on the current device (cached per device by the
 // caller; threads that launch at once store the same value).

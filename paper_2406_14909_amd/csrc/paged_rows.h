@@ -19,8 +19,6 @@
 
 namespace moa {
 
-__device__ __forceinline__ bool finite(float x) { return fabsf(x) < INFINITY; }
-
 constexpr float kRescaleSlack = 8.0f;   // log2 headroom before a running maximum is raised
 
 // One row tile and a part [num0, num1) of den of its key tiles.
@@ -270,6 +268,25 @@ __device__ __forceinline__ PagedItem prefix_item(const PagedArgs& a, int w) {
   it.den = a.prefix_piece[g + 1] - first;
   it.slot = w;
   return it;
+}
+
+// What work-group `block` of a launch over a shared prefix does: an item of the prefix, or a worker's
+// piece of the keys behind it.  The two kinds alternate, in eights, so that every die and most compute
+// units have both.  Neighbours of the prefix's items share a die.
+struct SharedWork {
+  bool prefix;
+  int index;
+};
+__device__ __forceinline__ SharedWork shared_work(const PagedArgs& a, int block) {
+  const int prefix = (a.prefix_items + kNumXcd - 1) / kNumXcd, own = (a.slots + kNumXcd - 1) / kNumXcd;
+  const int eight = block / kNumXcd, die = block % kNumXcd;
+  const int both = 2 * min(prefix, own);
+  const bool is_prefix = eight < both ? eight % 2 == 0 : prefix > own;
+  const int nth = eight < both ? eight / 2 : eight - both / 2;     // of its kind on this die
+  return {is_prefix, is_prefix ? die * prefix + nth : nth * kNumXcd + die};
+}
+inline unsigned shared_groups(const PagedArgs& a) {
+  return ((a.prefix_items + kNumXcd - 1) / kNumXcd + (a.slots + kNumXcd - 1) / kNumXcd) * kNumXcd;
 }
 
 }  // namespace moa

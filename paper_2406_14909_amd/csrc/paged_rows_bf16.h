@@ -28,6 +28,7 @@
 #include <type_traits>
 
 #include "paged_rows.h"
+#include "quant_device.h"
 
 namespace moa {
 
@@ -79,7 +80,8 @@ struct RowsBf16Lds {
 // Work-group w of a launch over ragged chunks, or (kShared) over a shared prefix.  KG groups
 // of 4 waves share its rows: group kg takes key tiles kg, kg + KG, ... through LDS stages of
 // its own, and their states meet in LDS at the end.
-template <int D, bool kShared, int KG>
+// k8: over 8-bit pages, which pass through registers on their way to LDS and are bf16 there.
+template <int D, bool kShared, int KG, bool k8 = false>
 __device__ __forceinline__ void rows_bf16(const PagedArgs& a, RowsBf16Lds<D, KG>& lds, int w) {
   using TL = RowTiles<D>;
   constexpr int KS = D / 16;              // steps over the head dimension
@@ -192,6 +194,15 @@ __device__ __forceinline__ void rows_bf16(const PagedArgs& a, RowsBf16Lds<D, KG>
     auto group_full = [&](int kb) {
       return kb + 16 <= key_end && (kb + 16 <= sinks || kb >= band_lo || sinks >= band_lo);
     };
+    // A key that no row sees takes a neighbour of its group (from kb on), or, where there is none, of
+    // the tile (from j0 on); so the whole group stays in one page.
+    auto seen_of = [&](int j, int kb, int j0) {
+      j = min(j, key_end - 1);
+      if (j < sinks || j >= band_lo) return j;
+      if (sinks > kb) return sinks - 1;
+      if (band_lo < kb + 16 && band_lo < key_end) return band_lo;
+      return sinks > j0 ? sinks - 1 : band_lo;
+    };
     auto group_desc = [&](const void* pool, int page, int kb) {
       const int r = page_row(page, a.num_pages, a.page_shift);
       return make_desc(static_cast<const char*>(pool) + int64_t(max(r, 0) + (kb & ps_mask)) * RB, r < 0 ? 0 : 16 * RB);
@@ -204,21 +215,54 @@ __device__ __forceinline__ void rows_bf16(const PagedArgs& a, RowsBf16Lds<D, KG>
         for (int i = 0; i < DPW; ++i) dma16_async(rs, src[i], lds + (wave * DPW + i) * 1024);
         return;
       }
-      // A key that no row sees takes a neighbour of its group, or, where there is none, of the
-      // tile; so the whole group stays in one page.
-      auto seen = [&](int j) {
-        j = min(j, key_end - 1);
-        if (j < sinks || j >= band_lo) return j;
-        if (sinks > kb) return sinks - 1;
-        if (band_lo < kb + 16 && band_lo < key_end) return band_lo;
-        return sinks > j0 ? sinks - 1 : band_lo;
-      };
+      auto seen = [&](int j) { return seen_of(j, kb, j0); };
       const int r = page_row(scalar_read(table, uniform(seen(kb)) >> a.page_shift), a.num_pages, a.page_shift);
       const i32x4 rs = make_desc(static_cast<const char*>(pool) + int64_t(max(r, 0)) * RB, r < 0 ? 0 : (ps_mask + 1) * RB);
 #pragma unroll
       for (int i = 0; i < DPW; ++i) {
         const int c = seen(kb + static_cast<int>(src[i] / RB));
         dma16_async(rs, uint32_t(c & ps_mask) * RB + src[i] % RB, lds + (wave * DPW + i) * 1024);
+      }
+    };
+
+    // 8-bit pages: this wave's 16 keys of a tile in registers, lane L's 16 bytes chunk L % CP8 of row
+    // L / CP8 (+ 64 / CP8) of the group, and what they become in LDS.
+    constexpr int CP8 = D / 16, LD8 = 16 * CP8 / 64, RP8 = 64 / CP8;
+    u32x4 k_raw[LD8], v_raw[LD8];
+    f32x2 raw_scale[LD8];
+    auto load_raw = [&](int j0, const Pages& pages) {
+      const int kb = j0 + 16 * wave;
+      const bool full = group_full(kb);
+      const int page = full ? mine(pages) : scalar_read(table, uniform(seen_of(kb, kb, j0)) >> a.page_shift);
+      const int r = page_row(page, a.num_pages, a.page_shift);
+#pragma unroll
+      for (int i = 0; i < LD8; ++i) {
+        const int j = kb + i * RP8 + lane / CP8;
+        const int64_t row = int64_t(max(r, 0)) + ((full ? j : seen_of(j, kb, j0)) & ps_mask);
+        raw_scale[i] = f32x2{1.0f, 1.0f};
+        k_raw[i] = v_raw[i] = u32x4{};
+        if (r >= 0) {                         // absent pages are zeros
+          raw_scale[i] = reinterpret_cast<const f32x2*>(a.scales)[row / kQuantBlock];
+          k_raw[i] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.kp) + row * D + lane % CP8 * 16);
+          v_raw[i] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.vp) + row * D + lane % CP8 * 16);
+        }
+      }
+    };
+    auto store_raw = [&](char* k_lds, char* v_lds, bool careful) {
+#pragma unroll
+      for (int i = 0; i < LD8; ++i) {
+        const int r = 16 * wave + i * RP8 + lane / CP8, c = 2 * (lane % CP8);
+        if (__builtin_expect(careful, 0)) {   // 0 in place of what is no number
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v_raw[i][e] &= ~((nan_bytes(v_raw[i][e]) >> 7) * 0xffu);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          *reinterpret_cast<bf16x8*>(k_lds + r * RB + (((c + h) ^ TL::swz_k(r)) * 16)) =
+              widen8(u32x2{k_raw[i][2 * h], k_raw[i][2 * h + 1]}, raw_scale[i][0]);
+          *reinterpret_cast<bf16x8*>(v_lds + r * RB + (((c + h) ^ TL::swz_v(r)) * 16)) =
+              widen8(u32x2{v_raw[i][2 * h], v_raw[i][2 * h + 1]}, raw_scale[i][1]);
+        }
       }
     };
 
@@ -262,13 +306,19 @@ __device__ __forceinline__ void rows_bf16(const PagedArgs& a, RowsBf16Lds<D, KG>
       if (ts < t1) {
         jt = tile_j0(ts);
         pt = fetch(jt);
-        tile_dma(a.vp, v_src, jt, pt, sV);
-        tile_dma(a.kp, k_src, jt, pt, sK);
+        if constexpr (k8) {
+          load_raw(jt, pt);
+          store_raw(sK, sV, careful);
+        } else {
+          tile_dma(a.vp, v_src, jt, pt, sV);
+          tile_dma(a.kp, k_src, jt, pt, sK);
+        }
       }
       if (ts + KG < t1) {
         j1 = tile_j0(ts + KG);
         p1 = fetch(j1);
-        tile_dma(a.kp, k_src, j1, p1, sK + TL::TILE_BYTES);
+        if constexpr (k8) load_raw(j1, p1);
+        else tile_dma(a.kp, k_src, j1, p1, sK + TL::TILE_BYTES);
       }
       if (ts + 2 * KG < t1) {
         j2 = tile_j0(ts + 2 * KG);
@@ -277,13 +327,15 @@ __device__ __forceinline__ void rows_bf16(const PagedArgs& a, RowsBf16Lds<D, KG>
       int k_now = 0, k_next = (KST - 1) * TL::TILE_BYTES, v_now = 0;      // byte offsets of stages
       // Wait for Q (and the first tiles) here, once: the compiler does not count the direct
       // loads and would otherwise wait for everything in flight inside the loop.
-      __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
+      if constexpr (!k8) __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
       for (int t = ts; t < t1 + kg; t += KG) {            // as many rounds for every group
         const int j0 = jt;
         const int ok = present(pt);
-        if (t + KG < t1) __builtin_amdgcn_s_waitcnt(0x0F70 | DPW);  // the next K may be in flight
-        else __builtin_amdgcn_s_waitcnt(0x0F70);
-        if (__builtin_expect(careful && t < t1, 0)) {   // this wave's values of the tile: 0 in place of what is not finite
+        if constexpr (!k8) {
+          if (t + KG < t1) __builtin_amdgcn_s_waitcnt(0x0F70 | DPW);  // the next K may be in flight
+          else __builtin_amdgcn_s_waitcnt(0x0F70);
+        }
+        if (__builtin_expect(!k8 && careful && t < t1, 0)) {   // this wave's values of the tile: 0 in place of what is not finite
 #pragma unroll 1
           for (int i = 0; i < DPW; ++i) {
             bf16x8* const at = reinterpret_cast<bf16x8*>(sV + v_now + (wave * DPW + i) * 1024 + lane * 16);
@@ -305,16 +357,20 @@ __device__ __forceinline__ void rows_bf16(const PagedArgs& a, RowsBf16Lds<D, KG>
         const bool any_vis = t < t1 && j0 <= w_last && (j0 < s || band_start(w_first) <= j0 + BN - 1);
         // At head_dim 128 the next tiles' loads go between the S products; issued at once they
         // would queue for the address unit with the waves standing still.
-        constexpr bool kSpread = D == 128;
+        constexpr bool kSpread = D == 128 && !k8;
         const bool spread = kSpread && any_vis && t + 2 * KG < t1 && group_full(j1 + 16 * wave) && group_full(j2 + 16 * wave);
-        if (!spread) {
+        if constexpr (k8) {
+          // The next tile, asked for a tile ago, goes to the other stage, and the one behind it is asked for.
+          if (t + KG < t1) store_raw(sK + (v_now ^ TL::TILE_BYTES), sV + (v_now ^ TL::TILE_BYTES), careful);
+          if (t + 2 * KG < t1) load_raw(j2, p2);
+        } else if (!spread) {
           if (t + KG < t1) tile_dma(a.vp, v_src, j1, p1, sV + (v_now ^ TL::TILE_BYTES));
           if (t + 2 * KG < t1) tile_dma(a.kp, k_src, j2, p2, sK + k_next);
         }
         if (any_vis) {
           const bool all_vis = wave_full && ok == 15 && j0 + BN - 1 <= w_first && j0 + BN <= key_end &&
                                (j0 + BN <= s || band_start(w_last) <= j0);
-          const char* kb = sK + k_now;
+          const char* kb = sK + (k8 ? v_now : k_now);
           auto kfrag = [&](int kk, int sub) {
             return *reinterpret_cast<const bf16x8*>(kb + sub * 32 * RB + k_off[kk]);
           };
@@ -442,16 +498,28 @@ __device__ __forceinline__ void rows_bf16(const PagedArgs& a, RowsBf16Lds<D, KG>
           if (kb >= key_end) continue;
           const int r = page_row(scalar_read(table, uniform(kb >> a.page_shift)), a.num_pages, a.page_shift);
           if (r < 0) continue;
-          const bf16* const rows = static_cast<const bf16*>(a.vp) + int64_t(r + (kb & ps_mask)) * D;
+          const int64_t at = int64_t(r + (kb & ps_mask)) * D;
+          const bf16* const rows = static_cast<const bf16*>(a.vp) + at;
+          const uint8_t* const codes = static_cast<const uint8_t*>(a.vp) + at;
           uint32_t odd = 0;                   // keys with such a value
+          if constexpr (k8) {
 #pragma unroll
-          for (int k = 0; k < 16; k += 64 / CPR) {
-            const bf16x8 v = *reinterpret_cast<const bf16x8*>(rows + k * D + lane * 8);
-            bool all = true;
+            for (int k = 0; k < 16; k += RP8) {
+              const u32x4 v = *reinterpret_cast<const u32x4*>(codes + k * D + lane * 16);
+              const bool any = (nan_bytes(v[0]) | nan_bytes(v[1]) | nan_bytes(v[2]) | nan_bytes(v[3])) != 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) all &= finite(static_cast<float>(v[e]));
+              for (int h = 0; h < RP8; ++h) odd |= (__ballot(any) >> (h * CP8) & ((uint64_t(1) << CP8) - 1)) ? 1u << (k + h) : 0;
+            }
+          } else {
 #pragma unroll
-            for (int h = 0; h < 64 / CPR; ++h) odd |= (__ballot(!all) >> (h * CPR) & ((uint64_t(1) << CPR) - 1)) ? 1u << (k + h) : 0;
+            for (int k = 0; k < 16; k += 64 / CPR) {
+              const bf16x8 v = *reinterpret_cast<const bf16x8*>(rows + k * D + lane * 8);
+              bool all = true;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) all &= finite(static_cast<float>(v[e]));
+#pragma unroll
+              for (int h = 0; h < 64 / CPR; ++h) odd |= (__ballot(!all) >> (h * CPR) & ((uint64_t(1) << CPR) - 1)) ? 1u << (k + h) : 0;
+            }
           }
           while (odd != 0) {
             const int k = __builtin_ctz(odd), j = kb + k;
@@ -459,12 +527,18 @@ __device__ __forceinline__ void rows_bf16(const PagedArgs& a, RowsBf16Lds<D, KG>
             const bool vis = (j <= min(my_pos, key_end - 1)) & ((j < s) | (j >= band_start(my_pos)));
 #pragma unroll
             for (int c = 0; c < D / 8; ++c) {
-              const bf16x4 v = *reinterpret_cast<const bf16x4*>(rows + k * D + c * 8 + half * 4);
+              float x[4];
+              if constexpr (k8) {
+                const uint32_t v = nan_bytes(*reinterpret_cast<const uint32_t*>(codes + k * D + c * 8 + half * 4));
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const float x = static_cast<float>(v[e]);
-                oacc[c / 4][c % 4 * 4 + e] += vis && !finite(x) ? x : 0.0f;
+                for (int e = 0; e < 4; ++e) x[e] = v >> (8 * e + 7) & 1 ? __builtin_nanf("") : 0.0f;
+              } else {
+                const bf16x4 v = *reinterpret_cast<const bf16x4*>(rows + k * D + c * 8 + half * 4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = static_cast<float>(v[e]);
               }
+#pragma unroll
+              for (int e = 0; e < 4; ++e) oacc[c / 4][c % 4 * 4 + e] += vis && !finite(x[e]) ? x[e] : 0.0f;
             }
           }
         }

@@ -25,18 +25,12 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 && D == 128 ? 1 : 2) 
     DecodeLds<T, D, G> decode;
     RowsLds rows;
   } lds;
-  const int prefix = (a.prefix_items + kNumXcd - 1) / kNumXcd, own = (a.slots + kNumXcd - 1) / kNumXcd;
-  const int eight = static_cast<int>(blockIdx.x) / kNumXcd, die = static_cast<int>(blockIdx.x) % kNumXcd;
-  const int both = 2 * min(prefix, own);
-  const bool is_prefix = eight < both ? eight % 2 == 0 : prefix > own;
-  const int nth = eight < both ? eight / 2 : eight - both / 2;     // of its kind on this die
-  // Neighbours of the prefix's items share a die.
-  const int w = is_prefix ? die * prefix + nth : nth * kNumXcd + die;
-  if (is_prefix) {
-    if constexpr (sizeof(T) == 2) rows_bf16<D, true, 1>(a, lds.rows, w);
-    else rows_f32<D, true>(a, lds.rows, w);
+  const SharedWork work = shared_work(a, blockIdx.x);
+  if (work.prefix) {
+    if constexpr (sizeof(T) == 2) rows_bf16<D, true, 1>(a, lds.rows, work.index);
+    else rows_f32<D, true>(a, lds.rows, work.index);
   } else {
-    decode_worker<T, D, G>(a, lds.decode, w);
+    decode_worker<T, D, G>(a, lds.decode, work.index);
   }
 }
 
@@ -44,8 +38,7 @@ template <typename T, int D, int G>
 int launch_t(const PagedArgs& a, void* stream) {
   PagedArgs copy = a;
   void* args[] = {&copy};
-  const int eights = (a.prefix_items + kNumXcd - 1) / kNumXcd + (a.slots + kNumXcd - 1) / kNumXcd;
-  hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(&paged_shared_kernel<T, D, G>), dim3(eights * kNumXcd),
+  hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(&paged_shared_kernel<T, D, G>), dim3(shared_groups(a)),
                                  dim3(kThreads), args, 0, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return static_cast<int>(e);
   e = hipLaunchKernel(reinterpret_cast<const void*>(&paged_combine_kernel<T, D, G, true>), combine_grid<G>(a), dim3(256),

@@ -32,7 +32,8 @@ EXPORTED = (
     "moa_decode_workspace_bytes", "moa_decode", "moa_last_error", "moa_kv_append_ragged",
     "moa_decode_ragged", "moa_influence", "moa_rule_loss", "moa_decode_noalloc",
     "moa_paged_append", "moa_paged_workspace_bytes", "moa_paged_prefill", "moa_paged_decode",
-    "moa_paged_decode_shared",
+    "moa_paged_decode_shared", "moa_paged_assign", "moa_quant_append", "moa_quant_prefill", "moa_quant_decode",
+    "moa_quant_decode_shared",
 )
 
 
@@ -61,6 +62,29 @@ class moa_pages_t(ctypes.Structure):
     ]
 
 
+class moa_page_tables_t(ctypes.Structure):
+    _fields_ = [
+        ("table", ctypes.c_void_p),
+        ("free_pages", ctypes.c_void_p),
+        ("counts", ctypes.c_void_p),
+        ("num_pages", ctypes.c_int64),
+        ("page_size", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32),
+    ]
+
+
+class moa_quant_pages_t(ctypes.Structure):
+    _fields_ = [
+        ("k_pages", ctypes.c_void_p),
+        ("v_pages", ctypes.c_void_p),
+        ("scales", ctypes.c_void_p),
+        ("table", ctypes.c_void_p),
+        ("num_pages", ctypes.c_int64),
+        ("page_size", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32),
+    ]
+
+
 class moa_rope_t(ctypes.Structure):
     _fields_ = [
         ("inv_freq", ctypes.c_void_p),
@@ -72,6 +96,7 @@ class moa_rope_t(ctypes.Structure):
 MOA_SPAN_INCLUDES_SINKS = 1
 MOA_BLOCK_BAND = 2
 MOA_BAND_BLOCK = 64
+MOA_QUANT_BLOCK = 16
 
 
 class MoaError(RuntimeError):
@@ -83,7 +108,8 @@ class MoaError(RuntimeError):
 # Entry points that the native call path takes, in the order of its table.
 _NATIVE = ("moa_prefill", "moa_kv_append", "moa_decode", "moa_decode_noalloc", "moa_kv_append_ragged",
            "moa_decode_ragged", "moa_influence", "moa_rule_loss", "moa_paged_append", "moa_paged_prefill",
-           "moa_paged_decode", "moa_paged_decode_shared")
+           "moa_paged_decode", "moa_paged_decode_shared", "moa_paged_assign", "moa_quant_append", "moa_quant_prefill",
+           "moa_quant_decode", "moa_quant_decode_shared")
 
 _lib = None
 _fast = None        # the native call path (_binding), loaded with the library
@@ -141,6 +167,12 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.moa_paged_decode.restype = ctypes.c_int
     lib.moa_paged_decode_shared.argtypes = [vp, pages, vp, i64, vp, vp, vp, i32, vp, ctypes.c_size_t, vp]
     lib.moa_paged_decode_shared.restype = ctypes.c_int
+    lib.moa_paged_assign.argtypes = [vp, ctypes.POINTER(moa_page_tables_t), vp, vp, vp, vp, i32, i64, vp, ctypes.c_size_t, vp]
+    lib.moa_paged_assign.restype = ctypes.c_int
+    for name in ("append", "prefill", "decode", "decode_shared"):      # the same calls on other pages
+        call, like = getattr(lib, "moa_quant_" + name), getattr(lib, "moa_paged_" + name)
+        call.argtypes = [vp, ctypes.POINTER(moa_quant_pages_t)] + list(like.argtypes[2:])
+        call.restype = ctypes.c_int
     lib.moa_last_error.argtypes = []
     lib.moa_last_error.restype = ctypes.c_char_p
     from . import _binding
@@ -518,16 +550,21 @@ def _need_rank(t, rank, name):
         raise MoaError(MOA_ERR_INVALID_ARG, f"{name}: expected {rank} dimensions, got shape {tuple(t.shape)}")
 
 
-def _pages(plan: Plan, k_pages, v_pages, table, bsz):
+def _pages(plan: Plan, k_pages, v_pages, table, bsz, scales=None):
+    """The call's pages: of the plan's type, or with scales in 8 bits."""
     import torch
     _need_rank(k_pages, 3, "k_pages")
     _need_rank(table, 3, "table")
     shape = (int(k_pages.shape[0]), int(k_pages.shape[1]), plan.head_dim)
-    _need(k_pages, shape, plan.torch_dtype, "k_pages")
-    _need(v_pages, shape, plan.torch_dtype, "v_pages")
+    dt = plan.torch_dtype if scales is None else torch.float8_e4m3fn
+    _need(k_pages, shape, dt, "k_pages")
+    _need(v_pages, shape, dt, "v_pages")
     _need(table, (bsz, plan.num_kv_heads, int(table.shape[2])), torch.int32, "table")
-    return moa_pages_t(k_pages.data_ptr(), v_pages.data_ptr(), table.data_ptr(), shape[0], shape[1],
-                       int(table.shape[2]))
+    sizes = (shape[0], shape[1], int(table.shape[2]))
+    if scales is None:
+        return moa_pages_t(k_pages.data_ptr(), v_pages.data_ptr(), table.data_ptr(), *sizes)
+    _need(scales, (shape[0], shape[1] // MOA_QUANT_BLOCK, 2), torch.float32, "scales")
+    return moa_quant_pages_t(k_pages.data_ptr(), v_pages.data_ptr(), scales.data_ptr(), table.data_ptr(), *sizes)
 
 
 def _token_stride(t, shape, dtype, name):
@@ -549,29 +586,20 @@ def _seq_start(seq_start, bsz):
     _need(seq_start, (bsz + 1,), torch.int32, "seq_start")
 
 
-def moa_paged_append(plan: Plan, k_pages, v_pages, table, q, k_new, v_new, positions, seq_start=None, inv_freq=None,
-                     interleaved: bool = False, q_out=None, stream=None):
-    """Stores packed new tokens in the pages and rotates queries and keys by their positions on the way.
-
-    q: [T, H_q, D] or None, k_new, v_new: [T, H_kv, D] (parts of one projection's output may be passed
-    as they are); positions: int32[B], of each sequence's first new token; seq_start: int32[B + 1], the
-    row where each sequence's tokens start (None: one token each, T = B); inv_freq: fp32 [R / 2], radians
-    per position (None: nothing is rotated).  Returns q_out, the rotated queries (q itself may be given)."""
-    if stream is None:
-        done = _fast.paged_append(plan._bound, k_pages, v_pages, table, q, k_new, v_new, positions, seq_start, inv_freq,
-                                  interleaved, q_out)
-        if done is not None:
-            return None if done is True else done
+def _append(plan, k_pages, v_pages, scales, table, q, k_new, v_new, positions, seq_start, inv_freq, interleaved, q_out,
+            stream):
     import torch
     _need_rank(k_new, 3, "k_new")
     _need_rank(positions, 1, "positions")
     n, bsz = int(k_new.shape[0]), int(positions.shape[0])
     dt = plan.torch_dtype
-    pages = _pages(plan, k_pages, v_pages, table, bsz)
+    pages = _pages(plan, k_pages, v_pages, table, bsz, scales)
     _positions(positions, bsz)
     k_stride = _token_stride(k_new, (n, plan.num_kv_heads, plan.head_dim), dt, "k_new")
     v_stride = _token_stride(v_new, (n, plan.num_kv_heads, plan.head_dim), dt, "v_new")
     tensors = dict(k_pages=k_pages, v_pages=v_pages, table=table, k_new=k_new, v_new=v_new, positions=positions)
+    if scales is not None:
+        tensors["scales"] = scales
     q_stride = 0
     if q is not None:
         shape = (n, plan.num_q_heads, plan.head_dim)
@@ -592,14 +620,32 @@ def moa_paged_append(plan: Plan, k_pages, v_pages, table, q, k_new, v_new, posit
         rope = ctypes.byref(moa_rope_t(inv_freq.data_ptr(), 2 * int(inv_freq.shape[0]), int(bool(interleaved))))
         tensors["inv_freq"] = inv_freq
     with torch.cuda.device(_one_device(**tensors)):
-        _check(load_library().moa_paged_append(
+        lib = load_library()
+        _check((lib.moa_paged_append if scales is None else lib.moa_quant_append)(
             plan.handle, ctypes.byref(pages), None if q is None else q.data_ptr(), q_stride, k_new.data_ptr(), k_stride,
             v_new.data_ptr(), v_stride, None if q is None else q_out.data_ptr(), rope, positions.data_ptr(),
             None if seq_start is None else seq_start.data_ptr(), bsz, n, _stream(k_new, stream)))
     return q_out
 
 
-def _paged_attention(plan, q, k_pages, v_pages, table, positions, workspace, o, stream, call, **more):
+def moa_paged_append(plan: Plan, k_pages, v_pages, table, q, k_new, v_new, positions, seq_start=None, inv_freq=None,
+                     interleaved: bool = False, q_out=None, stream=None):
+    """Stores packed new tokens in the pages and rotates queries and keys by their positions on the way.
+
+    q: [T, H_q, D] or None, k_new, v_new: [T, H_kv, D] (parts of one projection's output may be passed
+    as they are); positions: int32[B], of each sequence's first new token; seq_start: int32[B + 1], the
+    row where each sequence's tokens start (None: one token each, T = B); inv_freq: fp32 [R / 2], radians
+    per position (None: nothing is rotated).  Returns q_out, the rotated queries (q itself may be given)."""
+    if stream is None:
+        done = _fast.paged_append(plan._bound, k_pages, v_pages, table, q, k_new, v_new, positions, seq_start, inv_freq,
+                                  interleaved, q_out)
+        if done is not None:
+            return None if done is True else done
+    return _append(plan, k_pages, v_pages, None, table, q, k_new, v_new, positions, seq_start, inv_freq, interleaved,
+                   q_out, stream)
+
+
+def _paged_attention(plan, q, k_pages, v_pages, scales, table, positions, workspace, o, stream, call, **more):
     """The checks that the attention calls share; call(lib, pages, n, batch, workspace bytes, o, stream) makes it."""
     import torch
     _need_rank(q, 3, "q")
@@ -607,7 +653,9 @@ def _paged_attention(plan, q, k_pages, v_pages, table, positions, workspace, o, 
     n, bsz = int(q.shape[0]), int(positions.shape[0])
     dt = plan.torch_dtype
     _need(q, (n if "seq_start" in more else bsz, plan.num_q_heads, plan.head_dim), dt, "q")
-    pages = _pages(plan, k_pages, v_pages, table, bsz)
+    pages = _pages(plan, k_pages, v_pages, table, bsz, scales)
+    if scales is not None:
+        more["scales"] = scales
     _positions(positions, bsz)
     if o is None:
         o = _new(q.shape, dt, q.device, stream)
@@ -622,6 +670,36 @@ def _paged_attention(plan, q, k_pages, v_pages, table, positions, workspace, o, 
     return o
 
 
+def _prefill(plan, q, k_pages, v_pages, scales, table, positions, seq_start, workspace, o, stream):
+    _need_rank(positions, 1, "positions")
+    _seq_start(seq_start, int(positions.shape[0]))
+    return _paged_attention(
+        plan, q, k_pages, v_pages, scales, table, positions, workspace, o, stream,
+        lambda lib, pages, n, bsz, nbytes, out, s: (lib.moa_paged_prefill if scales is None else lib.moa_quant_prefill)(
+            plan.handle, pages, q.data_ptr(), out.data_ptr(), positions.data_ptr(), seq_start.data_ptr(), bsz, n,
+            workspace.data_ptr(), nbytes, s), seq_start=seq_start)
+
+
+def _decode(plan, q, k_pages, v_pages, scales, table, positions, workspace, o, stream):
+    return _paged_attention(
+        plan, q, k_pages, v_pages, scales, table, positions, workspace, o, stream,
+        lambda lib, pages, n, bsz, nbytes, out, s: (lib.moa_paged_decode if scales is None else lib.moa_quant_decode)(
+            plan.handle, pages, q.data_ptr(), out.data_ptr(), positions.data_ptr(), bsz, workspace.data_ptr(), nbytes,
+            s))
+
+
+def _decode_shared(plan, q, k_pages, v_pages, scales, prefix_table, prefix_len, table, positions, workspace, o, stream):
+    import torch
+    _need_rank(table, 3, "table")
+    _need(prefix_table, (plan.num_kv_heads, int(table.shape[2])), torch.int32, "prefix_table")
+    return _paged_attention(
+        plan, q, k_pages, v_pages, scales, table, positions, workspace, o, stream,
+        lambda lib, pages, n, bsz, nbytes, out, s: (
+            lib.moa_paged_decode_shared if scales is None else lib.moa_quant_decode_shared)(
+            plan.handle, pages, prefix_table.data_ptr(), int(prefix_len), q.data_ptr(), out.data_ptr(),
+            positions.data_ptr(), bsz, workspace.data_ptr(), nbytes, s), prefix_table=prefix_table)
+
+
 def moa_paged_prefill(plan: Plan, q, k_pages, v_pages, table, positions, seq_start, workspace, o=None, stream=None):
     """Attention of packed new tokens (rotated, and stored by moa_paged_append) over the pages.
 
@@ -630,13 +708,7 @@ def moa_paged_prefill(plan: Plan, q, k_pages, v_pages, table, positions, seq_sta
         done = _fast.paged_prefill(plan._bound, q, k_pages, v_pages, table, positions, seq_start, workspace, o)
         if done is not None:
             return done
-    _need_rank(positions, 1, "positions")
-    _seq_start(seq_start, int(positions.shape[0]))
-    return _paged_attention(
-        plan, q, k_pages, v_pages, table, positions, workspace, o, stream,
-        lambda lib, pages, n, bsz, nbytes, out, s: lib.moa_paged_prefill(
-            plan.handle, pages, q.data_ptr(), out.data_ptr(), positions.data_ptr(), seq_start.data_ptr(), bsz, n,
-            workspace.data_ptr(), nbytes, s), seq_start=seq_start)
+    return _prefill(plan, q, k_pages, v_pages, None, table, positions, seq_start, workspace, o, stream)
 
 
 def moa_paged_decode(plan: Plan, q, k_pages, v_pages, table, positions, workspace, o=None, stream=None):
@@ -645,11 +717,7 @@ def moa_paged_decode(plan: Plan, q, k_pages, v_pages, table, positions, workspac
         done = _fast.paged_decode(plan._bound, q, k_pages, v_pages, table, positions, workspace, o)
         if done is not None:
             return done
-    return _paged_attention(
-        plan, q, k_pages, v_pages, table, positions, workspace, o, stream,
-        lambda lib, pages, n, bsz, nbytes, out, s: lib.moa_paged_decode(
-            plan.handle, pages, q.data_ptr(), out.data_ptr(), positions.data_ptr(), bsz, workspace.data_ptr(), nbytes,
-            s))
+    return _decode(plan, q, k_pages, v_pages, None, table, positions, workspace, o, stream)
 
 
 def moa_paged_decode_shared(plan: Plan, q, k_pages, v_pages, prefix_table, prefix_len: int, table, positions, workspace,
@@ -661,11 +729,130 @@ def moa_paged_decode_shared(plan: Plan, q, k_pages, v_pages, prefix_table, prefi
                                          workspace, o)
         if done is not None:
             return done
+    return _decode_shared(plan, q, k_pages, v_pages, None, prefix_table, prefix_len, table, positions, workspace, o, stream)
+
+
+# ---------------------------------------------------------------------------
+# Page tables kept on the device.
+# ---------------------------------------------------------------------------
+def new_page_tables(plan: Plan, batch: int, max_pages: int, num_pages: int, device="cuda"):
+    """(table [batch, H_kv, max_pages], free_pages [num_pages], counts [2]), int32: no pages in any
+    table, all on the free list.  counts: free pages, and pages that the last call lacked."""
+    import torch
+    table = torch.full((int(batch), plan.num_kv_heads, int(max_pages)), -1, dtype=torch.int32, device=device)
+    free_pages = torch.arange(int(num_pages) - 1, -1, -1, dtype=torch.int32, device=device)
+    return table, free_pages, torch.tensor([int(num_pages), 0], dtype=torch.int32, device=device)
+
+
+def moa_paged_assign(plan: Plan, table, free_pages, counts, page_size: int, positions, workspace, seq_start=None,
+                     fresh=None, slots=None, stream=None):
+    """Brings page tables up to a call: pages that no later query sees go back to the free list, then new
+    tokens get pages from it (include/moa.h has the order).
+
+    positions: int32[B], of each sequence's first new token, negative: left as it is; seq_start: int32[B + 1], the
+    packed row where each sequence's tokens start (None: one token each); fresh: int32[B] or None,
+    nonzero: all pages of the sequence go back first; slots: int32 [T, H_kv] or None, gets the pool's row of each
+    new token and head (-1: no page).  Returns slots."""
+    if stream is None:
+        done = _fast.paged_assign(plan._bound, table, free_pages, counts, page_size, positions, workspace, seq_start,
+                                  fresh, slots)
+        if done is not None:
+            return slots
     import torch
     _need_rank(table, 3, "table")
-    _need(prefix_table, (plan.num_kv_heads, int(table.shape[2])), torch.int32, "prefix_table")
-    return _paged_attention(
-        plan, q, k_pages, v_pages, table, positions, workspace, o, stream,
-        lambda lib, pages, n, bsz, nbytes, out, s: lib.moa_paged_decode_shared(
-            plan.handle, pages, prefix_table.data_ptr(), int(prefix_len), q.data_ptr(), out.data_ptr(),
-            positions.data_ptr(), bsz, workspace.data_ptr(), nbytes, s), prefix_table=prefix_table)
+    _need_rank(positions, 1, "positions")
+    _need_rank(free_pages, 1, "free_pages")
+    bsz, n = int(positions.shape[0]), (1 << 30) - 1
+    _positions(positions, bsz)
+    _need(table, (bsz, plan.num_kv_heads, int(table.shape[2])), torch.int32, "table")
+    _need(free_pages, free_pages.shape, torch.int32, "free_pages")
+    _need(counts, (2,), torch.int32, "counts")
+    tensors = dict(table=table, free_pages=free_pages, counts=counts, positions=positions, workspace=workspace)
+    if seq_start is not None:
+        _seq_start(seq_start, bsz)
+        tensors["seq_start"] = seq_start
+    if fresh is not None:
+        _need(fresh, (bsz,), torch.int32, "fresh")
+        tensors["fresh"] = fresh
+    if slots is not None:
+        _need_rank(slots, 2, "slots")
+        n = int(slots.shape[0])
+        _need(slots, (n, plan.num_kv_heads), torch.int32, "slots")
+        tensors["slots"] = slots
+    if workspace.device.type != "cuda" or not workspace.is_contiguous():
+        raise MoaError(MOA_ERR_WORKSPACE, "workspace must be a contiguous GPU tensor")
+    tables = moa_page_tables_t(table.data_ptr(), free_pages.data_ptr(), counts.data_ptr(), int(free_pages.shape[0]),
+                               int(page_size), int(table.shape[2]))
+    at = lambda t: None if t is None else t.data_ptr()
+    with torch.cuda.device(_one_device(**tensors)):
+        _check(load_library().moa_paged_assign(
+            plan.handle, ctypes.byref(tables), positions.data_ptr(), at(seq_start), at(fresh), at(slots), bsz, n,
+            workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(table, stream)))
+    return slots
+
+
+# ---------------------------------------------------------------------------
+# Paged cache in 8 bits: k_pages, v_pages [num_pages, page_size, D] float8_e4m3fn, scales
+# [num_pages, page_size / 16, 2] fp32, powers of two: of the keys and of the values of every 16 rows.
+# A number stands for itself times its scale.  Plans are bf16 ones; all else as above.
+# ---------------------------------------------------------------------------
+def new_quant_cache(plan: Plan, num_pages: int, page_size: int = 64, device="cuda"):
+    """(k_pages, v_pages, scales) of `num_pages` pages in 8 bits."""
+    import torch
+    shape = (int(num_pages), int(page_size), plan.head_dim)
+    return (torch.zeros(shape, dtype=torch.float8_e4m3fn, device=device),
+            torch.zeros(shape, dtype=torch.float8_e4m3fn, device=device),
+            torch.zeros((shape[0], shape[1] // MOA_QUANT_BLOCK, 2), dtype=torch.float32, device=device))
+
+
+def moa_quant_append(plan: Plan, k_pages, v_pages, scales, table, q, k_new, v_new, positions, seq_start=None,
+                     inv_freq=None, interleaved: bool = False, q_out=None, stream=None):
+    """moa_paged_append into an 8-bit cache: each block of 16 positions of a head gets the scale that its
+    largest magnitude needs, and one that grows takes the rows in front along (include/moa.h)."""
+    if stream is None:
+        done = _fast.quant_append(plan._bound, k_pages, v_pages, scales, table, q, k_new, v_new, positions, seq_start,
+                                  inv_freq, interleaved, q_out)
+        if done is not None:
+            return None if done is True else done
+    _need_scales(scales)
+    return _append(plan, k_pages, v_pages, scales, table, q, k_new, v_new, positions, seq_start, inv_freq, interleaved,
+                   q_out, stream)
+
+
+def _need_scales(scales):
+    if scales is None:
+        raise MoaError(MOA_ERR_INVALID_ARG, "scales: an 8-bit cache has them")
+
+
+def moa_quant_prefill(plan: Plan, q, k_pages, v_pages, scales, table, positions, seq_start, workspace, o=None,
+                      stream=None):
+    """moa_paged_prefill over an 8-bit cache."""
+    if stream is None:
+        done = _fast.quant_prefill(plan._bound, q, k_pages, v_pages, scales, table, positions, seq_start, workspace, o)
+        if done is not None:
+            return done
+    _need_scales(scales)
+    return _prefill(plan, q, k_pages, v_pages, scales, table, positions, seq_start, workspace, o, stream)
+
+
+def moa_quant_decode(plan: Plan, q, k_pages, v_pages, scales, table, positions, workspace, o=None, stream=None):
+    """moa_paged_decode over an 8-bit cache."""
+    if stream is None:
+        done = _fast.quant_decode(plan._bound, q, k_pages, v_pages, scales, table, positions, workspace, o)
+        if done is not None:
+            return done
+    _need_scales(scales)
+    return _decode(plan, q, k_pages, v_pages, scales, table, positions, workspace, o, stream)
+
+
+def moa_quant_decode_shared(plan: Plan, q, k_pages, v_pages, scales, prefix_table, prefix_len: int, table, positions,
+                            workspace, o=None, stream=None):
+    """moa_paged_decode_shared over an 8-bit cache."""
+    if stream is None:
+        done = _fast.quant_decode_shared(plan._bound, q, k_pages, v_pages, scales, prefix_table, prefix_len, table,
+                                         positions, workspace, o)
+        if done is not None:
+            return done
+    _need_scales(scales)
+    return _decode_shared(plan, q, k_pages, v_pages, scales, prefix_table, prefix_len, table, positions, workspace, o,
+                          stream)
