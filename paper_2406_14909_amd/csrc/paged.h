@@ -64,7 +64,7 @@ struct AssignArgs {
   const int32_t* seq_start;  // null: one token per sequence
   const int32_t* fresh;      // null: none
   int32_t* slots;            // [n_tokens, hkv], or null
-  int64_t* plan;             // workspace: the list's length before step 2, then per pair the pages in front of its own
+  int64_t* plan;             // workspace
   int32_t n_tokens;
   int32_t batch;
   int32_t hkv;
@@ -162,7 +162,7 @@ int launch_paged_merge(const PagedArgs& a, int dtype, int head_dim, void* stream
 int launch_paged_shared(const PagedArgs& a, int dtype, int head_dim, int group, void* stream);
 int launch_paged_decode(const PagedArgs& a, int dtype, int head_dim, int group, void* stream);
 
-int launch_paged_assign(const AssignArgs& a, void* stream);
+int launch_paged_assign(const AssignArgs& a, size_t ws_bytes, void* stream);
 // 8-bit pages, bf16 queries and outputs.
 int launch_quant_append(const QuantAppendArgs& a, int head_dim, void* stream);
 int launch_quant_rows(const PagedArgs& a, int head_dim, int key_groups, int64_t groups, void* stream);

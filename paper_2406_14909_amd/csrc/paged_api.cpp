@@ -515,7 +515,8 @@ moa_status_t moa_paged_assign(const moa_plan_t* plan, const moa_page_tables_t* t
   a.table = tables->table; a.free_pages = tables->free_pages; a.counts = tables->counts;
   a.positions = positions; a.seq_start = seq_start; a.fresh = fresh; a.slots = slots;
   a.plan = static_cast<int64_t*>(workspace);
-  static_assert(kPagedPartPad * sizeof(float) >= 2 * sizeof(int64_t), "a pair's share of the workspace holds its counts");
+  // The workspace has kPagedMaxWorkers rows of head_dim + 4 floats and as many more as there are pairs:
+  // more than the 32 + 24 bytes a pair that the counts and their sums take.
   a.n_tokens = static_cast<int32_t>(n_tokens);
   a.batch = batch;
   a.hkv = d.num_kv_heads;
@@ -525,7 +526,7 @@ moa_status_t moa_paged_assign(const moa_plan_t* plan, const moa_page_tables_t* t
   a.num_sink = d.num_sink;
   a.block_band = (d.flags & MOA_BLOCK_BAND) != 0;
   for (int h = 0; h < d.num_kv_heads; ++h) a.window[h] = plan->window[h];
-  return launched(who, launch_paged_assign(a, hip_stream));
+  return launched(who, launch_paged_assign(a, need, hip_stream));
 }
 
 }  // extern "C"

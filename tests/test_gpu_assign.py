@@ -143,3 +143,20 @@ def test_another_stream():
     torch.cuda.synchronize()
     t.step([0, 3, -1, 0], [0, 100, 150, 150, 400], stream=s)
     t.step([100, 53, 9, 250], None, [0, 0, 1, 0], stream=s)
+
+
+@pytest.mark.parametrize("batch,hkv,width,count", [(9, 4, 60, 700), (4, 32, 100, 1500), (600, 8, 4, 9), (1500, 3, 6, 4),
+                                                   (200, 30, 1500, 25)])
+def test_many_tokens_and_pairs(batch, hkv, width, count):
+    """Rows by a kernel of their own; more pairs than one work-group adds up; tables larger than the
+    workspace holds copies of; sequences without tokens in between."""
+    _say("assign many", batch, hkv, width, count)
+    rng = np.random.default_rng(batch)
+    windows = [int(x) for x in rng.integers(1, 16 * width + 1, hkv)]
+    t = Tables(hkv, windows, 7, 16, batch, width, batch * hkv * min(width, count // 4 + 4))
+    at = rng.integers(-1, 40, batch)
+    counts = rng.integers(0, count, batch) * (rng.random(batch) < 0.7)
+    for step in range(2):
+        t.step(at, 1 + np.concatenate([[0], np.cumsum(counts)]), rng.random(batch) < 0.2 if step else None,
+               rows=int(counts.sum()) + 9)
+        at = np.where(at < 0, at, at + counts)
