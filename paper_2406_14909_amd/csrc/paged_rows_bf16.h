@@ -256,12 +256,16 @@ __device__ __forceinline__ void rows_bf16(const PagedArgs& a, RowsBf16Lds<D, KG>
 #pragma unroll
           for (int e = 0; e < 4; ++e) v_raw[i][e] &= ~((nan_bytes(v_raw[i][e]) >> 7) * 0xffu);
         }
+        // Lanes' chunks lie 32 bytes apart, their halves 16: half of the lanes write the upper one first,
+        // so that those that share a store's pass hit distinct banks.
+        const bool k_flip = (D == 128 ? c >> 3 : r) & 1, v_flip = (D == 128 ? c >> 3 ^ r : r) & 1;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          *reinterpret_cast<bf16x8*>(k_lds + r * RB + (((c + h) ^ TL::swz_k(r)) * 16)) =
-              widen8(u32x2{k_raw[i][2 * h], k_raw[i][2 * h + 1]}, raw_scale[i][0]);
-          *reinterpret_cast<bf16x8*>(v_lds + r * RB + (((c + h) ^ TL::swz_v(r)) * 16)) =
-              widen8(u32x2{v_raw[i][2 * h], v_raw[i][2 * h + 1]}, raw_scale[i][1]);
+          const int kh = h ^ k_flip, vh = h ^ v_flip;
+          *reinterpret_cast<bf16x8*>(k_lds + r * RB + (((c + kh) ^ TL::swz_k(r)) * 16)) =
+              widen8(kh ? u32x2{k_raw[i][2], k_raw[i][3]} : u32x2{k_raw[i][0], k_raw[i][1]}, raw_scale[i][0]);
+          *reinterpret_cast<bf16x8*>(v_lds + r * RB + (((c + vh) ^ TL::swz_v(r)) * 16)) =
+              widen8(vh ? u32x2{v_raw[i][2], v_raw[i][3]} : u32x2{v_raw[i][0], v_raw[i][1]}, raw_scale[i][1]);
         }
       }
     };

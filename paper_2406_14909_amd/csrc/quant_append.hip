@@ -104,21 +104,39 @@ __global__ void __launch_bounds__(kThreads) quant_append_kernel(QuantAppendArgs 
     {
       const int unit = threadIdx.x % UNITS, heads = q1 - q0;
       const Chunks c = chunks_of(a, unit, true);
-      for (int i = threadIdx.x / UNITS; i < heads * len; i += kThreads / UNITS) {
-        const int tok = ROWS == 1 ? 0 : i / heads, h = q0 + (ROWS == 1 ? i : i - tok * heads);
-        const bf16* src = reinterpret_cast<const bf16*>(static_cast<const char*>(a.q) + (t + tok) * a.q_stride) + h * D;
-        bf16* dst = static_cast<bf16*>(a.q_out) + (int64_t(t + tok) * a.hq + h) * D;
-        float x[16];
-        load_chunks(x, src, c);
-        turn(x, c, s_cos[tok], s_sin[tok]);
-        Vec16<bf16> lo, hi;
+      // Four rows of a thread are on their way at once.
+      constexpr int STEP = kThreads / UNITS, AHEAD = ROWS == 1 ? 1 : 4;
+      for (int i0 = threadIdx.x / UNITS; i0 < heads * len; i0 += AHEAD * STEP) {
+        Vec16<bf16> lo[AHEAD], hi[AHEAD];
+        int tok[AHEAD], h[AHEAD];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          lo.set(e, x[e]);
-          hi.set(e, x[8 + e]);
+        for (int n = 0; n < AHEAD; ++n) {
+          const int i = min(i0 + n * STEP, heads * len - 1);
+          tok[n] = ROWS == 1 ? 0 : i / heads;
+          h[n] = q0 + i - tok[n] * heads;
+          const bf16* src = reinterpret_cast<const bf16*>(static_cast<const char*>(a.q) + (t + tok[n]) * a.q_stride) + h[n] * D;
+          lo[n] = load16(src + c.e0);
+          hi[n] = load16(src + c.e1);
         }
-        *reinterpret_cast<bf16x8*>(dst + c.e0) = lo.v;
-        *reinterpret_cast<bf16x8*>(dst + c.e1) = hi.v;
+#pragma unroll
+        for (int n = 0; n < AHEAD; ++n) {
+          if (i0 + n * STEP >= heads * len) break;
+          bf16* dst = static_cast<bf16*>(a.q_out) + (int64_t(t + tok[n]) * a.hq + h[n]) * D;
+          float x[16];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            x[e] = lo[n].get(e);
+            x[8 + e] = hi[n].get(e);
+          }
+          turn(x, c, s_cos[tok[n]], s_sin[tok[n]]);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            lo[n].set(e, x[e]);
+            hi[n].set(e, x[8 + e]);
+          }
+          *reinterpret_cast<bf16x8*>(dst + c.e0) = lo[n].v;
+          *reinterpret_cast<bf16x8*>(dst + c.e1) = hi[n].v;
+        }
       }
     }
     const int64_t page_index = pos >> a.page_shift;

@@ -57,16 +57,25 @@ __device__ __forceinline__ void decode_quant(const PagedArgs& a, QuantLds<D>& ld
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) rd_off[dt] = vr * RB + ((dt ^ SW::swv(vr)) << 5) + 8 * (lane & 3);
   }
-  // LDS places of a lane's chunk of load u: its two halves of 8 keys (K) or all of it (V), the same
-  // every second load but for the rows in front.
+  // LDS places of the two halves of a lane's chunk of load u, the same every second load but for the
+  // rows in front.  The halves lie 16 bytes apart and lanes 32, so that half of the lanes write the upper one
+  // first: those that share a store's pass hit distinct banks.
   int kw[2][2], vw[2];
+  const int r8 = lane / CPR, c8 = lane % CPR;
+  const bool k_flip = (D == 128 ? c8 >> 2 : r8) & 1;
+  const bool v_flip = (D == 128 ? (c8 ^ SW::swv(r8)) >> 2 ^ r8 : r8) & 1;
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
-    const int r = u * RPL + lane / CPR, c = lane % CPR;
+    const int r = u * RPL + r8;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) kw[u][h] = lane / CPR * RB + (((2 * c + h) ^ SW::swk(r)) << 4);
-    vw[u] = lane / CPR * RB + ((c ^ SW::swv(r)) << 5);
+    for (int h = 0; h < 2; ++h) kw[u][h] = r8 * RB + (((2 * c8 + (h ^ k_flip)) ^ SW::swk(r)) << 4);
   }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) vw[h] = r8 * RB + ((c8 ^ SW::swv(r8)) << 5) + ((h ^ v_flip) << 4);
+  auto half = [](const u32x4& x, int h, bool flip) {
+    const u32x2 lo = {x[0], x[1]}, hi = {x[2], x[3]};
+    return (h == 0) == flip ? hi : lo;
+  };
 
   for_each_piece(a, s_walk, w, TL::kRoundShift, [&](int b, int g, const VisibleKeys& keys, int x0, int x1, bool whole, int pair) {
     bf16x8 qop[KS];               // B = Q^T: lane holds column n, dims 32*kk + 8*q4 .. +7
@@ -122,7 +131,7 @@ __device__ __forceinline__ void decode_quant(const PagedArgs& a, QuantLds<D>& ld
           const float f = __shfl(sc[0], u * RPL + lane / CPR, 64);
 #pragma unroll
           for (int h = 0; h < 2; ++h)
-            *reinterpret_cast<bf16x8*>(ts + kw[u & 1][h] + u * RPL * RB) = widen8(u32x2{kr[u][2 * h], kr[u][2 * h + 1]}, f);
+            *reinterpret_cast<bf16x8*>(ts + kw[u & 1][h] + u * RPL * RB) = widen8(half(kr[u], h, k_flip), f);
         }
         if (more) load(kbase, rows, kr);
         sched_fence();
@@ -178,9 +187,9 @@ __device__ __forceinline__ void decode_quant(const PagedArgs& a, QuantLds<D>& ld
 #pragma unroll
         for (int u = 0; u < LD; ++u) {
           const float f = __shfl(sc[1], u * RPL + lane / CPR, 64);
-          bf16x8* const at = reinterpret_cast<bf16x8*>(ts + vw[u & 1] + u * RPL * RB);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) at[h] = widen8(u32x2{vr[u][2 * h], vr[u][2 * h + 1]}, f);
+          for (int h = 0; h < 2; ++h)
+            *reinterpret_cast<bf16x8*>(ts + vw[h] + u * RPL * RB) = widen8(half(vr[u], h, v_flip), f);
         }
         if (more) load(vbase, rows, vr);
         sched_fence();
