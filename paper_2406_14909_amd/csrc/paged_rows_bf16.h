@@ -230,10 +230,10 @@ __device__ __forceinline__ void rows_bf16(const PagedArgs& a, RowsBf16Lds<D, KG>
     constexpr int CP8 = D / 16, LD8 = 16 * CP8 / 64, RP8 = 64 / CP8;
     u32x4 k_raw[LD8], v_raw[LD8];
     f32x2 raw_scale[LD8];
-    auto load_raw = [&](int j0, const Pages& pages) {
+    auto load_raw = [&](int j0, int my_page) {
       const int kb = j0 + 16 * wave;
       const bool full = group_full(kb);
-      const int page = full ? mine(pages) : scalar_read(table, uniform(seen_of(kb, kb, j0)) >> a.page_shift);
+      const int page = full ? my_page : scalar_read(table, uniform(seen_of(kb, kb, j0)) >> a.page_shift);
       const int r = page_row(page, a.num_pages, a.page_shift);
 #pragma unroll
       for (int i = 0; i < LD8; ++i) {
@@ -307,26 +307,49 @@ __device__ __forceinline__ void rows_bf16(const PagedArgs& a, RowsBf16Lds<D, KG>
       int jt = 0, j1 = 0, j2 = 0;
       Pages pt = {}, p1 = {}, p2 = {};
       const int ts = t0 + kg;               // the group's first
-      if (ts < t1) {
-        jt = tile_j0(ts);
-        pt = fetch(jt);
-        if constexpr (k8) {
-          load_raw(jt, pt);
+      // 8-bit pages: the page numbers of the group's next 16 tiles, a lane for every 16 keys, and of
+      // the 16 behind them.  (Read by scalar loads, as below, they would be waited for with every LDS read
+      // that follows, as the two share a counter and come out of order.)
+      int pages_now = 0, pages_next = 0, nth = 2, ok_t = 0, ok_1 = 0;       // nth: the group's tile two on
+      auto load_pages = [&](int block) {
+        const int t = ts + (16 * block + (lane >> 2)) * KG;
+        return t < t1 ? table[min(tile_j0(t) + 16 * (lane & 3), key_end - 1) >> a.page_shift] : -1;
+      };
+      auto page_of = [&](int n) { return __builtin_amdgcn_readlane(pages_now, (n & 15) * 4 + wave); };
+      auto there_of = [&](int n) {          // a bit for each of its groups of keys
+        const uint64_t all = __ballot(static_cast<uint32_t>(pages_now) < static_cast<uint32_t>(a.num_pages));
+        return static_cast<int>(all >> ((n & 15) * 4)) & 15;
+      };
+      if constexpr (k8) {
+        if (ts < t1) {
+          pages_now = load_pages(0);
+          pages_next = load_pages(1);
+          jt = tile_j0(ts);
+          load_raw(jt, page_of(0));
+          ok_t = there_of(0);
           store_raw(sK, sV, careful);
-        } else {
+        }
+        if (ts + KG < t1) {
+          j1 = tile_j0(ts + KG);
+          load_raw(j1, page_of(1));
+          ok_1 = there_of(1);
+        }
+      } else {
+        if (ts < t1) {
+          jt = tile_j0(ts);
+          pt = fetch(jt);
           tile_dma(a.vp, v_src, jt, pt, sV);
           tile_dma(a.kp, k_src, jt, pt, sK);
         }
-      }
-      if (ts + KG < t1) {
-        j1 = tile_j0(ts + KG);
-        p1 = fetch(j1);
-        if constexpr (k8) load_raw(j1, p1);
-        else tile_dma(a.kp, k_src, j1, p1, sK + TL::TILE_BYTES);
-      }
-      if (ts + 2 * KG < t1) {
-        j2 = tile_j0(ts + 2 * KG);
-        p2 = fetch(j2);
+        if (ts + KG < t1) {
+          j1 = tile_j0(ts + KG);
+          p1 = fetch(j1);
+          tile_dma(a.kp, k_src, j1, p1, sK + TL::TILE_BYTES);
+        }
+        if (ts + 2 * KG < t1) {
+          j2 = tile_j0(ts + 2 * KG);
+          p2 = fetch(j2);
+        }
       }
       int k_now = 0, k_next = (KST - 1) * TL::TILE_BYTES, v_now = 0;      // byte offsets of stages
       // Wait for Q (and the first tiles) here, once: the compiler does not count the direct
@@ -334,7 +357,7 @@ __device__ __forceinline__ void rows_bf16(const PagedArgs& a, RowsBf16Lds<D, KG>
       if constexpr (!k8) __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
       for (int t = ts; t < t1 + kg; t += KG) {            // as many rounds for every group
         const int j0 = jt;
-        const int ok = present(pt);
+        const int ok = k8 ? ok_t : present(pt);
         if constexpr (!k8) {
           if (t + KG < t1) __builtin_amdgcn_s_waitcnt(0x0F70 | DPW);  // the next K may be in flight
           else __builtin_amdgcn_s_waitcnt(0x0F70);
@@ -352,9 +375,11 @@ __device__ __forceinline__ void rows_bf16(const PagedArgs& a, RowsBf16Lds<D, KG>
         __syncthreads();                      // K(t), V(t) are there for every wave; K(t-1), V(t-1) are free
         Pages p3 = {};
         int j3 = 0;
-        if (t + 3 * KG < t1) {
-          j3 = tile_j0(t + 3 * KG);
-          p3 = fetch(j3);
+        if constexpr (!k8) {
+          if (t + 3 * KG < t1) {
+            j3 = tile_j0(t + 3 * KG);
+            p3 = fetch(j3);
+          }
         }
 
         // Does any (row, key) pair of this wave fall inside the mask?
@@ -366,7 +391,19 @@ __device__ __forceinline__ void rows_bf16(const PagedArgs& a, RowsBf16Lds<D, KG>
         if constexpr (k8) {
           // The next tile, asked for a tile ago, goes to the other stage, and the one behind it is asked for.
           if (t + KG < t1) store_raw(sK + (v_now ^ TL::TILE_BYTES), sV + (v_now ^ TL::TILE_BYTES), careful);
-          if (t + 2 * KG < t1) load_raw(j2, p2);
+          if (t + 2 * KG < t1) {
+            if ((nth & 15) == 0) {
+              pages_now = pages_next;
+              pages_next = load_pages((nth >> 4) + 1);
+            }
+            j2 = tile_j0(t + 2 * KG);
+            load_raw(j2, page_of(nth));
+            ok_t = ok_1;
+            ok_1 = there_of(nth);
+            ++nth;
+          } else {
+            ok_t = ok_1;
+          }
         } else if (!spread) {
           if (t + KG < t1) tile_dma(a.vp, v_src, j1, p1, sV + (v_now ^ TL::TILE_BYTES));
           if (t + 2 * KG < t1) tile_dma(a.kp, k_src, j2, p2, sK + k_next);
