@@ -88,8 +88,9 @@ __device__ __forceinline__ RowPair row_pair(const PagedArgs& a, int pair) {
 }
 
 // Calls tile(item) for each row tile that work-group `block` of WAVES waves has a part in.
-// Work-group uniform; `tile` ends with a barrier where LDS is used again.
-template <int ROWS, int WAVES, class Tile>
+// Work-group uniform; `tile` ends with a barrier where LDS is used again.  kWhole: of a launch without pieces
+// (a.plan null), whose code then has one copy of `tile`.
+template <int ROWS, int WAVES, bool kWhole = false, class Tile>
 __device__ __forceinline__ void for_each_row_tile(const PagedArgs& a, int block, RowPlanLds& s, Tile&& tile) {
   constexpr int kThreads = WAVES * 64;
   const int pairs = a.batch * a.hkv;
@@ -161,7 +162,7 @@ __device__ __forceinline__ void for_each_row_tile(const PagedArgs& a, int block,
   // Whole row tiles, where the longest takes little more than an equal share of the work.
   PagedSeg* const segs = reinterpret_cast<PagedSeg*>(a.plan);
   const int worth = 4 * all >= 3 * a.slots ? a.full_cost : a.whole_cost;
-  if (a.plan == nullptr || (longest - worth) * a.slots <= units) {
+  if (kWhole || a.plan == nullptr || (longest - worth) * a.slots <= units) {
     if (a.plan != nullptr && block < a.slots && threadIdx.x == 0) segs[block].rows = 0;
     // Dealt to the dies in units of 16 neighbours, one unit to each die in turn and back
     // again; few singly.  Of a pair the last first: theirs are the most keys.
@@ -186,6 +187,8 @@ __device__ __forceinline__ void for_each_row_tile(const PagedArgs& a, int block,
     tile(item_of(p, i, 0, 1, 1, -1));
     return;
   }
+
+  if constexpr (kWhole) return;
 
   // Pieces.  Workers of neighbouring pieces sit on one die.
   const RowSplit split = row_split(units, a.least_cost, a.log_slots);

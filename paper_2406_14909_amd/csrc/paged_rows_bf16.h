@@ -229,20 +229,34 @@ __device__ __forceinline__ void rows_bf16(const PagedArgs& a, RowsBf16Lds<D, KG>
     // L / CP8 (+ 64 / CP8) of the group, and what they become in LDS.
     constexpr int CP8 = D / 16, LD8 = 16 * CP8 / 64, RP8 = 64 / CP8;
     u32x4 k_raw[LD8], v_raw[LD8];
-    f32x2 raw_scale[LD8];
+    f32x2 raw_scale;
     auto load_raw = [&](int j0, int my_page) {
       const int kb = j0 + 16 * wave;
-      const bool full = group_full(kb);
-      const int page = full ? my_page : scalar_read(table, uniform(seen_of(kb, kb, j0)) >> a.page_shift);
-      const int r = page_row(page, a.num_pages, a.page_shift);
+      if (group_full(kb) && static_cast<uint32_t>(my_page) < static_cast<uint32_t>(a.num_pages)) {
+        // Rows that follow one another: scalar addresses, and one block's scales.
+        const int64_t row = (int64_t(my_page) << a.page_shift) + (kb & ps_mask);
+        const char* const k = static_cast<const char*>(a.kp) + row * D;
+        const char* const v = static_cast<const char*>(a.vp) + row * D;
+        raw_scale = reinterpret_cast<const f32x2*>(a.scales)[row / kQuantBlock];
+        const uint32_t at = lane * 16;
+#pragma unroll
+        for (int i = 0; i < LD8; ++i) {
+          k_raw[i] = *reinterpret_cast<const u32x4*>(k + i * 1024 + at);
+          v_raw[i] = *reinterpret_cast<const u32x4*>(v + i * 1024 + at);
+        }
+        return;
+      }
+      // A row that no row of the tile sees is a neighbour's.  The scales are those of the group's block, or, where
+      // none of it is seen, of that neighbour's.
+      const int j = uniform(seen_of(kb, kb, j0));
+      const int r = page_row(scalar_read(table, j >> a.page_shift), a.num_pages, a.page_shift);
+      raw_scale = f32x2{1.0f, 1.0f};
+      if (r >= 0) raw_scale = reinterpret_cast<const f32x2*>(a.scales)[(r + (j & ps_mask)) / kQuantBlock];
 #pragma unroll
       for (int i = 0; i < LD8; ++i) {
-        const int j = kb + i * RP8 + lane / CP8;
-        const int64_t row = int64_t(max(r, 0)) + ((full ? j : seen_of(j, kb, j0)) & ps_mask);
-        raw_scale[i] = f32x2{1.0f, 1.0f};
+        const int64_t row = int64_t(max(r, 0)) + (seen_of(kb + i * RP8 + lane / CP8, kb, j0) & ps_mask);
         k_raw[i] = v_raw[i] = u32x4{};
         if (r >= 0) {                         // absent pages are zeros
-          raw_scale[i] = reinterpret_cast<const f32x2*>(a.scales)[row / kQuantBlock];
           k_raw[i] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.kp) + row * D + lane % CP8 * 16);
           v_raw[i] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.vp) + row * D + lane % CP8 * 16);
         }
@@ -263,9 +277,9 @@ __device__ __forceinline__ void rows_bf16(const PagedArgs& a, RowsBf16Lds<D, KG>
         for (int h = 0; h < 2; ++h) {
           const int kh = h ^ k_flip, vh = h ^ v_flip;
           *reinterpret_cast<bf16x8*>(k_lds + r * RB + (((c + kh) ^ TL::swz_k(r)) * 16)) =
-              widen8(kh ? u32x2{k_raw[i][2], k_raw[i][3]} : u32x2{k_raw[i][0], k_raw[i][1]}, raw_scale[i][0]);
+              widen8(kh ? u32x2{k_raw[i][2], k_raw[i][3]} : u32x2{k_raw[i][0], k_raw[i][1]}, raw_scale[0]);
           *reinterpret_cast<bf16x8*>(v_lds + r * RB + (((c + vh) ^ TL::swz_v(r)) * 16)) =
-              widen8(vh ? u32x2{v_raw[i][2], v_raw[i][3]} : u32x2{v_raw[i][0], v_raw[i][1]}, raw_scale[i][1]);
+              widen8(vh ? u32x2{v_raw[i][2], v_raw[i][3]} : u32x2{v_raw[i][0], v_raw[i][1]}, raw_scale[1]);
         }
       }
     };
@@ -704,7 +718,7 @@ __device__ __forceinline__ void rows_bf16(const PagedArgs& a, RowsBf16Lds<D, KG>
     const PagedItem it = uniform(prefix_item<kRowsBf16>(a, w));
     if (it.rows > 0) tile(it);
   } else {
-    for_each_row_tile<kRowsBf16, 4 * KG>(a, w, *reinterpret_cast<RowPlanLds*>(lds.tiles), tile);
+    for_each_row_tile<kRowsBf16, 4 * KG, k8 && KG == 2>(a, w, *reinterpret_cast<RowPlanLds*>(lds.tiles), tile);
   }
 }
 
