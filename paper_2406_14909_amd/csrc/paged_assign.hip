@@ -211,6 +211,7 @@ __global__ void __launch_bounds__(kThreads) paged_take_kernel(AssignArgs a) {
   const int pairs = a.batch * a.hkv;
   const Space ws(a);
   const int p = static_cast<int>(blockIdx.x) * kWaves + wave;
+  const Pair r = pair_of(a, min(p, pairs - 1));           // asked for along with the counts
   const int64_t n = ws.head[0];
   int64_t listed, all_need;
   if constexpr (kStash) {
@@ -261,11 +262,6 @@ __global__ void __launch_bounds__(kThreads) paged_take_kernel(AssignArgs a) {
     a.counts[1] = static_cast<int>(min(max(all_need - listed, int64_t(0)), int64_t(0x7fffffff)));
   }
   if (p >= pairs) return;
-  if constexpr (kStash) {
-    const int first = s_gone[p], mine = s_gone[p + 1] - first;
-    for (int i = lane; i < mine; i += 64)
-      if (n + first + i < a.num_pages) a.free_pages[n + first + i] = ws.stash[int64_t(p) * a.max_pages + i];
-  }
   // Page i of the list as step 1 leaves it: what this call has put there may still be under way.
   auto page = [&](int64_t i) {
     if constexpr (!kStash) return a.free_pages[i];
@@ -279,23 +275,39 @@ __global__ void __launch_bounds__(kThreads) paged_take_kernel(AssignArgs a) {
     }
     return ws.stash[int64_t(lo) * a.max_pages + k - s_gone[lo]];
   };
-  const Pair r = pair_of(a, p);
   int32_t* table = a.table + int64_t(p) * a.max_pages;
   int64_t at = listed - 1;
   if constexpr (kStash) at -= s_need[p];
   else at -= ws.sums[2 * p + 1];
+  const bool rows = a.slots != nullptr && a.n_tokens < kManyTokens;
+  const int64_t end = r.pos + r.tokens;
+  auto write_rows = [&](int64_t lo, int64_t hi, auto entry_of) {      // of the tokens at positions lo .. hi - 1
+    for (int64_t x = lo; x < hi; x += 64) {
+      const int64_t pos = x + lane;
+      const int entry = entry_of(pos);
+      if (pos < hi) a.slots[(r.row + pos - r.pos) * a.hkv + r.g] = row_of_pool(a, entry, pos);
+    }
+  };
   for (int i = r.need_lo; i < r.need_hi; i += 64) {
-    const bool need = i + lane < r.need_hi && !present(a, table[i + lane]);
+    const bool in = i + lane < r.need_hi;
+    int entry = r.fresh || !in ? -1 : table[i + lane];
+    const bool need = in && !present(a, entry);
     const uint64_t which = __ballot(need);
     const int64_t from = at - below(which);
-    if (need && from >= 0) table[i + lane] = page(from);
+    if (need && from >= 0) {
+      entry = page(from);
+      table[i + lane] = entry;
+    }
     at -= __builtin_popcountll(which);
+    if (rows)
+      write_rows(max(r.pos, int64_t(i) << a.page_shift), min(end, int64_t(i + 64) << a.page_shift),
+                 [&](int64_t pos) { return __shfl(entry, static_cast<int>(pos >> a.page_shift) - i, 64); });
   }
-  if (a.slots == nullptr || a.n_tokens >= kManyTokens) return;
-  __threadfence_block();                  // the wave reads what its lanes have written
-  for (int64_t t = lane; t < r.tokens; t += 64) {
-    const int64_t pos = r.pos + t, i = pos >> a.page_shift;
-    a.slots[(r.row + t) * a.hkv + r.g] = row_of_pool(a, i < a.max_pages ? table[i] : -1, pos);
+  if (rows) write_rows(max(r.pos, int64_t(a.max_pages) << a.page_shift), end, [](int64_t) { return -1; });
+  if constexpr (kStash) {
+    const int first = s_gone[p], mine = s_gone[p + 1] - first;
+    for (int i = lane; i < mine; i += 64)
+      if (n + first + i < a.num_pages) a.free_pages[n + first + i] = ws.stash[int64_t(p) * a.max_pages + i];
   }
 }
 
