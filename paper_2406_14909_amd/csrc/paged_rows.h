@@ -274,15 +274,19 @@ __device__ __forceinline__ PagedItem prefix_item(const PagedArgs& a, int w) {
 }
 
 // What work-group `block` of a launch over a shared prefix does: an item of the prefix, or a worker's
-// piece of the keys behind it.  The two kinds alternate, in eights, so that every die and most compute
-// units have both.  Neighbours of the prefix's items share a die.
+// piece of the keys behind it.  The two kinds alternate, in eights, or (kFirst) the prefix comes first:
+// a die's work-groups go to its compute units in turn, so that each then has one of either kind (of those
+// that alternate, an even number of units away, two of one).  Neighbours of the prefix's items share a die.
 struct SharedWork {
   bool prefix;
   int index;
 };
+template <bool kFirst = false>
 __device__ __forceinline__ SharedWork shared_work(const PagedArgs& a, int block) {
   const int prefix = (a.prefix_items + kNumXcd - 1) / kNumXcd, own = (a.slots + kNumXcd - 1) / kNumXcd;
   const int eight = block / kNumXcd, die = block % kNumXcd;
+  if constexpr (kFirst)
+    return eight < prefix ? SharedWork{true, die * prefix + eight} : SharedWork{false, (eight - prefix) * kNumXcd + die};
   const int both = 2 * min(prefix, own);
   const bool is_prefix = eight < both ? eight % 2 == 0 : prefix > own;
   const int nth = eight < both ? eight / 2 : eight - both / 2;     // of its kind on this die

@@ -1,5 +1,16 @@
 // Decode of a batch over a prefix that its sequences share, in an 8-bit cache, and over what each
-// has behind it: the two kinds of work of one launch and the merge of paged_shared.hip.
+// has behind it: the two kinds of work of one launch and the merge of paged_shared.hip, with a work-group of
+// either kind on each compute unit.  Bound by the longest chain: a piece of the prefix is a dozen key tiles
+// one after the other, at 3,600 cycles each (48 sequences x 8 heads x 8 query heads over 32,700 shared
+// keys and up to 1,000 of their own: 41 us, 7 of them the merge; 46 with the kinds in turns).  More and
+// shorter pieces, or more work-groups for either kind, help some batches and cost others (sequences x KV heads x
+// query heads of each on a prefix, with up to so many keys of their own; work-groups for prefix and own keys; us):
+//                                   256 + 256   320 + 192   192 + 320   256 + 384
+//   48 x 8 x 8 on 32,700, 1,000          44.3        47.6        50.1        48.5
+//   16 x 8 x 4 on 8,001, 500             16.5        16.5        16.5        16.5
+//   16 x 32 x 1 on 8,001, 500            25.9        29.5        25.8        31.2
+//   48 x 32 x 1 on 8,001, 1,500           105         131          97         100
+//   32 x 8 x 4 on 2,000, 4,000           29.3        33.0        28.2        26.8
 #include "paged_rows_bf16.h"
 #include "quant_decode.h"
 
@@ -13,7 +24,7 @@ __global__ void __launch_bounds__(kThreads, 2) quant_shared_kernel(PagedArgs a) 
     QuantLds<D> decode;
     RowsBf16Lds<D, 1> rows;
   } lds;
-  const SharedWork work = shared_work(a, blockIdx.x);
+  const SharedWork work = shared_work<true>(a, blockIdx.x);
   if (work.prefix) rows_bf16<D, true, 1, true>(a, lds.rows, work.index);
   else decode_quant<D, G>(a, lds.decode, work.index);
 }
