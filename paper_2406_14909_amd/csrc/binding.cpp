@@ -599,7 +599,8 @@ PyObject* paged_assign(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   const at::Tensor* ss = args[7] != Py_None ? c(args[7], at::kInt, {bsz + 1}) : nullptr;
   const at::Tensor* fr = args[8] != Py_None ? c(args[8], at::kInt, {bsz}) : nullptr;
   const at::Tensor* sl = args[9] != Py_None ? c.any(args[9]) : nullptr;
-  if (sl && (sl->dim() != 2 || sl->scalar_type() != at::kInt || sl->size(1) != b->hkv)) return none();
+  if (sl && (sl->dim() != 2 || sl->scalar_type() != at::kInt || sl->size(1) != b->hkv || (!ss && sl->size(0) != bsz)))
+    return none();
   if (!c.done() || bsz > INT32_MAX || mp > INT32_MAX) return none();
   auto at_ = [](const at::Tensor* x) { return x ? static_cast<int32_t*>(x->data_ptr()) : nullptr; };
   const moa_page_tables_t tables = {at_(t), at_(f), at_(n2), f->size(0), static_cast<int32_t>(page), static_cast<int32_t>(mp)};

@@ -162,6 +162,7 @@ int launch_paged_merge(const PagedArgs& a, int dtype, int head_dim, void* stream
 int launch_paged_shared(const PagedArgs& a, int dtype, int head_dim, int group, void* stream);
 int launch_paged_decode(const PagedArgs& a, int dtype, int head_dim, int group, void* stream);
 
+constexpr int64_t kMaxGridThreads = int64_t(1) << 32;   // of one launch, along one axis
 int launch_paged_assign(const AssignArgs& a, size_t ws_bytes, void* stream);
 // 8-bit pages, bf16 queries and outputs.
 int launch_quant_append(const QuantAppendArgs& a, int head_dim, void* stream);

@@ -351,13 +351,15 @@ int launch_paged_assign(const AssignArgs& a, size_t ws_bytes, void* stream) {
                            static_cast<hipStream_t>(stream));
   };
   const int64_t pairs = int64_t(a.batch) * a.hkv, groups = (pairs + kWaves - 1) / kWaves;
+  const int64_t row_groups = a.slots == nullptr ? 0 : (int64_t(a.n_tokens) + kSlotTokens - 1) / kSlotTokens;
+  if (row_groups * kThreads >= kMaxGridThreads) return kGridTooLarge;      // nothing is launched
   const bool few = pairs <= kFewPairs && 32 + pairs * (8 + int64_t(4) * a.max_pages) <= static_cast<int64_t>(ws_bytes);
   hipError_t e = few ? run(&paged_count_kernel<true>, groups, kThreads) : run(&paged_count_kernel<false>, groups, kThreads);
   if (e == hipSuccess && !few) e = run(&paged_scan_kernel, 1, kScanThreads);
   if (e == hipSuccess && !few) e = run(&paged_release_kernel, groups, kThreads);
   if (e == hipSuccess) e = few ? run(&paged_take_kernel<true>, groups, kThreads) : run(&paged_take_kernel<false>, groups, kThreads);
   if (e == hipSuccess && a.slots != nullptr && a.n_tokens >= kManyTokens)
-    e = run(&paged_slots_kernel, (int64_t(a.n_tokens) + kSlotTokens - 1) / kSlotTokens, kThreads);
+    e = run(&paged_slots_kernel, row_groups, kThreads);
   return static_cast<int>(e);
 }
 

@@ -237,6 +237,7 @@ int launch_t(const QuantAppendArgs& args, void* stream) {
   // middle of a block leave at once.
   int span = a.seq_start != nullptr && a.n_tokens >= kQuantBlock * int64_t(a.batch) ? kQuantBlock : 1;
   const int64_t runs = (int64_t(a.n_tokens) + span - 1) / span;
+  if (runs * kThreads >= kMaxGridThreads) return kGridTooLarge;
   // Heads over four work-groups (8,190 tokens of 64/8 heads: over 2, 4 and 8 79.7, 77.0 and 90.4 us).
   const int parts = runs >= 2048 || a.hkv < 4 ? 1 : 4;
   void* params[] = {&copy, &span};

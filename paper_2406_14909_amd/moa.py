@@ -777,7 +777,7 @@ def moa_paged_assign(plan: Plan, table, free_pages, counts, page_size: int, posi
     if slots is not None:
         _need_rank(slots, 2, "slots")
         n = int(slots.shape[0])
-        _need(slots, (n, plan.num_kv_heads), torch.int32, "slots")
+        _need(slots, (n if seq_start is not None else bsz, plan.num_kv_heads), torch.int32, "slots")
         tensors["slots"] = slots
     if workspace.device.type != "cuda" or not workspace.is_contiguous():
         raise MoaError(MOA_ERR_WORKSPACE, "workspace must be a contiguous GPU tensor")

@@ -330,7 +330,8 @@ def test_refusals_of_attention_and_tables():
                      ((t, free, counts[:1], 16, at, sv.ws), "counts: expected shape"), ((t, free, counts, 24, at, sv.ws), "page_size"),
                      ((t, free, counts, 16, at.long(), sv.ws), "positions"), ((t, free, counts, 16, at, sv.ws[:512]), "workspace"),
                      ((t, free, counts, 16, at, sv.ws, start[:2]), "seq_start"), ((t, free, counts, 16, at, sv.ws, None, at[:2]), "fresh"),
-                     ((t, free, counts, 16, at, sv.ws, None, None, torch.zeros((4, 2), dtype=torch.int32, device="cuda")), "one token"),
+                     ((t, free, counts, 16, at, sv.ws, None, None, torch.zeros((4, 2), dtype=torch.int32, device="cuda")), "slots: expected shape"),
+                     ((t, free, counts, 16, at, sv.ws, None, None, torch.zeros((0, 2), dtype=torch.int32, device="cuda")), "slots: expected shape"),
                      ((t, free, counts, 16, at, sv.ws, start, None, torch.zeros((3, 3), dtype=torch.int32, device="cuda")), "slots"),
                      ((t, t.view(-1), counts, 16, at, sv.ws), "overlaps")):
         with pytest.raises(M.MoaError, match=match):

@@ -122,3 +122,9 @@ def test_no_tokens_are_nothing_to_do():
     none = dict(q=None, k_new=None, v_new=None, q_out=None, o=None)
     assert call("append", plan(), n=0, **none) == M.MOA_OK
     assert call("prefill", plan(), n=0, workspace=None, ws_bytes=0, **none) == M.MOA_OK
+
+
+def test_more_tokens_than_one_launch_takes_are_refused():
+    many = 1 << 29
+    assert call("append", plan(), n=many) == UNSUP and "too much" in lib.moa_last_error().decode()
+    assert call("assign", plan(), n=many) == UNSUP and "too much" in lib.moa_last_error().decode()
