@@ -80,7 +80,14 @@ struct RowsBf16Lds {
 // Work-group w of a launch over ragged chunks, or (kShared) over a shared prefix.  KG groups
 // of 4 waves share its rows: group kg takes key tiles kg, kg + KG, ... through LDS stages of
 // its own, and their states meet in LDS at the end.
-// k8: over 8-bit pages, which pass through registers on their way to LDS and are bf16 there.
+//
+// k8: over 8-bit pages.  A wave's 16 rows of a tile pass through its registers, asked for a tile ahead, and
+// are widened to bf16 as it writes them to LDS, once for all waves; the rest is the same.  2 prompts of
+// 12,000 tokens of 32 heads: 592 us, 861 TFLOP/s, as bf16 pages have; 6 chunks of 8 x 4 heads behind
+// up to 16,000: 178 us; 500 tokens: 18.9 us.  (Direct loads, and keys widened by every wave as it reads
+// its operands: 727 us for the prompts; direct loads of the wave's own rows, widened from LDS to LDS: 733; the
+// widening between the S products instead of in front of them: 617, where 626 were had without, and 23.2
+// for 20.5 of the short prompt.)
 template <int D, bool kShared, int KG, bool k8 = false>
 __device__ __forceinline__ void rows_bf16(const PagedArgs& a, RowsBf16Lds<D, KG>& lds, int w) {
   using TL = RowTiles<D>;
@@ -270,16 +277,12 @@ __device__ __forceinline__ void rows_bf16(const PagedArgs& a, RowsBf16Lds<D, KG>
 #pragma unroll
           for (int e = 0; e < 4; ++e) v_raw[i][e] &= ~((nan_bytes(v_raw[i][e]) >> 7) * 0xffu);
         }
-        // Lanes' chunks lie 32 bytes apart, their halves 16: half of the lanes write the upper one first,
-        // so that those that share a store's pass hit distinct banks.
-        const bool k_flip = (D == 128 ? c >> 3 : r) & 1, v_flip = (D == 128 ? c >> 3 ^ r : r) & 1;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int kh = h ^ k_flip, vh = h ^ v_flip;
-          *reinterpret_cast<bf16x8*>(k_lds + r * RB + (((c + kh) ^ TL::swz_k(r)) * 16)) =
-              widen8(kh ? u32x2{k_raw[i][2], k_raw[i][3]} : u32x2{k_raw[i][0], k_raw[i][1]}, raw_scale[0]);
-          *reinterpret_cast<bf16x8*>(v_lds + r * RB + (((c + vh) ^ TL::swz_v(r)) * 16)) =
-              widen8(vh ? u32x2{v_raw[i][2], v_raw[i][3]} : u32x2{v_raw[i][0], v_raw[i][1]}, raw_scale[1]);
+          *reinterpret_cast<bf16x8*>(k_lds + r * RB + (((c + h) ^ TL::swz_k(r)) * 16)) =
+              widen8(u32x2{k_raw[i][2 * h], k_raw[i][2 * h + 1]}, raw_scale[0]);
+          *reinterpret_cast<bf16x8*>(v_lds + r * RB + (((c + h) ^ TL::swz_v(r)) * 16)) =
+              widen8(u32x2{v_raw[i][2 * h], v_raw[i][2 * h + 1]}, raw_scale[1]);
         }
       }
     };

@@ -1,11 +1,19 @@
 // Decode over an 8-bit paged cache: the split, the walk and the merge of paged_decode.h, over
 // half the bytes.
 //
-// A wave's tile is 64 keys, so that as many bytes are on their way as of 32 keys in bf16.  Keys and
-// values are e4m3 numbers times a scale of their 16 rows: a lane that holds 16 of a row turns them
-// into bf16, exactly, as it writes them to LDS, and from there on the products are those of bf16
-// pages: S^T = K Q^T and O^T += V^T P^T in 16x16x32 matrix instructions, query heads padded to 16
-// columns.
+// Keys and values are e4m3 numbers times a scale of their 16 rows: a lane that holds 16 of a row
+// turns them into bf16, exactly and in 8 instructions, as it writes them to LDS, and from there on the
+// products are those of bf16 pages: S^T = K Q^T and O^T += V^T P^T in 16x16x32 matrix instructions, query
+// heads padded to 16 columns.  (The 8-bit matrix instructions take no bf16 queries; of queries in
+// two 8-bit parts they need as long as bf16 ones, and add up less exactly: 1.4e-4 of a sum's magnitudes.)
+//
+// Bound by memory.  A wave's tile is 64 keys, so that as many bytes are on their way as of 32 keys in
+// bf16, and a cache's start (positions, page numbers, rows: three trips) and end (the waves' merge) weigh
+// twice as much against them: 16 sequences x 8 heads x 4 query heads, 179 MB, 38 us, 34 of them
+// this kernel at 5.3 TB/s; 61 x 8 x 8, 0.67 GB, 121 us, 116 at 5.8 TB/s, of which a tenth goes into
+// starts and ends; one sequence x 32 heads, 17 MB, 13 us, most of them start and merge.  Pieces are counted in
+// steps of all four waves (the first two calls in pieces counted in 64, 128, 256 and 512 keys: 40.8, 40.3,
+// 38.1 and 39.0 us; 128.8, 122.9, 122.8 and 121.3).
 #pragma once
 
 #include "paged_decode.h"
@@ -57,25 +65,16 @@ __device__ __forceinline__ void decode_quant(const PagedArgs& a, QuantLds<D>& ld
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) rd_off[dt] = vr * RB + ((dt ^ SW::swv(vr)) << 5) + 8 * (lane & 3);
   }
-  // LDS places of the two halves of a lane's chunk of load u, the same every second load but for the
-  // rows in front.  The halves lie 16 bytes apart and lanes 32, so that half of the lanes write the upper one
-  // first: those that share a store's pass hit distinct banks.
-  int kw[2][2], vw[2];
+  // LDS places of a lane's chunk of load u: its two halves of 8 keys' dimensions (K) or all of it (V), the
+  // same every second load but for the rows in front.
+  int kw[2][2];
   const int r8 = lane / CPR, c8 = lane % CPR;
-  const bool k_flip = (D == 128 ? c8 >> 2 : r8) & 1;
-  const bool v_flip = (D == 128 ? (c8 ^ SW::swv(r8)) >> 2 ^ r8 : r8) & 1;
 #pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const int r = u * RPL + r8;
+  for (int h = 0; h < 2; ++h) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) kw[u][h] = r8 * RB + (((2 * c8 + (h ^ k_flip)) ^ SW::swk(r)) << 4);
+    for (int u = 0; u < 2; ++u) kw[u][h] = r8 * RB + (((2 * c8 + h) ^ SW::swk(u * RPL + r8)) << 4);
   }
-#pragma unroll
-  for (int h = 0; h < 2; ++h) vw[h] = r8 * RB + ((c8 ^ SW::swv(r8)) << 5) + ((h ^ v_flip) << 4);
-  auto half = [](const u32x4& x, int h, bool flip) {
-    const u32x2 lo = {x[0], x[1]}, hi = {x[2], x[3]};
-    return (h == 0) == flip ? hi : lo;
-  };
+  const int vw = r8 * RB + ((c8 ^ SW::swv(r8)) << 5);
 
   for_each_piece(a, s_walk, w, TL::kRoundShift, [&](int b, int g, const VisibleKeys& keys, int x0, int x1, bool whole, int pair) {
     bf16x8 qop[KS];               // B = Q^T: lane holds column n, dims 32*kk + 8*q4 .. +7
@@ -131,7 +130,7 @@ __device__ __forceinline__ void decode_quant(const PagedArgs& a, QuantLds<D>& ld
           const float f = __shfl(sc[0], u * RPL + lane / CPR, 64);
 #pragma unroll
           for (int h = 0; h < 2; ++h)
-            *reinterpret_cast<bf16x8*>(ts + kw[u & 1][h] + u * RPL * RB) = widen8(half(kr[u], h, k_flip), f);
+            *reinterpret_cast<bf16x8*>(ts + kw[u & 1][h] + u * RPL * RB) = widen8(u32x2{kr[u][2 * h], kr[u][2 * h + 1]}, f);
         }
         if (more) load(kbase, rows, kr);
         sched_fence();
@@ -189,7 +188,7 @@ __device__ __forceinline__ void decode_quant(const PagedArgs& a, QuantLds<D>& ld
           const float f = __shfl(sc[1], u * RPL + lane / CPR, 64);
 #pragma unroll
           for (int h = 0; h < 2; ++h)
-            *reinterpret_cast<bf16x8*>(ts + vw[h] + u * RPL * RB) = widen8(half(vr[u], h, v_flip), f);
+            *reinterpret_cast<bf16x8*>(ts + vw + u * RPL * RB + 16 * h) = widen8(u32x2{vr[u][2 * h], vr[u][2 * h + 1]}, f);
         }
         if (more) load(vbase, rows, vr);
         sched_fence();
