@@ -9,9 +9,10 @@
 //
 // Bound by memory: every element is read and written once, keys and values to half their
 // bytes (8,190 tokens of 64 + 16 heads of 128, 0.32 GB: 73 us, 87 % of a copy's rate; single tokens of 16
-// sequences 4.4 us, the launch and three trips to memory).  A work-group takes the blocks that begin in a run of packed rows, with the angles of their
-// tokens formed once; a wave holds the rows of one head's block in registers while their maximum is
-// found (16 x 128 elements, 32 per lane).  Single tokens have 8 lanes (of heads of 128) each.
+// sequences 4.4 us, the launch and three trips to memory).  A work-group takes the blocks that
+// begin in a run of packed rows, with the angles of their tokens formed once; a wave holds the rows of
+// one head's block in registers while their maximum is found (16 x 128 elements, 32 per lane).  Single
+// tokens have 8 lanes (of heads of 128) each.
 #include "quant_device.h"
 
 namespace moa {
@@ -221,7 +222,7 @@ __global__ void __launch_bounds__(kThreads, 4) quant_append_kernel(QuantAppendAr
       const int64_t pos = p0 + (t - first);
       const int in = static_cast<int>(pos & (kQuantBlock - 1));
       const int len = static_cast<int>(min(int64_t(kQuantBlock - in), last - t));
-      if (t == first || in == 0) {
+      if (t == max(first, int64_t(0)) || in == 0) {
         block(b, static_cast<int>(t), pos, len);
         __syncthreads();                         // the angles make room for the next block's
       }
@@ -239,7 +240,8 @@ int launch_t(const QuantAppendArgs& args, void* stream) {
   int span = a.seq_start != nullptr && a.n_tokens >= kQuantBlock * int64_t(a.batch) ? kQuantBlock : 1;
   const int64_t runs = (int64_t(a.n_tokens) + span - 1) / span;
   if (runs * kThreads >= kMaxGridThreads) return kGridTooLarge;
-  // Heads over four work-groups (8,190 tokens of 64/8 heads: over 2, 4 and 8 79.7, 77.0 and 90.4 us).
+  // Heads over four work-groups (8,190 tokens of 64/8 heads: over 2, 4 and 8 79.7, 77.0 and 90.4 us
+  // when this was chosen).
   const int parts = runs >= 2048 || a.hkv < 4 ? 1 : 4;
   void* params[] = {&copy, &span};
   const void* kernel = a.seq_start == nullptr ? reinterpret_cast<const void*>(&quant_append_kernel<D, 1, kInterleaved>)

@@ -15,7 +15,7 @@ constexpr float kQuantMost = 448.0f;                        // the largest e4m3 
 constexpr uint32_t kQuantNan = 0x7f;
 
 // Eight e4m3 numbers times a power of two in bf16, without rounding (one instruction per pair;
-// checked on gfx950 for every code and scale: only the exponent bits of the scale count).
+// checked on gfx950 for every code at ten scales from the least to the largest: only the exponent bits of the scale count).
 __device__ __forceinline__ bf16x8 widen8(u32x2 x, float scale) {
 #if defined(__HIP_DEVICE_COMPILE__)
   const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[0], scale, false);

@@ -208,6 +208,26 @@ def test_append_in_place_and_past_the_table():
     assert torch.equal(same, ref) and not torch.equal(ref, q)
 
 
+def test_append_of_rows_in_front_of_the_tensors():
+    """A sequence whose first rows are in front of the tensors is stored from row 0 on, like one that starts there."""
+    _say("append rows in front")
+    plan = M.moa_plan(4, 2, 128, 0, 100, "bf16", [10.0] * 2, [0.0] * 2)
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    q = torch.randn((9, 4, 128), generator=gen, device="cuda").bfloat16()
+    k, v = torch.randn((2, 9, 2, 128), generator=gen, device="cuda").bfloat16()
+    f = torch.logspace(0, -3, 64, device="cuda")
+    table = torch.arange(8, dtype=torch.int32, device="cuda").view(2, 2, 2)
+    at = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    for p0 in (0, 10, 14):                       # row 0 within a block, and past one's end
+        caches = [M.new_quant_cache(plan, 8, 16) for _ in range(2)]
+        out = [torch.full_like(q, 7.0) for _ in range(2)]
+        M.moa_quant_append(plan, *caches[0], table, q, k, v, at(p0 + 3, 2), at(0, 5, 9), f, q_out=out[0])
+        M.moa_quant_append(plan, *caches[1], table, q, k, v, at(p0, 2), at(-3, 5, 9), f, q_out=out[1])
+        assert torch.equal(*out) and not (out[0] == 7.0).all(2).any()
+        for a, b in zip(*caches):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
 # ---------------------------------------------------------------------------
 # Attention.
 # ---------------------------------------------------------------------------
@@ -223,7 +243,7 @@ def _windows(hkv, i):
 def test_every_number_and_scale_comes_out_as_it_is(d):
     """With one visible key the output is its value, whatever it is; NaN stays NaN."""
     _say("all codes", d)
-    exponents = [-117, -100, -9, -1, 0, 1, 7, 60, 118]
+    exponents = [-117, -100, -9, -1, 0, 1, 7, 60, 118, 119]
     b = 256 * len(exponents) // d
     plan = M.moa_plan(1, 1, d, 0, 100, "bf16", [1.0], [0.0])
     codes = torch.arange(256, dtype=torch.uint8).repeat(len(exponents)).view(b, 1, d)
