@@ -28,7 +28,6 @@ constexpr int kWaves = kThreads / 64;
 constexpr int kScanThreads = 1024;
 constexpr int kScanWaves = kScanThreads / 64;
 constexpr int kFewPairs = 4096;          // counts of all pairs in LDS
-constexpr int kAhead = 4;                // entries asked for at once: so many for each lane of a wave
 constexpr int kSlotTokens = 16;          // tokens per work-group of the rows' kernel
 constexpr int kManyTokens = 4096;        // from here on rows have a kernel of their own
 
@@ -117,22 +116,14 @@ __global__ void __launch_bounds__(kThreads) paged_count_kernel(AssignArgs a) {
   const Pair r = pair_of(a, p);
   int32_t* table = a.table + int64_t(p) * a.max_pages;
   int gone = 0, need = 0;
-  for (int i = r.gone_lo; i < r.gone_hi; i += 64 * kAhead) {
-    int entry[kAhead];
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const int at = i + 64 * u + lane;
-      entry[u] = at < r.gone_hi ? table[at] : -1;
+  for (int i = r.gone_lo; i < r.gone_hi; i += 64) {
+    const int entry = i + lane < r.gone_hi ? table[i + lane] : -1;
+    const uint64_t which = __ballot(present(a, entry));
+    if (kStash && present(a, entry)) {
+      ws.stash[int64_t(p) * a.max_pages + gone + below(which)] = entry;
+      table[i + lane] = -1;
     }
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const uint64_t which = __ballot(present(a, entry[u]));
-      if (kStash && present(a, entry[u])) {
-        ws.stash[int64_t(p) * a.max_pages + gone + below(which)] = entry[u];
-        table[i + 64 * u + lane] = -1;
-      }
-      gone += __builtin_popcountll(which);
-    }
+    gone += __builtin_popcountll(which);
   }
   if (r.fresh) {
     need = r.need_hi - r.need_lo;
@@ -273,10 +264,10 @@ __global__ void __launch_bounds__(kThreads) paged_take_kernel(AssignArgs a) {
     a.counts[1] = static_cast<int>(min(max(all_need - listed, int64_t(0)), int64_t(0x7fffffff)));
   }
   if (p >= pairs) return;
-  // Where page i of the list as step 1 leaves it is: what this call has put there may still be under way.
-  auto place = [&](int64_t i) -> const int32_t* {
-    if constexpr (!kStash) return a.free_pages + i;
-    if (i < n) return a.free_pages + i;
+  // Page i of the list as step 1 leaves it: what this call has put there may still be under way.
+  auto page = [&](int64_t i) {
+    if constexpr (!kStash) return a.free_pages[i];
+    if (i < n) return a.free_pages[i];
     const int k = static_cast<int>(i - n);
     int lo = 0, hi = pairs;                               // s_gone[lo] <= k < s_gone[hi]
     while (hi - lo > 1) {
@@ -284,7 +275,7 @@ __global__ void __launch_bounds__(kThreads) paged_take_kernel(AssignArgs a) {
       if (s_gone[mid] <= k) lo = mid;
       else hi = mid;
     }
-    return ws.stash + (int64_t(lo) * a.max_pages + k - s_gone[lo]);
+    return ws.stash[int64_t(lo) * a.max_pages + k - s_gone[lo]];
   };
   int32_t* table = a.table + int64_t(p) * a.max_pages;
   int64_t at = listed - 1;
@@ -299,33 +290,20 @@ __global__ void __launch_bounds__(kThreads) paged_take_kernel(AssignArgs a) {
       if (pos < hi) a.slots[(r.row + pos - r.pos) * a.hkv + r.g] = row_of_pool(a, entry, pos);
     }
   };
-  for (int i = r.need_lo; i < r.need_hi; i += 64 * kAhead) {
-    int entry[kAhead];
-    const int32_t* from[kAhead];
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const int to = i + 64 * u + lane;
-      entry[u] = r.fresh || to >= r.need_hi ? -1 : table[to];
+  for (int i = r.need_lo; i < r.need_hi; i += 64) {
+    const bool in = i + lane < r.need_hi;
+    int entry = r.fresh || !in ? -1 : table[i + lane];
+    const bool need = in && !present(a, entry);
+    const uint64_t which = __ballot(need);
+    const int64_t from = at - below(which);
+    if (need && from >= 0) {
+      entry = page(from);
+      table[i + lane] = entry;
     }
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const bool need = i + 64 * u + lane < r.need_hi && !present(a, entry[u]);
-      const uint64_t which = __ballot(need);
-      const int64_t nth = at - below(which);
-      from[u] = need && nth >= 0 ? place(nth) : nullptr;
-      at -= __builtin_popcountll(which);
-    }
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u)
-      if (from[u] != nullptr) entry[u] = *from[u];
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const int i0 = i + 64 * u;
-      if (from[u] != nullptr) table[i0 + lane] = entry[u];
-      if (rows && i0 < r.need_hi)
-        write_rows(max(r.pos, int64_t(i0) << a.page_shift), min(end, int64_t(i0 + 64) << a.page_shift),
-                   [&](int64_t pos) { return __shfl(entry[u], static_cast<int>(pos >> a.page_shift) - i0, 64); });
-    }
+    at -= __builtin_popcountll(which);
+    if (rows)
+      write_rows(max(r.pos, int64_t(i) << a.page_shift), min(end, int64_t(i + 64) << a.page_shift),
+                 [&](int64_t pos) { return __shfl(entry, static_cast<int>(pos >> a.page_shift) - i, 64); });
   }
   if (rows) write_rows(max(r.pos, int64_t(a.max_pages) << a.page_shift), end, [](int64_t) { return -1; });
   if constexpr (kStash) {
@@ -377,7 +355,6 @@ int launch_paged_assign(const AssignArgs& a, size_t ws_bytes, void* stream) {
   const int64_t pairs = int64_t(a.batch) * a.hkv, groups = (pairs + kWaves - 1) / kWaves;
   const int64_t row_groups = a.slots == nullptr ? 0 : (int64_t(a.n_tokens) + kSlotTokens - 1) / kSlotTokens;
   if (row_groups * kThreads >= kMaxGridThreads) return kGridTooLarge;      // nothing is launched
-  // Few pairs are added up in 32 bits.
   // Few pairs are added up in 32 bits.
   const bool few = pairs <= kFewPairs && pairs * a.max_pages <= INT32_MAX &&
                    32 + pairs * (8 + int64_t(4) * a.max_pages) <= static_cast<int64_t>(ws_bytes);
