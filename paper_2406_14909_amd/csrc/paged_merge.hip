@@ -7,6 +7,8 @@
 // kernels held them: 1 KB is 32 rows x 8 columns, lane l's float4 row l % 32, columns
 // 4 * (l / 32) ..; so a wave reads whole blocks.  Each wave takes one of 4 such blocks, or,
 // of more than kMany pieces, a quarter of the pieces of one, and they meet in LDS.
+#include <type_traits>
+
 #include "paged_rows.h"
 
 namespace moa {
@@ -82,33 +84,40 @@ __global__ void __launch_bounds__(kThreads) paged_merge_kernel(PagedArgs a) {
       const float* base = a.rows_part + int64_t(2 * w) * SLOT;
       const float* block = base + ((r32 * BLOCKS + c8) * 64 + lane) * 4;
       const float* stat = base + ROWS * D + row * 2;
-      for (int p0 = share; p0 < seg.pieces; p0 += kFlight * step) {
-        float mp[kFlight], lp[kFlight];
-        f32x4 xp[kFlight];
+      // F pieces in flight, one after the other.
+      auto add = [&](auto flight) {
+        constexpr int F = decltype(flight)::value;
+        for (int p0 = share; p0 < seg.pieces; p0 += F * step) {
+          float mp[F], lp[F];
+          f32x4 xp[F];
 #pragma unroll
-        for (int u = 0; u < kFlight; ++u) {
-          const int p = min(p0 + u * step, seg.pieces - 1);
-          const int64_t at = int64_t(p == 0 ? 1 : 2 * p) * SLOT;
-          mp[u] = stat[at];
-          lp[u] = stat[at + 1];
-          xp[u] = *reinterpret_cast<const f32x4*>(block + at);
+          for (int u = 0; u < F; ++u) {
+            const int p = min(p0 + u * step, seg.pieces - 1);
+            const int64_t at = int64_t(p == 0 ? 1 : 2 * p) * SLOT;
+            mp[u] = stat[at];
+            lp[u] = stat[at + 1];
+            xp[u] = *reinterpret_cast<const f32x4*>(block + at);
+          }
+          float mx = m;
+#pragma unroll
+          for (int u = 0; u < F; ++u) mx = fmaxf(mx, mp[u]);
+          const float f = fast_exp2(m - mx);
+          l *= f;
+          acc *= f;
+          m = mx;
+#pragma unroll
+          for (int u = 0; u < F; ++u) {
+            // past the last piece, which is read again there, sums count as zeros: they may be infinite
+            const bool more = p0 + u * step < seg.pieces;
+            const float wgt = more ? fast_exp2(mp[u] - mx) : 0.0f;
+            l += wgt * lp[u];
+            acc += (more ? xp[u] : f32x4{0.0f, 0.0f, 0.0f, 0.0f}) * wgt;
+          }
         }
-        float mx = m;
-#pragma unroll
-        for (int u = 0; u < kFlight; ++u) mx = fmaxf(mx, mp[u]);
-        const float f = fast_exp2(m - mx);
-        l *= f;
-        acc *= f;
-        m = mx;
-#pragma unroll
-        for (int u = 0; u < kFlight; ++u) {
-          // past the last piece, which is read again there, sums count as zeros: they may be infinite
-          const bool more = p0 + u * step < seg.pieces;
-          const float wgt = more ? fast_exp2(mp[u] - mx) : 0.0f;
-          l += wgt * lp[u];
-          acc += (more ? xp[u] : f32x4{0.0f, 0.0f, 0.0f, 0.0f}) * wgt;
-        }
-      }
+      };
+      if (seg.pieces <= 2) add(std::integral_constant<int, 2>{});
+      else if (seg.pieces <= 4) add(std::integral_constant<int, 4>{});
+      else add(std::integral_constant<int, kFlight>{});
     }
     if (many) {
       __syncthreads();
@@ -136,8 +145,8 @@ __global__ void __launch_bounds__(kThreads) paged_merge_kernel(PagedArgs a) {
     const int gs = a.group_shift;
     T* op = static_cast<T*>(a.o) + (int64_t(seg.token + (row >> gs)) * a.hq + (seg.head << gs) + (row & ((1 << gs) - 1))) * D +
             c8 * 8 + (lane >> 5) * 4;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) op[e] = static_cast<T>(acc[e]);
+    typedef T t4 __attribute__((ext_vector_type(4)));
+    *reinterpret_cast<t4*>(op) = __builtin_convertvector(acc, t4);
   }
 }
 
