@@ -1,8 +1,9 @@
 // Merge of the partial results of row tiles whose keys were cut into pieces:
 // o = sum_p 2^(m_p - M) acc_p / sum_p 2^(m_p - M) l_p, M = max_p m_p.
 //
-// Bound by latency, then by memory (512 tiles in two or three pieces each, 55 MB: 20 us).  Few tiles are cut into many pieces or many into few, and
-// only the device knows: every work-group reads the notes of all workers and shares out what
+// Bound by latency, then by memory (400 row tiles in two or three pieces each, 54 MB: 14 us; with 8 loads
+// in flight whatever the number of pieces, the last ones the same, 18.5).  Few tiles are cut into
+// many pieces or many into few, and only the device knows: every work-group reads the notes of all workers and shares out what
 // they left, 32 rows and 32 columns at a time.  Partial results lie as the lanes of the row
 // kernels held them: 1 KB is 32 rows x 8 columns, lane l's float4 row l % 32, columns
 // 4 * (l / 32) ..; so a wave reads whole blocks.  Each wave takes one of 4 such blocks, or,

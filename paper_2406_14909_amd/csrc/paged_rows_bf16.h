@@ -84,7 +84,7 @@ struct RowsBf16Lds {
 // k8: over 8-bit pages.  A wave's 16 rows of a tile pass through its registers, asked for a tile ahead, and
 // are widened to bf16 as it writes them to LDS, once for all waves; the rest is the same.  2 prompts of
 // 12,000 tokens of 32 heads: 592 us, 861 TFLOP/s, as bf16 pages have; 6 chunks of 8 x 4 heads behind
-// up to 16,000: 178 us; 500 tokens: 18.9 us.  (Direct loads, and keys widened by every wave as it reads
+// up to 16,000: 177 us; 500 tokens: 18.9 us.  (Direct loads, and keys widened by every wave as it reads
 // its operands: 727 us for the prompts; direct loads of the wave's own rows, widened from LDS to LDS: 733; the
 // widening between the S products instead of in front of them: 617, where 626 were had without, and 23.2
 // for 20.5 of the short prompt.)
