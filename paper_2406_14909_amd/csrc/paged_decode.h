@@ -36,7 +36,7 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * 64;
 constexpr int kPageRows = 1024;      // page numbers held in LDS
-constexpr int kPlanHead = 4;         // plan: workers, per, rem, pad, then the rounds in front of each pair that has any
+constexpr int kPlanHead = 4;         // plan: workers, per, rem, the rounds of a start, then those in front of each pair that has any
 
 __device__ __forceinline__ f32x4 mma16(const bf16x8& a, const bf16x8& b, const f32x4& c) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -70,8 +70,9 @@ struct Walk {
 
 // Calls seg(b, g, keys, x0, x1, whole, pair) for each cache that this worker's piece
 // touches: visible keys [x0, x1) of KV head g of sequence b, `whole` when these are all.
-// Work-group uniform; every thread takes part.
-template <class Seg>
+// Work-group uniform; every thread takes part.  kStarts: of at least as many caches as workers, of
+// two rounds or more on average, each also costs a round in front of its own, for its start.
+template <bool kStarts = false, class Seg>
 __device__ __forceinline__ void for_each_piece(const PagedArgs& a, Walk& s, uint32_t w, int round_shift, Seg&& seg) {
   const int pairs = a.batch * a.hkv;
   const int each = (pairs + kThreads - 1) / kThreads;
@@ -108,12 +109,20 @@ __device__ __forceinline__ void for_each_piece(const PagedArgs& a, Walk& s, uint
     longest = max(longest, s.wave_max[v]);
   }
   before += incl - sum;
+  const uint32_t start = kStarts && pairs >= a.slots && units >= 2 * static_cast<uint32_t>(pairs) ? 1 : 0;
+  if (start > 0) {
+    units += pairs;
+    longest += 1;
+    before += min(pairs, p0);
+    sum += max(p1 - p0, 0);
+  }
   const PagedSplit split = paged_split(units, longest, a.slots);
   if (w >= split.workers) return;
   if (w == 0 && threadIdx.x == 0) {
     a.plan[0] = split.workers;
     a.plan[1] = split.per;
     a.plan[2] = split.rem;
+    if (kStarts) a.plan[3] = start;
   }
   uint32_t x = split.start(w);
   const uint32_t x_end = split.start(w + 1);
@@ -123,7 +132,7 @@ __device__ __forceinline__ void for_each_piece(const PagedArgs& a, Walk& s, uint
     for (; each > 1; ++p) {
       const int b = p / a.hkv;
       pos = a.positions[b];
-      const uint32_t n = rounds_of(a, pos, p - b * a.hkv, round_shift);
+      const uint32_t n = rounds_of(a, pos, p - b * a.hkv, round_shift) + start;
       if (x < at + n) break;
       at += n;
     }
@@ -137,13 +146,15 @@ __device__ __forceinline__ void for_each_piece(const PagedArgs& a, Walk& s, uint
   pos = uniform(s.pos);
   int b = pair / a.hkv, g = pair - b * a.hkv;
   while (true) {
-    const uint32_t n = rounds_of(a, pos, g, round_shift);
+    const uint32_t n = rounds_of(a, pos, g, round_shift) + start;
     if (n > 0) {
       const VisibleKeys keys = keys_of(a, pos, g);
       const uint32_t lo = x - at, hi = min(n, lo + (x_end - x));
       if (lo == 0 && threadIdx.x == 0) a.plan[kPlanHead + pair] = static_cast<int32_t>(at);
-      seg(b, g, keys, static_cast<int>(lo << round_shift),
-          static_cast<int>(min(static_cast<uint32_t>(keys.count), hi << round_shift)), lo == 0 && hi == n, pair);
+      const uint32_t first = max(lo, start) - start, last = max(hi, start) - start;    // rounds of keys
+      if (last > 0)
+        seg(b, g, keys, static_cast<int>(first << round_shift),
+            static_cast<int>(min(static_cast<uint32_t>(keys.count), last << round_shift)), lo <= start && hi == n, pair);
       x += hi - lo;
       if (x >= x_end) break;
     }
@@ -574,7 +585,7 @@ __device__ __forceinline__ void decode_worker(const PagedArgs& a, DecodeLds<T, D
 template <int G>
 constexpr int merge_heads() { return G <= 2 ? G : 2; }
 
-template <typename T, int D, int G, bool kShared, int kRoundShift = decode_round_shift<T, D, G>()>
+template <typename T, int D, int G, bool kShared, int kRoundShift = decode_round_shift<T, D, G>(), bool kStarts = false>
 __global__ void __launch_bounds__(256) paged_combine_kernel(PagedArgs a) {
   constexpr int PS = D + kPagedPartPad;
   constexpr int V4 = D / 4;
@@ -590,7 +601,8 @@ __global__ void __launch_bounds__(256) paged_combine_kernel(PagedArgs a) {
   const int h0 = (static_cast<int>(blockIdx.x) - pair * (G / HS)) * HS;
   const int b = pair / a.hkv, g = pair - b * a.hkv;
   const int pos = a.positions[b];
-  const uint32_t x0 = a.plan[kPlanHead + pair];       // written by the worker that began with the pair, if one did
+  uint32_t x0 = a.plan[kPlanHead + pair];             // written by the worker that began with the pair, if one did
+  if constexpr (kStarts) x0 += a.plan[3];             // where its keys' rounds begin
   const PagedSplit split = {static_cast<uint32_t>(a.plan[0]), static_cast<uint32_t>(a.plan[1]),
                             static_cast<uint32_t>(a.plan[2])};
   const int pg = static_cast<int>(threadIdx.x) / TPR, j = static_cast<int>(threadIdx.x) % TPR;

@@ -76,7 +76,7 @@ __device__ __forceinline__ void decode_quant(const PagedArgs& a, QuantLds<D>& ld
   }
   const int vw = r8 * RB + ((c8 ^ SW::swv(r8)) << 5);
 
-  for_each_piece(a, s_walk, w, TL::kRoundShift, [&](int b, int g, const VisibleKeys& keys, int x0, int x1, bool whole, int pair) {
+  for_each_piece<true>(a, s_walk, w, TL::kRoundShift, [&](int b, int g, const VisibleKeys& keys, int x0, int x1, bool whole, int pair) {
     bf16x8 qop[KS];               // B = Q^T: lane holds column n, dims 32*kk + 8*q4 .. +7
     if (n < PARTS * G) {
       const bf16* qp = static_cast<const bf16*>(a.q) + (int64_t(b) * a.hq + g * G + n % G) * D + 8 * q4;

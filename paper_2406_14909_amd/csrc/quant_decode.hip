@@ -20,7 +20,7 @@ int launch_t(PagedArgs a, void* stream) {
   hipError_t e = hipLaunchKernel(kernel, dim3(static_cast<unsigned>(a.slots)), dim3(kThreads), args, 0,
                                  static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return static_cast<int>(e);
-  e = hipLaunchKernel(reinterpret_cast<const void*>(&paged_combine_kernel<bf16, D, G, false, QuantTile<D>::kRoundShift>),
+  e = hipLaunchKernel(reinterpret_cast<const void*>(&paged_combine_kernel<bf16, D, G, false, QuantTile<D>::kRoundShift, true>),
                       combine_grid<G>(a), dim3(256), args, 0, static_cast<hipStream_t>(stream));
   return static_cast<int>(e);
 }

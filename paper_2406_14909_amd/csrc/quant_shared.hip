@@ -36,7 +36,7 @@ int launch_t(const PagedArgs& a, void* stream) {
   hipError_t e = hipLaunchKernel(reinterpret_cast<const void*>(&quant_shared_kernel<D, G>), dim3(shared_groups(a)),
                                  dim3(kThreads), args, 0, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return static_cast<int>(e);
-  e = hipLaunchKernel(reinterpret_cast<const void*>(&paged_combine_kernel<bf16, D, G, true, QuantTile<D>::kRoundShift>),
+  e = hipLaunchKernel(reinterpret_cast<const void*>(&paged_combine_kernel<bf16, D, G, true, QuantTile<D>::kRoundShift, true>),
                       combine_grid<G>(a), dim3(256), args, 0, static_cast<hipStream_t>(stream));
   return static_cast<int>(e);
 }
