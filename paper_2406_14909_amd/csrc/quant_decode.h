@@ -13,7 +13,10 @@
 // this kernel at 5.3 TB/s; 61 x 8 x 8, 0.67 GB, 121 us, 116 at 5.8 TB/s, of which a tenth goes into
 // starts and ends; one sequence x 32 heads, 17 MB, 13 us, most of them start and merge.  Pieces are counted in
 // steps of all four waves (the first two calls in pieces counted in 64, 128, 256 and 512 keys: 40.8, 40.3,
-// 38.1 and 39.0 us; 128.8, 122.9, 122.8 and 121.3).
+// 38.1 and 39.0 us; 128.8, 122.9, 122.8 and 121.3).  Of as many caches as workers and more, workers would
+// differ in starts, so each counts as a round, too (48 x 32 heads of up to 4,200 keys 139.5 -> 125.5 us; of fewer
+// caches it costs: the first call 38.2 -> 39.2; of caches of one round, 512 of up to 500 keys behind
+// a prefix, 25.6 -> 27.1).
 #pragma once
 
 #include "paged_decode.h"

@@ -9,7 +9,7 @@
 //   48 x 8 x 8 on 32,700, 1,000          44.3        47.6        50.1        48.5
 //   16 x 8 x 4 on 8,001, 500             16.5        16.5        16.5        16.5
 //   16 x 32 x 1 on 8,001, 500            25.9        29.5        25.8        31.2
-//   48 x 32 x 1 on 8,001, 1,500           105         131          97         100
+//   48 x 32 x 1 on 8,001, 1,500           105         131          97         100    (92 since starts count)
 //   32 x 8 x 4 on 2,000, 4,000           29.3        33.0        28.2        26.8
 #include "paged_rows_bf16.h"
 #include "quant_decode.h"
