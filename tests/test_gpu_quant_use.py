@@ -154,6 +154,22 @@ def test_large_batches():
     QuantPaged(4, 2, 64, 3, [9, 100], "bf16", where, prefix_len=60, seed=4).check("shared by 300")
 
 
+@pytest.mark.parametrize("d,hq,prefix", [(64, 2, 0), (128, 4, 0), (64, 8, 100)])
+def test_many_caches_of_several_rounds(d, hq, prefix):
+    """At least as many caches as workers (two per compute unit, behind a prefix one), of two rounds of 256 keys or
+    more on average: starts count in the split.  Idle sequences, short caches and heads, and long ones among them."""
+    _say("many caches", d, hq, prefix)
+    rng = np.random.default_rng(7)
+    b, s, windows = (150 if prefix else 300), 3, [1400, 200]
+    where = prefix + rng.integers(1000, 1500, size=b)
+    where[rng.permutation(b)[:40]] = prefix + rng.integers(0, 60, size=40)
+    where[[0, 17, 18, b - 1]] = -1
+    where[[1, b - 2]] = prefix
+    own = [sum(-(-min(max(p + 1 - prefix, 0), w + (s if not prefix else 0)) // 256) for p in where) for w in windows]
+    assert sum(own) >= 2 * 2 * b
+    QuantPaged(hq, 2, d, s, windows, "bf16", [int(x) for x in where], page=32, prefix_len=prefix, seed=8).check("many")
+
+
 def test_a_long_sequence_among_many():
     _say("long among many")
     rng = np.random.default_rng(5)
