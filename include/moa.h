@@ -40,7 +40,7 @@
  *   moa_paged_assign
  *                  the page tables of that cache kept on the device: pages that
  *                  no later query sees go back to a free list, new tokens get
- *                  pages from it.
+ *                  pages from it (moa_paged_assign_state: of an 8-bit cache).
  *   moa_quant_append, moa_quant_prefill, moa_quant_decode,
  *   moa_quant_decode_shared
  *                  the paged cache in 8 bits per element, with a scale for every
@@ -426,6 +426,18 @@ moa_status_t moa_paged_assign(const moa_plan_t* plan, const moa_page_tables_t* t
                               const int32_t* seq_start, const int32_t* fresh, int32_t* slots, int32_t batch,
                               int64_t n_tokens, void* workspace, size_t ws_bytes, void* hip_stream);
 
+/* What the call keeps besides the tables. */
+typedef struct {
+  float* scales;             /* of an 8-bit cache (moa_quant_pages_t), 8-byte aligned; or NULL */
+} moa_page_state_t;
+
+/* moa_paged_assign, and: the scales of every page that the call gives out become 0 (nothing
+ * is stored), whatever stood there before.  state NULL: moa_paged_assign itself. */
+moa_status_t moa_paged_assign_state(const moa_plan_t* plan, const moa_page_tables_t* tables,
+                                    const moa_page_state_t* state, const int32_t* positions, const int32_t* seq_start,
+                                    const int32_t* fresh, int32_t* slots, int32_t batch, int64_t n_tokens,
+                                    void* workspace, size_t ws_bytes, void* hip_stream);
+
 /* --------------------------------------------------------------------------
  * Paged cache in 8 bits.
  *
@@ -456,7 +468,10 @@ typedef struct {
  * tokens gets the smallest scale that keeps the largest finite magnitude of its new tokens (keys:
  * after rotation, in fp32) within 448.  Of a block that is entered behind its first position, the
  * scale is the larger of that and the stored one, and where it grows the rows in front of the
- * new tokens are rounded once more, to the new scale.  Rows behind the new tokens of a block
+ * new tokens are rounded once more, to the new scale.  A stored 0 is no scale yet, so the scales
+ * of a page have to be 0 when a sequence begins in the middle of one of its blocks (behind a
+ * shared prefix whose length is no multiple of 16, say): those of new pages, and of pages that
+ * another sequence had (moa_paged_assign_state).  Rows behind the new tokens of a block
  * mean nothing afterwards.  Two sequences of one append must not write to the same block.
  * Values, keys and queries are otherwise as in moa_paged_append; q_out is bf16. */
 moa_status_t moa_quant_append(const moa_plan_t* plan, const moa_quant_pages_t* pages, const void* q, int64_t q_stride,

@@ -49,6 +49,7 @@ struct Api {
   decltype(&moa_quant_prefill) quant_prefill;
   decltype(&moa_quant_decode) quant_decode;
   decltype(&moa_quant_decode_shared) quant_decode_shared;
+  decltype(&moa_paged_assign_state) paged_assign_state;
 };
 
 // What the checks need of a library and a plan; held by a capsule.
@@ -580,9 +581,10 @@ PyObject* pages_decode_shared(PyObject*, PyObject* const* args, Py_ssize_t nargs
 }
 constexpr auto paged_decode_shared = pages_decode_shared<false>, quant_decode_shared = pages_decode_shared<true>;
 
-// paged_assign(bound, table, free_pages, counts, page_size, positions, workspace, seq_start, fresh, slots)
-PyObject* paged_assign(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
-  MOA_ENTER(10)
+// (bound, table, free_pages, counts, page_size, positions, workspace, seq_start, fresh, slots[, scales])
+template <bool kState>
+PyObject* assign(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  MOA_ENTER(kState ? 11 : 10)
   int64_t page;
   const at::Tensor* t = c.any(args[1]);
   const at::Tensor* f = c.any(args[2]);
@@ -601,6 +603,13 @@ PyObject* paged_assign(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   const at::Tensor* sl = args[9] != Py_None ? c.any(args[9]) : nullptr;
   if (sl && (sl->dim() != 2 || sl->scalar_type() != at::kInt || sl->size(1) != b->hkv || (!ss && sl->size(0) != bsz)))
     return none();
+  const at::Tensor* sc = nullptr;
+  if constexpr (kState) {
+    sc = args[10] != Py_None ? c.any(args[10]) : nullptr;
+    if (sc && (sc->dim() != 3 || sc->scalar_type() != at::kFloat || sc->size(0) < f->size(0) ||
+               sc->size(1) != page / MOA_QUANT_BLOCK || sc->size(2) != 2))
+      return none();
+  }
   if (!c.done() || bsz > INT32_MAX || mp > INT32_MAX) return none();
   auto at_ = [](const at::Tensor* x) { return x ? static_cast<int32_t*>(x->data_ptr()) : nullptr; };
   const moa_page_tables_t tables = {at_(t), at_(f), at_(n2), f->size(0), static_cast<int32_t>(page), static_cast<int32_t>(mp)};
@@ -609,13 +618,19 @@ PyObject* paged_assign(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   const size_t nw = w->nbytes();
   const int32_t *pp = at_(ps), *pss = at_(ss), *pf = at_(fr);
   int32_t* psl = at_(sl);
+  const moa_page_state_t state = {sc ? static_cast<float*>(sc->data_ptr()) : nullptr};
   if (!call(*b, [&] {
-        return b->api.paged_assign(b->plan, &tables, pp, pss, pf, psl, static_cast<int32_t>(bsz), n, pw, nw, s);
+        const int32_t batch = static_cast<int32_t>(bsz);
+        if constexpr (kState)
+          return b->api.paged_assign_state(b->plan, &tables, &state, pp, pss, pf, psl, batch, n, pw, nw, s);
+        else
+          return b->api.paged_assign(b->plan, &tables, pp, pss, pf, psl, batch, n, pw, nw, s);
       }))
     return nullptr;
   Py_RETURN_TRUE;
   MOA_LEAVE
 }
+constexpr auto paged_assign = assign<false>, paged_assign_state = assign<true>;
 
 // bind(addresses of the entry points, plan address or 0, num_q_heads, num_kv_heads, head_dim, cache rows, is bf16,
 //      function that raises for a status)
@@ -659,7 +674,8 @@ PyMethodDef kMethods[] = {
     MOA_FAST(prefill), MOA_FAST(kv_append), MOA_FAST(kv_append_ragged), MOA_FAST(decode), MOA_FAST(decode_noalloc),
     MOA_FAST(decode_ragged), MOA_FAST(influence), MOA_FAST(rule_loss), MOA_FAST(paged_append), MOA_FAST(paged_prefill),
     MOA_FAST(paged_decode), MOA_FAST(paged_decode_shared), MOA_FAST(paged_assign), MOA_FAST(quant_append),
-    MOA_FAST(quant_prefill), MOA_FAST(quant_decode), MOA_FAST(quant_decode_shared), {"bind", bind, METH_VARARGS, nullptr},
+    MOA_FAST(quant_prefill), MOA_FAST(quant_decode), MOA_FAST(quant_decode_shared), MOA_FAST(paged_assign_state),
+    {"bind", bind, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

@@ -65,6 +65,7 @@ struct AssignArgs {
   const int32_t* fresh;      // null: none
   int32_t* slots;            // [n_tokens, hkv], or null
   int64_t* plan;             // workspace
+  float* scales;             // 8-bit cache: those of pages given out become 0; or null
   int32_t n_tokens;
   int32_t batch;
   int32_t hkv;

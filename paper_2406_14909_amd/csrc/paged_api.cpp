@@ -398,6 +398,63 @@ moa_status_t paged_decode_shared(const char* who, const moa_plan_t* plan, const 
   return launched(who, run_decode(*plan, *pages, a, hip_stream));
 }
 
+moa_status_t paged_assign(const char* who, const moa_plan_t* plan, const moa_page_tables_t* tables,
+                          const moa_page_state_t* state, const int32_t* positions, const int32_t* seq_start,
+                          const int32_t* fresh, int32_t* slots, int32_t batch, int64_t n_tokens, void* workspace,
+                          size_t ws_bytes, void* hip_stream) {
+  if (!plan || !tables) return invalid(who, "null plan or tables");
+  if (!tables->table || !tables->free_pages || !tables->counts || !positions) return invalid(who, "null pointer");
+  const void* const ints[] = {tables->table, tables->free_pages, tables->counts, positions, seq_start, fresh, slots};
+  for (const void* p : ints)
+    if (!aligned4(p)) return invalid(who, "tensors must be 4-byte aligned");
+  const moa_status_t st = check_sizes(who, tables->page_size, tables->num_pages, tables->max_pages, batch, n_tokens);
+  if (st != MOA_OK) return st;
+  if (!seq_start && slots && n_tokens != batch) return invalid(who, "without seq_start there is one token per sequence");
+  const moa_desc_t& d = plan->desc;
+  float* const scales = state ? state->scales : nullptr;
+  if (scales && d.dtype != MOA_BF16) return fail(MOA_ERR_UNSUPPORTED, std::string(who) + ": an 8-bit cache takes bf16 plans");
+  if (!aligned8(scales)) return invalid(who, "misaligned scales (8-byte aligned)");
+  const size_t need = moa_paged_workspace_bytes(plan, batch, std::max<int64_t>(n_tokens, 1));
+  if (!workspace || ws_bytes < need)
+    return fail(MOA_ERR_WORKSPACE, std::string(who) + ": workspace missing or smaller than moa_paged_workspace_bytes (" +
+                                       std::to_string(need) + " bytes)");
+  if (reinterpret_cast<uintptr_t>(workspace) & 255u)
+    return fail(MOA_ERR_WORKSPACE, std::string(who) + ": workspace must be 256-byte aligned");
+  const size_t i4 = sizeof(int32_t), pairs = static_cast<size_t>(batch) * d.num_kv_heads;
+  const struct { const void* p; size_t n; } args[] = {     // the first six are written
+      {tables->table, i4 * pairs * tables->max_pages},
+      {tables->free_pages, i4 * static_cast<size_t>(tables->num_pages)},
+      {tables->counts, i4 * 2},
+      {slots, slots ? i4 * static_cast<size_t>(n_tokens) * d.num_kv_heads : 0},
+      {workspace, need},
+      {scales, scales ? sizeof(float) * 2 * static_cast<size_t>(tables->num_pages) * (tables->page_size / kQuantBlock) : 0},
+      {positions, i4 * batch},
+      {seq_start, seq_start ? i4 * (static_cast<size_t>(batch) + 1) : 0},
+      {fresh, fresh ? i4 * batch : 0}};
+  for (int i = 0; i < 6; ++i)
+    for (int j = i + 1; j < 9; ++j)
+      if (args[i].n && args[j].n && overlaps(args[i].p, args[i].n, args[j].p, args[j].n))
+        return invalid(who, "an argument that is written overlaps another one");
+  AssignArgs a;
+  memset(&a, 0, sizeof(a));
+  a.table = tables->table; a.free_pages = tables->free_pages; a.counts = tables->counts;
+  a.positions = positions; a.seq_start = seq_start; a.fresh = fresh; a.slots = slots;
+  a.plan = static_cast<int64_t*>(workspace);
+  a.scales = scales;
+  // The workspace has kPagedMaxWorkers rows of head_dim + 4 floats and as many more as there are pairs:
+  // more than the 32 + 24 bytes a pair that the counts and their sums take.
+  a.n_tokens = static_cast<int32_t>(n_tokens);
+  a.batch = batch;
+  a.hkv = d.num_kv_heads;
+  a.num_pages = static_cast<int32_t>(std::min<int64_t>(tables->num_pages, INT32_MAX));
+  a.page_shift = __builtin_ctz(static_cast<unsigned>(tables->page_size));
+  a.max_pages = tables->max_pages;
+  a.num_sink = d.num_sink;
+  a.block_band = (d.flags & MOA_BLOCK_BAND) != 0;
+  for (int h = 0; h < d.num_kv_heads; ++h) a.window[h] = plan->window[h];
+  return launched(who, launch_paged_assign(a, need, hip_stream));
+}
+
 }  // namespace
 
 }  // namespace moa
@@ -480,53 +537,16 @@ moa_status_t moa_quant_decode_shared(const moa_plan_t* plan, const moa_quant_pag
 moa_status_t moa_paged_assign(const moa_plan_t* plan, const moa_page_tables_t* tables, const int32_t* positions,
                               const int32_t* seq_start, const int32_t* fresh, int32_t* slots, int32_t batch,
                               int64_t n_tokens, void* workspace, size_t ws_bytes, void* hip_stream) {
-  const char* who = "moa_paged_assign";
-  if (!plan || !tables) return invalid(who, "null plan or tables");
-  if (!tables->table || !tables->free_pages || !tables->counts || !positions) return invalid(who, "null pointer");
-  const void* const ints[] = {tables->table, tables->free_pages, tables->counts, positions, seq_start, fresh, slots};
-  for (const void* p : ints)
-    if (!aligned4(p)) return invalid(who, "tensors must be 4-byte aligned");
-  const moa_status_t st = check_sizes(who, tables->page_size, tables->num_pages, tables->max_pages, batch, n_tokens);
-  if (st != MOA_OK) return st;
-  if (!seq_start && slots && n_tokens != batch) return invalid(who, "without seq_start there is one token per sequence");
-  const moa_desc_t& d = plan->desc;
-  const size_t need = moa_paged_workspace_bytes(plan, batch, std::max<int64_t>(n_tokens, 1));
-  if (!workspace || ws_bytes < need)
-    return fail(MOA_ERR_WORKSPACE, std::string(who) + ": workspace missing or smaller than moa_paged_workspace_bytes (" +
-                                       std::to_string(need) + " bytes)");
-  if (reinterpret_cast<uintptr_t>(workspace) & 255u)
-    return fail(MOA_ERR_WORKSPACE, std::string(who) + ": workspace must be 256-byte aligned");
-  const size_t i4 = sizeof(int32_t), pairs = static_cast<size_t>(batch) * d.num_kv_heads;
-  const struct { const void* p; size_t n; } args[] = {     // the first five are written
-      {tables->table, i4 * pairs * tables->max_pages},
-      {tables->free_pages, i4 * static_cast<size_t>(tables->num_pages)},
-      {tables->counts, i4 * 2},
-      {slots, slots ? i4 * static_cast<size_t>(n_tokens) * d.num_kv_heads : 0},
-      {workspace, need},
-      {positions, i4 * batch},
-      {seq_start, seq_start ? i4 * (static_cast<size_t>(batch) + 1) : 0},
-      {fresh, fresh ? i4 * batch : 0}};
-  for (int i = 0; i < 5; ++i)
-    for (int j = i + 1; j < 8; ++j)
-      if (args[i].n && args[j].n && overlaps(args[i].p, args[i].n, args[j].p, args[j].n))
-        return invalid(who, "an argument that is written overlaps another one");
-  AssignArgs a;
-  memset(&a, 0, sizeof(a));
-  a.table = tables->table; a.free_pages = tables->free_pages; a.counts = tables->counts;
-  a.positions = positions; a.seq_start = seq_start; a.fresh = fresh; a.slots = slots;
-  a.plan = static_cast<int64_t*>(workspace);
-  // The workspace has kPagedMaxWorkers rows of head_dim + 4 floats and as many more as there are pairs:
-  // more than the 32 + 24 bytes a pair that the counts and their sums take.
-  a.n_tokens = static_cast<int32_t>(n_tokens);
-  a.batch = batch;
-  a.hkv = d.num_kv_heads;
-  a.num_pages = static_cast<int32_t>(std::min<int64_t>(tables->num_pages, INT32_MAX));
-  a.page_shift = __builtin_ctz(static_cast<unsigned>(tables->page_size));
-  a.max_pages = tables->max_pages;
-  a.num_sink = d.num_sink;
-  a.block_band = (d.flags & MOA_BLOCK_BAND) != 0;
-  for (int h = 0; h < d.num_kv_heads; ++h) a.window[h] = plan->window[h];
-  return launched(who, launch_paged_assign(a, need, hip_stream));
+  return paged_assign("moa_paged_assign", plan, tables, nullptr, positions, seq_start, fresh, slots, batch, n_tokens,
+                      workspace, ws_bytes, hip_stream);
+}
+
+moa_status_t moa_paged_assign_state(const moa_plan_t* plan, const moa_page_tables_t* tables,
+                                    const moa_page_state_t* state, const int32_t* positions, const int32_t* seq_start,
+                                    const int32_t* fresh, int32_t* slots, int32_t batch, int64_t n_tokens,
+                                    void* workspace, size_t ws_bytes, void* hip_stream) {
+  return paged_assign("moa_paged_assign_state", plan, tables, state, positions, seq_start, fresh, slots, batch, n_tokens,
+                      workspace, ws_bytes, hip_stream);
 }
 
 }  // extern "C"

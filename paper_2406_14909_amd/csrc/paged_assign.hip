@@ -17,6 +17,8 @@
 // Rows of many tokens are written by a kernel of their own, in whole lines (16,000 tokens of 32 heads
 // 16.1 us in all, without it 22.9).  48 sequences x 8 heads, 3 of them new with 1,600 tokens: 8.4 us; by one
 // work-group for all counts 57.
+#include <type_traits>
+
 #include "paged_device.h"
 
 namespace moa {
@@ -30,6 +32,10 @@ constexpr int kScanWaves = kScanThreads / 64;
 constexpr int kFewPairs = 4096;          // counts of all pairs in LDS
 constexpr int kSlotTokens = 16;          // tokens per work-group of the rows' kernel
 constexpr int kManyTokens = 4096;        // from here on rows have a kernel of their own
+constexpr int kQuantShift = 4;
+static_assert(kQuantBlock == 1 << kQuantShift, "positions of one scale");
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 // Pages that pairs give back and need.
 struct Counts {
@@ -205,8 +211,9 @@ __device__ __forceinline__ int row_of_pool(const AssignArgs& a, int entry, int64
 }
 
 // A wave gives out the pages of one pair, and writes its tokens' rows where there are few.  kStash:
-// it adds up all pairs' counts first and puts its pair's pages on the list.
-template <bool kStash>
+// it adds up all pairs' counts first and puts its pair's pages on the list.  kState: the scales of
+// the pages that it gives out become 0 (asked in every call, 8.43 -> 8.57 us without any).
+template <bool kStash, bool kState>
 __global__ void __launch_bounds__(kThreads) paged_take_kernel(AssignArgs a) {
   __shared__ int s_gone[kStash ? kFewPairs + 1 : 1], s_need[kStash ? kFewPairs : 1], s_wave[2][kWaves];
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
@@ -299,6 +306,12 @@ __global__ void __launch_bounds__(kThreads) paged_take_kernel(AssignArgs a) {
     if (need && from >= 0) {
       entry = page(from);
       table[i + lane] = entry;
+      if constexpr (kState) {
+        if (a.scales != nullptr && present(a, entry)) {
+          f32x2* const of = reinterpret_cast<f32x2*>(a.scales) + (int64_t(entry) << (a.page_shift - kQuantShift));
+          for (int k = 0; k < 1 << (a.page_shift - kQuantShift); ++k) of[k] = f32x2{0.0f, 0.0f};
+        }
+      }
     }
     at -= __builtin_popcountll(which);
     if (rows)
@@ -361,7 +374,12 @@ int launch_paged_assign(const AssignArgs& a, size_t ws_bytes, void* stream) {
   hipError_t e = few ? run(&paged_count_kernel<true>, groups, kThreads) : run(&paged_count_kernel<false>, groups, kThreads);
   if (e == hipSuccess && !few) e = run(&paged_scan_kernel, 1, kScanThreads);
   if (e == hipSuccess && !few) e = run(&paged_release_kernel, groups, kThreads);
-  if (e == hipSuccess) e = few ? run(&paged_take_kernel<true>, groups, kThreads) : run(&paged_take_kernel<false>, groups, kThreads);
+  const bool state = a.scales != nullptr;
+  auto take = [&](auto stash) {
+    constexpr bool kStash = decltype(stash)::value;
+    return state ? run(&paged_take_kernel<kStash, true>, groups, kThreads) : run(&paged_take_kernel<kStash, false>, groups, kThreads);
+  };
+  if (e == hipSuccess) e = few ? take(std::true_type{}) : take(std::false_type{});
   if (e == hipSuccess && a.slots != nullptr && a.n_tokens >= kManyTokens)
     e = run(&paged_slots_kernel, row_groups, kThreads);
   return static_cast<int>(e);

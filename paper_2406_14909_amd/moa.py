@@ -33,7 +33,7 @@ EXPORTED = (
     "moa_decode_ragged", "moa_influence", "moa_rule_loss", "moa_decode_noalloc",
     "moa_paged_append", "moa_paged_workspace_bytes", "moa_paged_prefill", "moa_paged_decode",
     "moa_paged_decode_shared", "moa_paged_assign", "moa_quant_append", "moa_quant_prefill", "moa_quant_decode",
-    "moa_quant_decode_shared",
+    "moa_quant_decode_shared", "moa_paged_assign_state",
 )
 
 
@@ -73,6 +73,12 @@ class moa_page_tables_t(ctypes.Structure):
     ]
 
 
+class moa_page_state_t(ctypes.Structure):
+    _fields_ = [
+        ("scales", ctypes.c_void_p),
+    ]
+
+
 class moa_quant_pages_t(ctypes.Structure):
     _fields_ = [
         ("k_pages", ctypes.c_void_p),
@@ -109,7 +115,7 @@ class MoaError(RuntimeError):
 _NATIVE = ("moa_prefill", "moa_kv_append", "moa_decode", "moa_decode_noalloc", "moa_kv_append_ragged",
            "moa_decode_ragged", "moa_influence", "moa_rule_loss", "moa_paged_append", "moa_paged_prefill",
            "moa_paged_decode", "moa_paged_decode_shared", "moa_paged_assign", "moa_quant_append", "moa_quant_prefill",
-           "moa_quant_decode", "moa_quant_decode_shared")
+           "moa_quant_decode", "moa_quant_decode_shared", "moa_paged_assign_state")
 
 _lib = None
 _fast = None        # the native call path (_binding), loaded with the library
@@ -169,6 +175,9 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.moa_paged_decode_shared.restype = ctypes.c_int
     lib.moa_paged_assign.argtypes = [vp, ctypes.POINTER(moa_page_tables_t), vp, vp, vp, vp, i32, i64, vp, ctypes.c_size_t, vp]
     lib.moa_paged_assign.restype = ctypes.c_int
+    like = lib.moa_paged_assign.argtypes
+    lib.moa_paged_assign_state.argtypes = [*like[:2], ctypes.POINTER(moa_page_state_t), *like[2:]]
+    lib.moa_paged_assign_state.restype = ctypes.c_int
     for name in ("append", "prefill", "decode", "decode_shared"):      # the same calls on other pages
         call, like = getattr(lib, "moa_quant_" + name), getattr(lib, "moa_paged_" + name)
         call.argtypes = [vp, ctypes.POINTER(moa_quant_pages_t)] + list(like.argtypes[2:])
@@ -745,17 +754,19 @@ def new_page_tables(plan: Plan, batch: int, max_pages: int, num_pages: int, devi
 
 
 def moa_paged_assign(plan: Plan, table, free_pages, counts, page_size: int, positions, workspace, seq_start=None,
-                     fresh=None, slots=None, stream=None):
+                     fresh=None, slots=None, stream=None, scales=None):
     """Brings page tables up to a call: pages that no later query sees go back to the free list, then new
     tokens get pages from it (include/moa.h has the order).
 
     positions: int32[B], of each sequence's first new token, negative: left as it is; seq_start: int32[B + 1], the
     packed row where each sequence's tokens start (None: one token each); fresh: int32[B] or None,
     nonzero: all pages of the sequence go back first; slots: int32 [T, H_kv] or None, gets the pool's row of each
-    new token and head (-1: no page).  Returns slots."""
+    new token and head (-1: no page); scales: those of an 8-bit cache [at least num_pages, page_size / 16, 2], of which
+    the pages given out get zeros, as a sequence that begins inside a block (behind a shared prefix) needs.
+    Returns slots."""
     if stream is None:
-        done = _fast.paged_assign(plan._bound, table, free_pages, counts, page_size, positions, workspace, seq_start,
-                                  fresh, slots)
+        args = (plan._bound, table, free_pages, counts, page_size, positions, workspace, seq_start, fresh, slots)
+        done = _fast.paged_assign(*args) if scales is None else _fast.paged_assign_state(*args, scales)
         if done is not None:
             return slots
     import torch
@@ -779,15 +790,24 @@ def moa_paged_assign(plan: Plan, table, free_pages, counts, page_size: int, posi
         n = int(slots.shape[0])
         _need(slots, (n if seq_start is not None else bsz, plan.num_kv_heads), torch.int32, "slots")
         tensors["slots"] = slots
+    if scales is not None:
+        _need_rank(scales, 3, "scales")
+        _need(scales, (max(int(scales.shape[0]), int(free_pages.shape[0])), int(page_size) // MOA_QUANT_BLOCK, 2), torch.float32,
+              "scales")
+        tensors["scales"] = scales
     if workspace.device.type != "cuda" or not workspace.is_contiguous():
         raise MoaError(MOA_ERR_WORKSPACE, "workspace must be a contiguous GPU tensor")
     tables = moa_page_tables_t(table.data_ptr(), free_pages.data_ptr(), counts.data_ptr(), int(free_pages.shape[0]),
                                int(page_size), int(table.shape[2]))
     at = lambda t: None if t is None else t.data_ptr()
+    state = None if scales is None else ctypes.byref(moa_page_state_t(at(scales)))
     with torch.cuda.device(_one_device(**tensors)):
-        _check(load_library().moa_paged_assign(
-            plan.handle, ctypes.byref(tables), positions.data_ptr(), at(seq_start), at(fresh), at(slots), bsz, n,
-            workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(table, stream)))
+        lib, rest = load_library(), (positions.data_ptr(), at(seq_start), at(fresh), at(slots), bsz, n, workspace.data_ptr(),
+                                     workspace.numel() * workspace.element_size(), _stream(table, stream))
+        if state is None:
+            _check(lib.moa_paged_assign(plan.handle, ctypes.byref(tables), *rest))
+        else:
+            _check(lib.moa_paged_assign_state(plan.handle, ctypes.byref(tables), state, *rest))
     return slots
 
 
