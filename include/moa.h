@@ -40,7 +40,8 @@
  *   moa_paged_assign
  *                  the page tables of that cache kept on the device: pages that
  *                  no later query sees go back to a free list, new tokens get
- *                  pages from it (moa_paged_assign_state: of an 8-bit cache).
+ *                  pages from it (moa_paged_assign_state: of an 8-bit cache, or
+ *                  where the list may run out).
  *   moa_quant_append, moa_quant_prefill, moa_quant_decode,
  *   moa_quant_decode_shared
  *                  the paged cache in 8 bits per element, with a scale for every
@@ -411,7 +412,11 @@ typedef struct {
  *  2. Absent entries of the positions of new tokens get pages, in the order of the table:
  *     each the last page of the free list.  Where the list runs out the remaining ones
  *     stay absent (moa_paged_append does not store their tokens), counts[0] is 0 and counts[1] the
- *     number of pages lacked, otherwise counts[1] is 0.
+ *     number of pages lacked, otherwise counts[1] is 0.  A later call gives such an entry a
+ *     page if it has new tokens there, and the rows of the tokens that were not stored then hold what
+ *     was there before, which attention sees: a sequence that lacked a page has to begin anew (fresh), or
+ *     get its tokens from the first that was not stored on once more.  counts[1] tells of the last call
+ *     alone, and not which sequences; moa_paged_assign_state keeps that.
  * positions and seq_start are as in moa_paged_append (seq_start NULL: one token per
  * sequence); a negative positions[b] has no new tokens, nor has a sequence whose rows are
  * not all within [0, n_tokens).  fresh (device int32 [batch]) may be NULL: none.
@@ -429,10 +434,18 @@ moa_status_t moa_paged_assign(const moa_plan_t* plan, const moa_page_tables_t* t
 /* What the call keeps besides the tables. */
 typedef struct {
   float* scales;             /* of an 8-bit cache (moa_quant_pages_t), 8-byte aligned; or NULL */
+  int32_t* lacked;           /* device [batch], zeros with new tables; or NULL */
 } moa_page_state_t;
 
-/* moa_paged_assign, and: the scales of every page that the call gives out become 0 (nothing
- * is stored), whatever stood there before.  state NULL: moa_paged_assign itself. */
+/* moa_paged_assign, and
+ *  scales   those of every page that the call gives out become 0 (nothing is stored), whatever stood
+ *           there before.
+ *  lacked   lacked[b] becomes 1 where sequence b lacks a page, and stays so through any number of
+ *           calls.  A sequence with lacked[b] != 0 gets no pages (and counts[1] does not count what it
+ *           would need), so that no position that was not stored is ever on a page of its own; pages
+ *           still go back.  fresh[b] != 0 makes it 0 in front of all else.  A caller may clear it, too, and
+ *           then gives the sequence's tokens from the first that was not stored on once more.
+ * state NULL: moa_paged_assign itself. */
 moa_status_t moa_paged_assign_state(const moa_plan_t* plan, const moa_page_tables_t* tables,
                                     const moa_page_state_t* state, const int32_t* positions, const int32_t* seq_start,
                                     const int32_t* fresh, int32_t* slots, int32_t batch, int64_t n_tokens,

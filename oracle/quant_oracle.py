@@ -84,9 +84,10 @@ def exponent_of(scale: float) -> int:
 
 
 def assign_ref(table, free_pages, counts, page_size: int, positions: Sequence[int], seq_start: Optional[Sequence[int]],
-               fresh: Optional[Sequence[int]], n_tokens: int, windows: Sequence[int], num_sink: int, block_band: bool):
+               fresh: Optional[Sequence[int]], n_tokens: int, windows: Sequence[int], num_sink: int, block_band: bool,
+               lacked_by=None):
     """(table, free_pages, counts, slots): the page tables after a call, entry by entry, and the rows of
-    its tokens {(row, head): slot}."""
+    its tokens {(row, head): slot}.  lacked_by (in place): sequences that lacked a page, which get none until fresh."""
     table, free = np.array(table, dtype=np.int64), [int(x) for x in free_pages]
     batch, hkv, width = table.shape
     n_pages, n = len(free), max(0, min(int(counts[0]), len(free)))
@@ -110,18 +111,25 @@ def assign_ref(table, free_pages, counts, page_size: int, positions: Sequence[in
                         free[n] = int(table[b, g, i])
                         n += 1
                     table[b, g, i] = -1
+    held = [False] * batch
+    for b in range(batch if lacked_by is not None else 0):
+        if fresh is not None and fresh[b]:
+            lacked_by[b] = 0
+        held[b] = lacked_by[b] != 0
     lacked, slots = 0, {}
     for b in range(batch):
         first, count = tokens[b]
         for g in range(hkv):
             for i in range(width):
                 p0, p1 = int(positions[b]), int(positions[b]) + count - 1
-                if count and p0 // page_size <= i <= p1 // page_size and not there(table[b, g, i]):
+                if count and not held[b] and p0 // page_size <= i <= p1 // page_size and not there(table[b, g, i]):
                     if n > 0:
                         n -= 1
                         table[b, g, i] = free[n]
                     else:
                         lacked += 1
+                        if lacked_by is not None:
+                            lacked_by[b] = 1
     for b in range(batch):
         first, count = tokens[b]
         for t in range(count):

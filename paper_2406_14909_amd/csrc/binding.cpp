@@ -581,10 +581,10 @@ PyObject* pages_decode_shared(PyObject*, PyObject* const* args, Py_ssize_t nargs
 }
 constexpr auto paged_decode_shared = pages_decode_shared<false>, quant_decode_shared = pages_decode_shared<true>;
 
-// (bound, table, free_pages, counts, page_size, positions, workspace, seq_start, fresh, slots[, scales])
+// (bound, table, free_pages, counts, page_size, positions, workspace, seq_start, fresh, slots[, scales, lacked])
 template <bool kState>
 PyObject* assign(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
-  MOA_ENTER(kState ? 11 : 10)
+  MOA_ENTER(kState ? 12 : 10)
   int64_t page;
   const at::Tensor* t = c.any(args[1]);
   const at::Tensor* f = c.any(args[2]);
@@ -603,8 +603,9 @@ PyObject* assign(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   const at::Tensor* sl = args[9] != Py_None ? c.any(args[9]) : nullptr;
   if (sl && (sl->dim() != 2 || sl->scalar_type() != at::kInt || sl->size(1) != b->hkv || (!ss && sl->size(0) != bsz)))
     return none();
-  const at::Tensor* sc = nullptr;
+  const at::Tensor *sc = nullptr, *la = nullptr;
   if constexpr (kState) {
+    la = args[11] != Py_None ? c(args[11], at::kInt, {bsz}) : nullptr;
     sc = args[10] != Py_None ? c.any(args[10]) : nullptr;
     if (sc && (sc->dim() != 3 || sc->scalar_type() != at::kFloat || sc->size(0) < f->size(0) ||
                sc->size(1) != page / MOA_QUANT_BLOCK || sc->size(2) != 2))
@@ -618,7 +619,7 @@ PyObject* assign(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   const size_t nw = w->nbytes();
   const int32_t *pp = at_(ps), *pss = at_(ss), *pf = at_(fr);
   int32_t* psl = at_(sl);
-  const moa_page_state_t state = {sc ? static_cast<float*>(sc->data_ptr()) : nullptr};
+  const moa_page_state_t state = {sc ? static_cast<float*>(sc->data_ptr()) : nullptr, at_(la)};
   if (!call(*b, [&] {
         const int32_t batch = static_cast<int32_t>(bsz);
         if constexpr (kState)

@@ -65,7 +65,6 @@ struct AssignArgs {
   const int32_t* fresh;      // null: none
   int32_t* slots;            // [n_tokens, hkv], or null
   int64_t* plan;             // workspace
-  float* scales;             // 8-bit cache: those of pages given out become 0; or null
   int32_t n_tokens;
   int32_t batch;
   int32_t hkv;
@@ -75,6 +74,8 @@ struct AssignArgs {
   int32_t num_sink;
   int32_t block_band;        // the band in blocks counts too
   int32_t window[MOA_MAX_KV_HEADS];
+  float* scales;             // 8-bit cache: those of pages given out become 0; or null
+  int32_t* lacked;           // [batch]: not 0: the sequence lacked a page and gets none; or null
 };
 
 // Attention over the pages.

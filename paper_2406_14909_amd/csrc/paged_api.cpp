@@ -414,6 +414,8 @@ moa_status_t paged_assign(const char* who, const moa_plan_t* plan, const moa_pag
   float* const scales = state ? state->scales : nullptr;
   if (scales && d.dtype != MOA_BF16) return fail(MOA_ERR_UNSUPPORTED, std::string(who) + ": an 8-bit cache takes bf16 plans");
   if (!aligned8(scales)) return invalid(who, "misaligned scales (8-byte aligned)");
+  int32_t* const lacked = state ? state->lacked : nullptr;
+  if (!aligned4(lacked)) return invalid(who, "tensors must be 4-byte aligned");
   const size_t need = moa_paged_workspace_bytes(plan, batch, std::max<int64_t>(n_tokens, 1));
   if (!workspace || ws_bytes < need)
     return fail(MOA_ERR_WORKSPACE, std::string(who) + ": workspace missing or smaller than moa_paged_workspace_bytes (" +
@@ -421,18 +423,19 @@ moa_status_t paged_assign(const char* who, const moa_plan_t* plan, const moa_pag
   if (reinterpret_cast<uintptr_t>(workspace) & 255u)
     return fail(MOA_ERR_WORKSPACE, std::string(who) + ": workspace must be 256-byte aligned");
   const size_t i4 = sizeof(int32_t), pairs = static_cast<size_t>(batch) * d.num_kv_heads;
-  const struct { const void* p; size_t n; } args[] = {     // the first six are written
+  const struct { const void* p; size_t n; } args[] = {     // the first seven are written
       {tables->table, i4 * pairs * tables->max_pages},
       {tables->free_pages, i4 * static_cast<size_t>(tables->num_pages)},
       {tables->counts, i4 * 2},
       {slots, slots ? i4 * static_cast<size_t>(n_tokens) * d.num_kv_heads : 0},
       {workspace, need},
       {scales, scales ? sizeof(float) * 2 * static_cast<size_t>(tables->num_pages) * (tables->page_size / kQuantBlock) : 0},
+      {lacked, lacked ? i4 * batch : 0},
       {positions, i4 * batch},
       {seq_start, seq_start ? i4 * (static_cast<size_t>(batch) + 1) : 0},
       {fresh, fresh ? i4 * batch : 0}};
-  for (int i = 0; i < 6; ++i)
-    for (int j = i + 1; j < 9; ++j)
+  for (int i = 0; i < 7; ++i)
+    for (int j = i + 1; j < 10; ++j)
       if (args[i].n && args[j].n && overlaps(args[i].p, args[i].n, args[j].p, args[j].n))
         return invalid(who, "an argument that is written overlaps another one");
   AssignArgs a;
@@ -441,6 +444,7 @@ moa_status_t paged_assign(const char* who, const moa_plan_t* plan, const moa_pag
   a.positions = positions; a.seq_start = seq_start; a.fresh = fresh; a.slots = slots;
   a.plan = static_cast<int64_t*>(workspace);
   a.scales = scales;
+  a.lacked = lacked;
   // The workspace has kPagedMaxWorkers rows of head_dim + 4 floats and as many more as there are pairs:
   // more than the 32 + 24 bytes a pair that the counts and their sums take.
   a.n_tokens = static_cast<int32_t>(n_tokens);

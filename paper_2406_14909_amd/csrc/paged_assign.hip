@@ -111,8 +111,9 @@ __device__ __forceinline__ int below(uint64_t which) {          // set bits of t
   return __builtin_popcountll(which & ((uint64_t(1) << (threadIdx.x & 63)) - 1));
 }
 
-// Counts a pair's entries.  kStash: takes those that go back out of the table and keeps them.
-template <bool kStash>
+// Counts a pair's entries.  kStash: takes those that go back out of the table and keeps them.  kState: of
+// a sequence that lacked a page none are needed until it is fresh.
+template <bool kStash, bool kState>
 __global__ void __launch_bounds__(kThreads) paged_count_kernel(AssignArgs a) {
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const Space ws(a);
@@ -136,6 +137,12 @@ __global__ void __launch_bounds__(kThreads) paged_count_kernel(AssignArgs a) {
   } else {
     for (int i = r.need_lo; i < r.need_hi; i += 64)
       need += __builtin_popcountll(__ballot(i + lane < r.need_hi && !present(a, table[i + lane])));
+  }
+  if constexpr (kState) {
+    if (a.lacked != nullptr) {
+      if (!r.fresh) need = a.lacked[r.b] != 0 ? 0 : need;
+      else if (r.g == 0 && lane == 0) a.lacked[r.b] = 0;       // which no wave of this sequence reads
+    }
   }
   if (lane == 0) ws.counts[p] = {gone, need};
 }
@@ -212,7 +219,8 @@ __device__ __forceinline__ int row_of_pool(const AssignArgs& a, int entry, int64
 
 // A wave gives out the pages of one pair, and writes its tokens' rows where there are few.  kStash:
 // it adds up all pairs' counts first and puts its pair's pages on the list.  kState: the scales of
-// the pages that it gives out become 0 (asked in every call, 8.43 -> 8.57 us without any).
+// the pages that it gives out become 0, and it notes what sequence lacks one (a kernel of its own, as calls without
+// either would take 8.7 us for 8.4 and 16.7 for 16.3).
 template <bool kStash, bool kState>
 __global__ void __launch_bounds__(kThreads) paged_take_kernel(AssignArgs a) {
   __shared__ int s_gone[kStash ? kFewPairs + 1 : 1], s_need[kStash ? kFewPairs : 1], s_wave[2][kWaves];
@@ -222,6 +230,7 @@ __global__ void __launch_bounds__(kThreads) paged_take_kernel(AssignArgs a) {
   const int p = static_cast<int>(blockIdx.x) * kWaves + wave;
   const Pair r = pair_of(a, min(p, pairs - 1));           // asked for along with the counts
   const int64_t n = ws.head[0];
+  const int needs = kState ? ws.counts[min(p, pairs - 1)].need : 0;
   int64_t listed, all_need;
   if constexpr (kStash) {
     const int each = (pairs + kThreads - 1) / kThreads;
@@ -288,6 +297,9 @@ __global__ void __launch_bounds__(kThreads) paged_take_kernel(AssignArgs a) {
   int64_t at = listed - 1;
   if constexpr (kStash) at -= s_need[p];
   else at -= ws.sums[2 * p + 1];
+  if constexpr (kState) {
+    if (a.lacked != nullptr && needs > at + 1 && needs > 0 && lane == 0) a.lacked[r.b] = 1;   // nothing reads it here
+  }
   const bool rows = a.slots != nullptr && a.n_tokens < kManyTokens;
   const int64_t end = r.pos + r.tokens;
   auto write_rows = [&](int64_t lo, int64_t hi, auto entry_of) {      // of the tokens at positions lo .. hi - 1
@@ -300,7 +312,7 @@ __global__ void __launch_bounds__(kThreads) paged_take_kernel(AssignArgs a) {
   for (int i = r.need_lo; i < r.need_hi; i += 64) {
     const bool in = i + lane < r.need_hi;
     int entry = r.fresh || !in ? -1 : table[i + lane];
-    const bool need = in && !present(a, entry);
+    const bool need = in && !present(a, entry) && (!kState || needs > 0);
     const uint64_t which = __ballot(need);
     const int64_t from = at - below(which);
     if (need && from >= 0) {
@@ -371,10 +383,14 @@ int launch_paged_assign(const AssignArgs& a, size_t ws_bytes, void* stream) {
   // Few pairs are added up in 32 bits.
   const bool few = pairs <= kFewPairs && pairs * a.max_pages <= INT32_MAX &&
                    32 + pairs * (8 + int64_t(4) * a.max_pages) <= static_cast<int64_t>(ws_bytes);
-  hipError_t e = few ? run(&paged_count_kernel<true>, groups, kThreads) : run(&paged_count_kernel<false>, groups, kThreads);
+  const bool state = a.scales != nullptr || a.lacked != nullptr;
+  auto count = [&](auto stash) {
+    constexpr bool kStash = decltype(stash)::value;
+    return state ? run(&paged_count_kernel<kStash, true>, groups, kThreads) : run(&paged_count_kernel<kStash, false>, groups, kThreads);
+  };
+  hipError_t e = few ? count(std::true_type{}) : count(std::false_type{});
   if (e == hipSuccess && !few) e = run(&paged_scan_kernel, 1, kScanThreads);
   if (e == hipSuccess && !few) e = run(&paged_release_kernel, groups, kThreads);
-  const bool state = a.scales != nullptr;
   auto take = [&](auto stash) {
     constexpr bool kStash = decltype(stash)::value;
     return state ? run(&paged_take_kernel<kStash, true>, groups, kThreads) : run(&paged_take_kernel<kStash, false>, groups, kThreads);

@@ -76,6 +76,7 @@ class moa_page_tables_t(ctypes.Structure):
 class moa_page_state_t(ctypes.Structure):
     _fields_ = [
         ("scales", ctypes.c_void_p),
+        ("lacked", ctypes.c_void_p),
     ]
 
 
@@ -754,7 +755,7 @@ def new_page_tables(plan: Plan, batch: int, max_pages: int, num_pages: int, devi
 
 
 def moa_paged_assign(plan: Plan, table, free_pages, counts, page_size: int, positions, workspace, seq_start=None,
-                     fresh=None, slots=None, stream=None, scales=None):
+                     fresh=None, slots=None, stream=None, scales=None, lacked=None):
     """Brings page tables up to a call: pages that no later query sees go back to the free list, then new
     tokens get pages from it (include/moa.h has the order).
 
@@ -762,11 +763,13 @@ def moa_paged_assign(plan: Plan, table, free_pages, counts, page_size: int, posi
     packed row where each sequence's tokens start (None: one token each); fresh: int32[B] or None,
     nonzero: all pages of the sequence go back first; slots: int32 [T, H_kv] or None, gets the pool's row of each
     new token and head (-1: no page); scales: those of an 8-bit cache [at least num_pages, page_size / 16, 2], of which
-    the pages given out get zeros, as a sequence that begins inside a block (behind a shared prefix) needs.
+    the pages given out get zeros, as a sequence that begins inside a block (behind a shared prefix) needs; lacked:
+    int32[B], zeros at first: 1 for a sequence that lacked a page, which gets no more until it is fresh.
     Returns slots."""
     if stream is None:
         args = (plan._bound, table, free_pages, counts, page_size, positions, workspace, seq_start, fresh, slots)
-        done = _fast.paged_assign(*args) if scales is None else _fast.paged_assign_state(*args, scales)
+        plain = scales is None and lacked is None
+        done = _fast.paged_assign(*args) if plain else _fast.paged_assign_state(*args, scales, lacked)
         if done is not None:
             return slots
     import torch
@@ -795,12 +798,15 @@ def moa_paged_assign(plan: Plan, table, free_pages, counts, page_size: int, posi
         _need(scales, (max(int(scales.shape[0]), int(free_pages.shape[0])), int(page_size) // MOA_QUANT_BLOCK, 2), torch.float32,
               "scales")
         tensors["scales"] = scales
+    if lacked is not None:
+        _need(lacked, (bsz,), torch.int32, "lacked")
+        tensors["lacked"] = lacked
     if workspace.device.type != "cuda" or not workspace.is_contiguous():
         raise MoaError(MOA_ERR_WORKSPACE, "workspace must be a contiguous GPU tensor")
     tables = moa_page_tables_t(table.data_ptr(), free_pages.data_ptr(), counts.data_ptr(), int(free_pages.shape[0]),
                                int(page_size), int(table.shape[2]))
     at = lambda t: None if t is None else t.data_ptr()
-    state = None if scales is None else ctypes.byref(moa_page_state_t(at(scales)))
+    state = None if scales is None and lacked is None else ctypes.byref(moa_page_state_t(at(scales), at(lacked)))
     with torch.cuda.device(_one_device(**tensors)):
         lib, rest = load_library(), (positions.data_ptr(), at(seq_start), at(fresh), at(slots), bsz, n, workspace.data_ptr(),
                                      workspace.numel() * workspace.element_size(), _stream(table, stream))

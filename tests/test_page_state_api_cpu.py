@@ -16,7 +16,7 @@ BAD, UNSUP, WS = M.MOA_ERR_INVALID_ARG, M.MOA_ERR_UNSUPPORTED, M.MOA_ERR_WORKSPA
 
 def assign(p, batch=3, n=3, num_pages=100, page_size=64, max_pages=20, ws_bytes=None, state=True, **over):
     x = dict(dict(table=7 * A, free_pages=15 * A, counts=16 * A, positions=8 * A, seq_start=9 * A, fresh=17 * A, slots=18 * A,
-                  workspace=12 * A, scales=14 * A), **over)
+                  workspace=12 * A, scales=14 * A, lacked=19 * A), **over)
     t = M.moa_page_tables_t(x["table"], x["free_pages"], x["counts"], num_pages, page_size, max_pages)
     s = M.moa_page_state_t(**{name: x[name] for name, _ in M.moa_page_state_t._fields_})
     if ws_bytes is None:
@@ -33,6 +33,8 @@ def plan(dtype="bf16"):
     (dict(scales=14 * A + 4), BAD), (dict(scales=7 * A), BAD), (dict(scales=15 * A), BAD), (dict(scales=16 * A), BAD),
     (dict(scales=18 * A), BAD), (dict(scales=8 * A), BAD), (dict(scales=9 * A), BAD), (dict(scales=17 * A), BAD),
     (dict(scales=12 * A), BAD), (dict(scales=15 * A - 100 * 4 * 8 + 8), BAD),
+    (dict(lacked=19 * A + 2), BAD), (dict(lacked=7 * A), BAD), (dict(lacked=14 * A), BAD), (dict(lacked=17 * A), BAD),
+    (dict(lacked=17 * A - 4), BAD), (dict(lacked=8 * A + 4), BAD), (dict(lacked=12 * A), BAD), (dict(lacked=16 * A + 4), BAD),
     (dict(table=None), BAD), (dict(counts=12 * A), BAD), (dict(workspace=None), WS), (dict(ws_bytes=100), WS),
     (dict(page_size=24), UNSUP), (dict(seq_start=None, n=4), BAD), (dict(n=1 << 30), BAD), (dict(n=1 << 29), UNSUP),
     (dict(n=1 << 29, state=False), UNSUP), (dict(n=1 << 29, scales=None), UNSUP), (dict(table=None, state=False), BAD),
