@@ -307,7 +307,7 @@ moa_status_t moa_rule_loss(const float* ebar, int32_t num_heads, int64_t n, int3
  * [batch + 1]) is non-decreasing; rows in front of seq_start[0] and from
  * seq_start[batch] on belong to no sequence and are left as they were in o and
  * q_out.  A sequence whose rows are not all within [0, n_tokens) has none in
- * moa_paged_prefill.  A negative positions[b] leaves sequence b's rows and pages
+ * moa_paged_prefill and moa_paged_assign; the appends store those of its rows that are.  A negative positions[b] leaves sequence b's rows and pages
  * as they were.  table and positions live on the device, so a captured graph replays
  * with their present contents.
  *
@@ -425,7 +425,8 @@ typedef struct {
  * left as they were.
  * A page may stand in one entry only: pages of a shared prefix belong in prefix tables
  * (moa_paged_decode_shared), which this call does not touch.  The workspace is as in
- * the attention calls (moa_paged_workspace_bytes).  The result does not depend on the
+ * the attention calls (moa_paged_workspace_bytes).  n_tokens is that of the append that follows,
+ * with slots or without: it says which sequences have rows.  The result does not depend on the
  * launch order.  1 <= batch <= 65535, 0 <= n_tokens < 2^30. */
 moa_status_t moa_paged_assign(const moa_plan_t* plan, const moa_page_tables_t* tables, const int32_t* positions,
                               const int32_t* seq_start, const int32_t* fresh, int32_t* slots, int32_t batch,

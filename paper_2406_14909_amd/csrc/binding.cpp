@@ -581,10 +581,10 @@ PyObject* pages_decode_shared(PyObject*, PyObject* const* args, Py_ssize_t nargs
 }
 constexpr auto paged_decode_shared = pages_decode_shared<false>, quant_decode_shared = pages_decode_shared<true>;
 
-// (bound, table, free_pages, counts, page_size, positions, workspace, seq_start, fresh, slots[, scales, lacked])
+// (bound, table, free_pages, counts, page_size, positions, workspace, seq_start, fresh, slots[, scales, lacked, n_tokens])
 template <bool kState>
 PyObject* assign(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
-  MOA_ENTER(kState ? 12 : 10)
+  MOA_ENTER(kState ? 13 : 10)
   int64_t page;
   const at::Tensor* t = c.any(args[1]);
   const at::Tensor* f = c.any(args[2]);
@@ -604,7 +604,9 @@ PyObject* assign(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   if (sl && (sl->dim() != 2 || sl->scalar_type() != at::kInt || sl->size(1) != b->hkv || (!ss && sl->size(0) != bsz)))
     return none();
   const at::Tensor *sc = nullptr, *la = nullptr;
+  int64_t n = sl ? sl->size(0) : (int64_t(1) << 30) - 1;
   if constexpr (kState) {
+    if (args[12] != Py_None && (sl || !as_int(args[12], &n))) return none();
     la = args[11] != Py_None ? c(args[11], at::kInt, {bsz}) : nullptr;
     sc = args[10] != Py_None ? c.any(args[10]) : nullptr;
     if (sc && (sc->dim() != 3 || sc->scalar_type() != at::kFloat || sc->size(0) < f->size(0) ||
@@ -614,7 +616,6 @@ PyObject* assign(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   if (!c.done() || bsz > INT32_MAX || mp > INT32_MAX) return none();
   auto at_ = [](const at::Tensor* x) { return x ? static_cast<int32_t*>(x->data_ptr()) : nullptr; };
   const moa_page_tables_t tables = {at_(t), at_(f), at_(n2), f->size(0), static_cast<int32_t>(page), static_cast<int32_t>(mp)};
-  const int64_t n = sl ? sl->size(0) : (int64_t(1) << 30) - 1;
   void *pw = w->data_ptr(), *s = c.stream();
   const size_t nw = w->nbytes();
   const int32_t *pp = at_(ps), *pss = at_(ss), *pf = at_(fr);

@@ -755,7 +755,7 @@ def new_page_tables(plan: Plan, batch: int, max_pages: int, num_pages: int, devi
 
 
 def moa_paged_assign(plan: Plan, table, free_pages, counts, page_size: int, positions, workspace, seq_start=None,
-                     fresh=None, slots=None, stream=None, scales=None, lacked=None):
+                     fresh=None, slots=None, stream=None, scales=None, lacked=None, n_tokens=None):
     """Brings page tables up to a call: pages that no later query sees go back to the free list, then new
     tokens get pages from it (include/moa.h has the order).
 
@@ -764,12 +764,13 @@ def moa_paged_assign(plan: Plan, table, free_pages, counts, page_size: int, posi
     nonzero: all pages of the sequence go back first; slots: int32 [T, H_kv] or None, gets the pool's row of each
     new token and head (-1: no page); scales: those of an 8-bit cache [at least num_pages, page_size / 16, 2], of which
     the pages given out get zeros, as a sequence that begins inside a block (behind a shared prefix) needs; lacked:
-    int32[B], zeros at first: 1 for a sequence that lacked a page, which gets no more until it is fresh.
-    Returns slots."""
+    int32[B], zeros at first: 1 for a sequence that lacked a page, which gets no more until it is fresh;
+    n_tokens: packed rows of the append that follows, where slots do not tell: a sequence with rows outside them gets
+    no pages (None without slots: as many rows as there can be).  Returns slots."""
     if stream is None:
         args = (plan._bound, table, free_pages, counts, page_size, positions, workspace, seq_start, fresh, slots)
-        plain = scales is None and lacked is None
-        done = _fast.paged_assign(*args) if plain else _fast.paged_assign_state(*args, scales, lacked)
+        plain = scales is None and lacked is None and n_tokens is None
+        done = _fast.paged_assign(*args) if plain else _fast.paged_assign_state(*args, scales, lacked, n_tokens)
         if done is not None:
             return slots
     import torch
@@ -793,6 +794,10 @@ def moa_paged_assign(plan: Plan, table, free_pages, counts, page_size: int, posi
         n = int(slots.shape[0])
         _need(slots, (n if seq_start is not None else bsz, plan.num_kv_heads), torch.int32, "slots")
         tensors["slots"] = slots
+    if n_tokens is not None:
+        if slots is not None and int(n_tokens) != n:
+            raise MoaError(MOA_ERR_INVALID_ARG, f"n_tokens: slots have {n} rows, not {n_tokens}")
+        n = int(n_tokens)
     if scales is not None:
         _need_rank(scales, 3, "scales")
         _need(scales, (max(int(scales.shape[0]), int(free_pages.shape[0])), int(page_size) // MOA_QUANT_BLOCK, 2), torch.float32,
