@@ -70,8 +70,7 @@ struct Walk {
 
 // Calls seg(b, g, keys, x0, x1, whole, pair) for each cache that this worker's piece
 // touches: visible keys [x0, x1) of KV head g of sequence b, `whole` when these are all.
-// Work-group uniform; every thread takes part.  kStarts: of at least as many caches as workers, of
-// two rounds or more on average, each also costs a round in front of its own, for its start.
+// Work-group uniform; every thread takes part.  kStarts: starts count in the split (paged_start_rounds).
 template <bool kStarts = false, class Seg>
 __device__ __forceinline__ void for_each_piece(const PagedArgs& a, Walk& s, uint32_t w, int round_shift, Seg&& seg) {
   const int pairs = a.batch * a.hkv;
@@ -109,7 +108,7 @@ __device__ __forceinline__ void for_each_piece(const PagedArgs& a, Walk& s, uint
     longest = max(longest, s.wave_max[v]);
   }
   before += incl - sum;
-  const uint32_t start = kStarts && pairs >= a.slots && units >= 2 * static_cast<uint32_t>(pairs) ? 1 : 0;
+  const uint32_t start = kStarts ? paged_start_rounds(units, pairs, a.slots) : 0;
   if (start > 0) {
     units += pairs;
     longest += 1;
@@ -151,10 +150,10 @@ __device__ __forceinline__ void for_each_piece(const PagedArgs& a, Walk& s, uint
       const VisibleKeys keys = keys_of(a, pos, g);
       const uint32_t lo = x - at, hi = min(n, lo + (x_end - x));
       if (lo == 0 && threadIdx.x == 0) a.plan[kPlanHead + pair] = static_cast<int32_t>(at);
-      const uint32_t first = max(lo, start) - start, last = max(hi, start) - start;    // rounds of keys
-      if (last > 0)
-        seg(b, g, keys, static_cast<int>(first << round_shift),
-            static_cast<int>(min(static_cast<uint32_t>(keys.count), last << round_shift)), lo <= start && hi == n, pair);
+      const PagedPart part(lo, hi, n, start);
+      if (part.last > 0)
+        seg(b, g, keys, static_cast<int>(part.first << round_shift),
+            static_cast<int>(min(static_cast<uint32_t>(keys.count), part.last << round_shift)), part.whole, pair);
       x += hi - lo;
       if (x >= x_end) break;
     }

@@ -43,6 +43,21 @@ MOA_PAGED_FN uint32_t paged_rounds(int32_t pos, int32_t count, int round_shift, 
   return n == 0 && !merge_writes ? 1 : n;
 }
 
+// Rounds that each cache's start counts as, in front of its own: of at least as many caches as workers, of two
+// rounds or more on average, one, as workers would else differ in starts.
+MOA_PAGED_FN uint32_t paged_start_rounds(uint32_t units, uint32_t pairs, uint32_t slots) {
+  return pairs >= slots && units >= 2 * pairs ? 1 : 0;
+}
+
+// Of a cache of n rounds, `start` of them its start: what a piece that has rounds [lo, hi) of them
+// reads, rounds [first, last) of the keys (none where it has the start alone), and whether that is all.
+struct PagedPart {
+  uint32_t first, last;
+  bool whole;
+  MOA_PAGED_FN PagedPart(uint32_t lo, uint32_t hi, uint32_t n, uint32_t start)
+      : first((lo > start ? lo : start) - start), last((hi > start ? hi : start) - start), whole(lo <= start && hi == n) {}
+};
+
 // A cache's pages in the order of its visible keys: those of the sinks, then those of
 // the band (one of them may be in both).
 struct VisiblePages {
