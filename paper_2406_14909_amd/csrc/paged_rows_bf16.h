@@ -6,7 +6,7 @@
 // the query heads that use it, and a short chunk or a batch of single tokens fills a tile of
 // 128 rows.  What bounds it: in long prompts the matrix units and the board's power (32 heads,
 // 16,384 tokens of 2 sequences: 849 us, 890 TFLOP/s, matrix units busy 41 % at 1.8 GHz; 6 chunks of
-// 8 x 4 heads behind up to 16,000: 259 us, 652 TFLOP/s), memory and the chain of tiles where rows are few.
+// 8 x 4 heads behind up to 16,000: 254 to 261 us, 647 to 664 TFLOP/s), memory and the chain of tiles where rows are few.
 // Key tiles of few row tiles are cut into pieces for other work-groups (paged_rows.h).
 //
 // One work-group = 4 waves of 32 rows over the same 64-key tiles, which it stages in LDS by

@@ -1,7 +1,7 @@
 // New tokens into an 8-bit paged cache, with the rotation of their positions on the way.
 //
-// Rotation as in paged_append.hip, with sines and cosines to fp64 (a code is a rounding to four
-// bits, so that a key next to a border would else be another code than its definition's).
+// Rotation as in paged_append.hip, with sines and cosines formed in fp64 and rounded to fp32 (a code is a
+// rounding to four bits, so that a key next to a border would else be another code than its definition's).
 // Then, for the new tokens x of each block of 16 positions of each head, keys and values apart:
 //   e = the smallest integer with max |x| <= 448 * 2^e, code = e4m3(x * 2^-e),
 // and in a block that is entered behind its first position no less than the stored e; where

@@ -12,7 +12,6 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kQuantLowest = -117, kQuantHighest = 119;    // exponents of scales: every number is a normal fp32 and bf16
 constexpr float kQuantMost = 448.0f;                        // the largest e4m3 number
-constexpr uint32_t kQuantNan = 0x7f;
 
 // Eight e4m3 numbers times a power of two in bf16, without rounding (one instruction per pair;
 // checked on gfx950 for every code at ten scales from the least to the largest: only the exponent bits of the scale count).

@@ -4,13 +4,14 @@
 // one after the other, at 3,600 cycles each (48 sequences x 8 heads x 8 query heads over 32,700 shared
 // keys and up to 1,000 of their own: 41 us, 7 of them the merge; 46 with the kinds in turns).  More and
 // shorter pieces, or more work-groups for either kind, help some batches and cost others (sequences x KV heads x
-// query heads of each on a prefix, with up to so many keys of their own; work-groups for prefix and own keys; us):
+// query heads of each on a prefix, with up to so many keys of their own; work-groups for prefix and own keys; us of
+// passes over two sets of inputs in turn, where the first call takes 43 for the 41 of more sets):
 //                                   256 + 256   320 + 192   192 + 320   256 + 384
-//   48 x 8 x 8 on 32,700, 1,000          44.3        47.6        50.1        48.5
-//   16 x 8 x 4 on 8,001, 500             16.5        16.5        16.5        16.5
-//   16 x 32 x 1 on 8,001, 500            25.9        29.5        25.8        31.2
-//   48 x 32 x 1 on 8,001, 1,500           105         131          97         100    (92 since starts count)
-//   32 x 8 x 4 on 2,000, 4,000           29.3        33.0        28.2        26.8
+//   48 x 8 x 8 on 32,700, 1,000          43.2        44.5        48.9        47.3
+//   16 x 8 x 4 on 8,001, 500             19.8        19.9        21.1        20.0
+//   16 x 32 x 1 on 8,001, 500            37.4        32.6        42.6        37.4
+//   48 x 32 x 1 on 8,001, 1,500          90.7       109.5        92.6       101.3
+//   32 x 8 x 4 on 2,000, 4,000           38.4        42.8        42.1        37.1
 #include "paged_rows_bf16.h"
 #include "quant_decode.h"
 
