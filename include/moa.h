@@ -307,9 +307,10 @@ moa_status_t moa_rule_loss(const float* ebar, int32_t num_heads, int64_t n, int3
  * [batch + 1]) is non-decreasing; rows in front of seq_start[0] and from
  * seq_start[batch] on belong to no sequence and are left as they were in o and
  * q_out.  A sequence whose rows are not all within [0, n_tokens) has none in
- * moa_paged_prefill and moa_paged_assign; the appends store those of its rows that are.  A negative positions[b] leaves sequence b's rows and pages
- * as they were.  table and positions live on the device, so a captured graph replays
- * with their present contents.
+ * moa_paged_prefill and moa_paged_assign; the appends store those of its rows that
+ * are.  A negative positions[b] leaves sequence b's rows and pages as they were.
+ * table and positions live on the device, so a captured graph replays with their
+ * present contents.
  *
  * A query at position p of head g sees the keys j <= p with j < s or in its band,
  * token-exact in the two decode calls and, with MOA_BLOCK_BAND, in blocks in
